@@ -339,6 +339,89 @@ fp8_status fp8_gemm_splitk(const fp8_gemm_desc* d, const uint8_t* A, const uint8
                            void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /*
+ * Fused epilogues — Sections 2 and 4.1: what surrounds the matrix multiplies of a transformer layer (bias, activation,
+ * residual addition, the gate of a gated feed-forward block) is applied to the binary32 dot products before they leave
+ * the chip, and the result is stored in a wider type or converted to FP8 on the way out.
+ *
+ * What a result is stored as: a wide type, or FP8 codes  encode(v * scale_d)  by the rules of fp8_quantize.
+ */
+typedef enum { FP8_STORE_F32 = 0, FP8_STORE_BF16 = 1, FP8_STORE_E4M3 = 2, FP8_STORE_E5M2 = 3 } fp8_store;
+/*
+ * Activations: relu max(z,0); gelu z*Phi(z) with the normal distribution function Phi; gelu_tanh
+ * z*(1 + tanh(sqrt(2/pi)*(z + 0.044715 z^3)))/2; silu z/(1 + exp(-z)).  Computed in binary32; at -inf they are 0 (their
+ * limit), NaN stays NaN.  The derivative of relu at 0 is 0.
+ */
+typedef enum { FP8_ACT_NONE = 0, FP8_ACT_RELU = 1, FP8_ACT_GELU = 2, FP8_ACT_GELU_TANH = 3, FP8_ACT_SILU = 4 } fp8_activation;
+
+/*
+ * fp8_gemm_epilogue — the product of fp8_gemm with bias, activation and residual:
+ *   z[i,j] = (sum_k decode_fa(A[i,k]) * decode_fb(B[k,j])) * (sa_inv * sb_inv) + bias[j]
+ *   v[i,j] = act(z[i,j]) + residual[i,j]                       (all in binary32)
+ *   D[i,j] = v rounded to the wide type, or encode(v * scale_d)
+ *   pre[i,j] = z rounded to pre_t: what fp8_epilogue_backward reads
+ *   *amax_d_dev = amax of D as stored (wide types), of v before scaling and conversion (FP8); as the other products.
+ * d->out is ignored (e->store names the type).  In *e, NULL leaves a part out: bias (N elements), residual (M x N, pitch
+ * ldr), pre (M x N, pitch ldp), scale_inv_b_vec_dev (N floats, one inverse scale per column of B, taken in place of
+ * scale_inv_b_dev, which may then be NULL).  scale_d_dev is required for the FP8 stores.  residual may be D itself (same
+ * address, pitch and type), otherwise the written matrices overlap nothing.
+ * bias needs the alignment of its type; residual, pre and D are 16-byte aligned with pitches that are multiples of 16
+ * bytes (FP8_ERR_ALIGN); pitches at least N (FP8_ERR_SHAPE).  K == 0 is an empty sum: z = bias.  M*N == 0 is a no-op
+ * (amax = 0).  `acc` is accepted as by fp8_gemm; partial sums are added in registers in both of its values where the
+ * kernel for few rows is taken.
+ */
+typedef struct {
+    fp8_activation act;
+    fp8_store store;
+    fp8_overflow overflow;
+    fp8_wide bias_t, residual_t, pre_t;
+    const float* scale_inv_b_vec_dev;
+    const void* bias;
+    const void* residual;
+    void* pre;
+    int64_t ldr, ldp;
+} fp8_epilogue;
+
+fp8_status fp8_gemm_epilogue(const fp8_gemm_desc* d, const fp8_epilogue* e, const uint8_t* A, const uint8_t* B, void* D,
+                             const float* scale_inv_a_dev, const float* scale_inv_b_dev, const float* scale_d_dev,
+                             float* amax_d_dev, void* stream);
+
+/*
+ * fp8_gemm_gated — the two up projections of a gated feed-forward block, the activation and the product, in one kernel:
+ *   g = (A . Bg) * (sa_inv * sbg_inv),  u = (A . Bu) * (sa_inv * sbu_inv),  h = act(g) * u      (binary32)
+ *   H = h rounded to the wide type, or encode(h * scale_h);  amax as fp8_gemm_epilogue.
+ *   d         M, N, K of ONE projection (N = the block's inner width), formats, layouts, ldb of both B operands, ldd of H.
+ *   w->gate, w->up   both or neither: M x N, pitch ldg, OVERWRITTEN with g and u rounded to gate_t, for the backward pass.
+ * The two B operands may be halves of one matrix ([K, 2N] or [2N, K]): ldb is its pitch.
+ * Alignment and special cases as fp8_gemm_epilogue (K == 0 gives g = u = 0).
+ */
+typedef struct {
+    fp8_activation act;
+    fp8_store store;
+    fp8_overflow overflow;
+    fp8_wide gate_t;
+    void* gate;
+    void* up;
+    int64_t ldg;
+} fp8_gated;
+
+fp8_status fp8_gemm_gated(const fp8_gemm_desc* d, const fp8_gated* w, const uint8_t* A, const uint8_t* Bg, const uint8_t* Bu, void* H,
+                          const float* scale_inv_a_dev, const float* scale_inv_bg_dev, const float* scale_inv_bu_dev,
+                          const float* scale_h_dev, float* amax_h_dev, void* stream);
+
+/*
+ * fp8_gemm_gated_backward — the data gradient of the down projection and the derivative of the gate in one kernel; the
+ * gradient of h never reaches memory:
+ *   dh = (A . B) * (sa_inv * sb_inv)           A = dY codes (M x K), B = the down weights as K x N, N = the inner width
+ *   dG = dh * u * act'(g),  dU = dh * act(g)   g, u = w->gate, w->up as fp8_gemm_gated stored them (read)
+ * stored as wide values or as encode(. * scale_d): ONE scale and one amax for both, so that [dG | dU] can be the two halves
+ * of one M x 2N tensor of pitch ldd, the operand of the two remaining products (dX = [dG|dU] . [Bg|Bu]^T and
+ * d[Bg|Bu] = X^T . [dG|dU], both fp8_gemm).  *amax_dev covers both.
+ */
+fp8_status fp8_gemm_gated_backward(const fp8_gemm_desc* d, const fp8_gated* w, const uint8_t* A, const uint8_t* B, void* dG, void* dU,
+                                   const float* scale_inv_a_dev, const float* scale_inv_b_dev, const float* scale_d_dev,
+                                   float* amax_dev, void* stream);
+
+/*
  * fp8_async_status — reads and clears the device-side error latch of the
  * current device (synchronises the device).  FP8_OK, or FP8_ERR_TIMEOUT if a
  * kernel gave up on a bounded wait since the last call; *detail (optional, host

@@ -19,12 +19,15 @@ F32, BF16 = 0, 1             # fp8_wide
 SATURATE, NOSAT = 0, 1       # fp8_overflow
 MAJOR_K, MAJOR_MN = 0, 1     # fp8_major
 ACC_SPLIT, ACC_FAST = 0, 1    # fp8_accumulate: bounded error for any data (default) / one accumulator
+STORE_F32, STORE_BF16, STORE_E4M3, STORE_E5M2 = 0, 1, 2, 3                       # fp8_store
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4            # fp8_activation
 
 EXPORTS = ["fp8_amax", "fp8_scale_from_amax", "fp8_quantize", "fp8_quantize_current",
            "fp8_quantize_current_workspace_bytes", "fp8_quantize_current_static", "fp8_dequantize", "fp8_fake_quantize",
            "fp8_scale_pow2_from_amax", "fp8_gemm", "fp8_gemm_fp8out", "fp8_amax_channels", "fp8_scales_from_amax",
            "fp8_quantize_channels", "fp8_quantize_transpose", "fp8_gemm_channel_scales", "fp8_gemm_batched",
            "fp8_gemm_splitk", "fp8_gemm_splitk_workspace",
+           "fp8_gemm_epilogue", "fp8_gemm_gated", "fp8_gemm_gated_backward",
            "fp8_async_status", "fp8_self_test_expire_wait", "fp8_sm_clock_probe", "fp8_status_string", "fp8_launch_count"]
 
 
@@ -36,6 +39,17 @@ class GemmDesc(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
                 ("fa", ctypes.c_int), ("fb", ctypes.c_int), ("ma", ctypes.c_int), ("mb", ctypes.c_int),
                 ("lda", ctypes.c_int64), ("ldb", ctypes.c_int64), ("ldd", ctypes.c_int64), ("out", ctypes.c_int), ("acc", ctypes.c_int)]
+
+
+class Epilogue(ctypes.Structure):
+    _fields_ = [("act", ctypes.c_int), ("store", ctypes.c_int), ("overflow", ctypes.c_int), ("bias_t", ctypes.c_int),
+                ("residual_t", ctypes.c_int), ("pre_t", ctypes.c_int), ("scale_inv_b_vec", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("pre", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("ldp", ctypes.c_int64)]
+
+
+class Gated(ctypes.Structure):
+    _fields_ = [("act", ctypes.c_int), ("store", ctypes.c_int), ("overflow", ctypes.c_int), ("gate_t", ctypes.c_int),
+                ("gate", ctypes.c_void_p), ("up", ctypes.c_void_p), ("ldg", ctypes.c_int64)]
 
 
 _lib = None
@@ -100,6 +114,12 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.fp8_gemm_splitk_workspace.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(ctypes.c_int), ctypes.POINTER(sz)]
     lib.fp8_gemm_splitk.restype = i32
     lib.fp8_gemm_splitk.argtypes = [ctypes.POINTER(GemmDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.fp8_gemm_epilogue.restype = i32
+    lib.fp8_gemm_epilogue.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Epilogue), vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fp8_gemm_gated.restype = i32
+    lib.fp8_gemm_gated.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Gated), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fp8_gemm_gated_backward.restype = i32
+    lib.fp8_gemm_gated_backward.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Gated), vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.fp8_async_status.restype = i32
     lib.fp8_async_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     lib.fp8_self_test_expire_wait.restype = i32
@@ -369,6 +389,107 @@ def fp8_gemm_batched(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int
     _check(load().fp8_gemm_batched(ctypes.byref(d), batch, A.data_ptr(), A.stride(0), B.data_ptr(), B.stride(0),
                                    D.data_ptr(), D.stride(0), _scalar(scale_inv_a, "scale_inv_a"), _scalar(scale_inv_b, "scale_inv_b"),
                                    None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()), "fp8_gemm_batched")
+
+
+def _wide2d(t: torch.Tensor, shape, name: str) -> int:
+    """fp8_wide of a 2-D float32 or bfloat16 CUDA tensor of the given shape with unit inner stride"""
+    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be a 2-D tensor of shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_cuda or t.stride(1) != 1:
+        raise ValueError("%s must be a CUDA tensor with unit inner stride" % name)
+    return _wide_of(t)
+
+
+def _store_of(D: torch.Tensor, fd: int | None, scale_d: torch.Tensor | None) -> tuple[int, int | None]:
+    """(fp8_store, address of the output scale) of an output tensor: wide, or uint8 codes of format fd"""
+    if D.dtype == torch.uint8:
+        if fd is None or scale_d is None:
+            raise TypeError("a uint8 output needs its format fd and its scale_d")
+        if fd not in (E4M3, E5M2):
+            raise Fp8Error("fd must be E4M3 or E5M2, got %r" % (fd,))
+        return STORE_E4M3 + fd, _scalar(scale_d, "scale_d")
+    if fd is not None or scale_d is not None:
+        raise TypeError("fd and scale_d go with a uint8 output, not %s" % D.dtype)
+    return _wide_of(D), None
+
+
+def fp8_gemm_epilogue(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int, mb: int, D: torch.Tensor,
+                      scale_inv_a: torch.Tensor, scale_inv_b: torch.Tensor, act: int = ACT_NONE, bias: torch.Tensor | None = None,
+                      residual: torch.Tensor | None = None, pre: torch.Tensor | None = None, fd: int | None = None,
+                      scale_d: torch.Tensor | None = None, amax_out: torch.Tensor | None = None, overflow: int = SATURATE,
+                      acc: int = ACC_SPLIT) -> None:
+    """D = act((A . B) * scale_inv_a * scale_inv_b + bias) + residual, one kernel.  Operands as fp8_gemm; ``scale_inv_b``
+    has one element or one per column of B.  D is float32, bfloat16, or uint8 codes of format ``fd`` made with ``scale_d``.
+    ``pre`` (wide) receives the value before the activation, which fp8_epilogue_backward reads."""
+    codes = D.dtype == torch.uint8
+    d = _gemm_desc_2d(A, ma, B, mb, D, fa, fb, acc, codes_out=codes)
+    store, scale_d_ptr = _store_of(D, fd, scale_d)
+    e = Epilogue(act, store, overflow)
+    if scale_inv_b.numel() == 1:
+        sb = _scalar(scale_inv_b, "scale_inv_b")
+    else:
+        sb, e.scale_inv_b_vec = None, _vec(scale_inv_b, d.N, "scale_inv_b")
+    if bias is not None:
+        if bias.numel() != d.N:
+            raise ValueError("bias must have %d elements" % d.N)
+        e.bias_t, e.bias = _wide_of(bias), _dev(bias, "bias")
+    if residual is not None:
+        e.residual_t, e.residual, e.ldr = _wide2d(residual, D.shape, "residual"), residual.data_ptr(), residual.stride(0)
+    if pre is not None:
+        e.pre_t, e.pre, e.ldp = _wide2d(pre, D.shape, "pre"), pre.data_ptr(), pre.stride(0)
+    _check(load().fp8_gemm_epilogue(ctypes.byref(d), ctypes.byref(e), A.data_ptr(), B.data_ptr(), D.data_ptr(),
+                                    _scalar(scale_inv_a, "scale_inv_a"), sb, scale_d_ptr,
+                                    None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()), "fp8_gemm_epilogue")
+
+
+def _gate_of(gate, up, shape, act, store, overflow) -> Gated:
+    w = Gated(act, store, overflow)
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up go together")
+    if gate is not None:
+        w.gate_t, w.gate, w.up, w.ldg = _wide2d(gate, shape, "gate"), gate.data_ptr(), up.data_ptr(), gate.stride(0)
+        if _wide2d(up, shape, "up") != w.gate_t or up.stride(0) != gate.stride(0):
+            raise ValueError("gate and up must have one dtype and one row pitch")
+    return w
+
+
+def fp8_gemm_gated(A: torch.Tensor, fa: int, ma: int, Bg: torch.Tensor, Bu: torch.Tensor, fb: int, mb: int, H: torch.Tensor,
+                   scale_inv_a: torch.Tensor, scale_inv_bg: torch.Tensor, scale_inv_bu: torch.Tensor, act: int = ACT_SILU,
+                   gate: torch.Tensor | None = None, up: torch.Tensor | None = None, fd: int | None = None,
+                   scale_d: torch.Tensor | None = None, amax_out: torch.Tensor | None = None, overflow: int = SATURATE,
+                   acc: int = ACC_SPLIT) -> None:
+    """H = act((A . Bg) * sa * sbg) * ((A . Bu) * sa * sbu), one kernel.  Bg and Bu have one shape, layout and row pitch
+    (they may be the halves of one matrix); H as D of fp8_gemm_epilogue; ``gate`` and ``up`` (wide, optional) receive the
+    two products for the backward pass."""
+    if Bg.shape != Bu.shape or Bg.stride() != Bu.stride() or Bu.dtype != Bg.dtype or not Bu.is_cuda:
+        raise ValueError("Bg and Bu must be CUDA tensors of one dtype, one shape and one row pitch")
+    d = _gemm_desc_2d(A, ma, Bg, mb, H, fa, fb, acc, codes_out=H.dtype == torch.uint8)
+    store, scale_d_ptr = _store_of(H, fd, scale_d)
+    w = _gate_of(gate, up, H.shape, act, store, overflow)
+    _check(load().fp8_gemm_gated(ctypes.byref(d), ctypes.byref(w), A.data_ptr(), Bg.data_ptr(), Bu.data_ptr(), H.data_ptr(),
+                                 _scalar(scale_inv_a, "scale_inv_a"), _scalar(scale_inv_bg, "scale_inv_bg"),
+                                 _scalar(scale_inv_bu, "scale_inv_bu"), scale_d_ptr,
+                                 None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()), "fp8_gemm_gated")
+
+
+def fp8_gemm_gated_backward(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int, mb: int, gate: torch.Tensor, up: torch.Tensor,
+                            dG: torch.Tensor, dU: torch.Tensor, scale_inv_a: torch.Tensor, scale_inv_b: torch.Tensor,
+                            act: int = ACT_SILU, fd: int | None = None, scale_d: torch.Tensor | None = None,
+                            amax_out: torch.Tensor | None = None, overflow: int = SATURATE, acc: int = ACC_SPLIT) -> None:
+    """dh = (A . B) * sa * sb with A the codes of dY and B the down weights seen as [d_model, inner];
+    dG = dh * up * act'(gate), dU = dh * act(gate): two outputs of one dtype and row pitch (halves of one [M, 2 N] tensor),
+    converted with one ``scale_d`` and covered by one ``amax_out``."""
+    if dG.shape != dU.shape or dG.stride() != dU.stride() or dG.dtype != dU.dtype or not dU.is_cuda:
+        raise ValueError("dG and dU must be CUDA tensors of one dtype, one shape and one row pitch")
+    d = _gemm_desc_2d(A, ma, B, mb, dG, fa, fb, acc, codes_out=dG.dtype == torch.uint8)
+    store, scale_d_ptr = _store_of(dG, fd, scale_d)
+    if gate is None or up is None:
+        raise ValueError("gate and up are required")
+    w = _gate_of(gate, up, dG.shape, act, store, overflow)
+    _check(load().fp8_gemm_gated_backward(ctypes.byref(d), ctypes.byref(w), A.data_ptr(), B.data_ptr(), dG.data_ptr(), dU.data_ptr(),
+                                          _scalar(scale_inv_a, "scale_inv_a"), _scalar(scale_inv_b, "scale_inv_b"), scale_d_ptr,
+                                          None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()),
+           "fp8_gemm_gated_backward")
 
 
 TIMEOUT = 7                                   # FP8_ERR_TIMEOUT

@@ -1,0 +1,608 @@
+// FP8 products with fused epilogues (sm_100a): bias + activation + residual, the gated feed-forward block, and the
+// data gradient of its down projection fused with the gate's derivative.
+//
+// k_fused_rows: products with few rows (tokens).  Computed transposed: 128 columns of D (rows of the weights) are the
+// M side of the tensor core's tile and T tokens its N side, so that a tile wastes no tensor work on absent rows and one
+// CTA owns 128 weight rows.  K is cut into slices, one CTA of a cluster each; their binary32 partial sums meet in
+// distributed shared memory and are added in slice order, so the result does not depend on timing.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <mutex>
+
+#include "activation.cuh"
+#include "codec.cuh"
+#include "common.cuh"
+#include "umma.cuh"
+
+namespace fp8b200 {
+namespace fused {
+
+using namespace gemm;
+
+constexpr int MODE_EPILOGUE = 0;        // act(z + bias) + residual
+constexpr int MODE_GATED = 1;           // act(g) * u
+constexpr int MODE_GATED_BWD = 2;       // dh -> dG, dU
+
+constexpr int BK = 128;                 // K-block in elements = bytes = one swizzle row
+constexpr int UMMA_K = 32;
+
+struct Params {
+    int64_t M, N, K;                    // rows (tokens), columns, contraction
+    const float* sa_inv;
+    const float* sb_inv[2];             // [1]: the up projection of the gated block
+    const float* sb_inv_vec;            // optional, N entries
+    const float* scale_d;
+    const void* bias;                   // optional, N entries
+    const void* in[2];                  // residual | gate, up
+    void* keep[2];                      // pre | gate, up
+    void* D[2];                         // D | dG, dU
+    int64_t ld_in, ld_keep, ldd;        // elements
+    int bias_bf16, in_bf16, keep_bf16;
+    int store, nosat, act;
+    uint32_t* amax_bits;                // may be null
+    uint32_t idesc;
+    int w_mn;                           // weights stored with their N index contiguous
+};
+
+// codes written to the error latch (those of the plain products end at 9, the grid barrier's is 16)
+enum : uint32_t { F_WAIT_EMPTY = 33, F_WAIT_FULL = 34, F_WAIT_ACC_EMPTY = 35, F_WAIT_ACC_FULL = 36, F_WAIT_DRAIN = 37, F_WAIT_IN = 38 };
+
+// ---- element access ----------------------------------------------------------
+
+// Up to four consecutive elements of a wide row (missing ones read as 0).  Rows start on 16 bytes and the first index
+// is a multiple of 4, so a full group is one 8- or 16-byte access.
+__device__ __forceinline__ void load4(const void* base, bool bf16, int64_t at, int count, float (&v)[4]) {
+    if (count == 4) {
+        if (bf16) {
+            const uint2 w = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(base) + at);
+            v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+            v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        } else {
+            const float4 w = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at);
+            v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= count) v[i] = 0.0f;
+        else if (bf16) v[i] = __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(base)[at + i] << 16);
+        else v[i] = reinterpret_cast<const float*>(base)[at + i];
+    }
+}
+
+// The same without alignment (bias vectors, scale vectors).
+__device__ __forceinline__ void load4_any(const void* base, bool bf16, int64_t at, int count, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= count) v[i] = 0.0f;
+        else if (bf16) v[i] = __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(base)[at + i] << 16);
+        else v[i] = reinterpret_cast<const float*>(base)[at + i];
+    }
+}
+
+__device__ __forceinline__ void store4_wide(void* base, bool bf16, int64_t at, int count, const float (&v)[4]) {
+    if (bf16) {
+        const uint2 w = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        uint16_t* p = reinterpret_cast<uint16_t*>(base) + at;
+        if (count == 4) { *reinterpret_cast<uint2*>(p) = w; return; }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) p[i] = (uint16_t)(((i & 2) ? w.y : w.x) >> (16 * (i & 1)));
+    } else {
+        float* p = reinterpret_cast<float*>(base) + at;
+        if (count == 4) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); return; }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) p[i] = v[i];
+    }
+}
+
+template <int FMT>
+__device__ __forceinline__ uint32_t encode4(const float (&v)[4], float scale_d, bool nosat) {
+    float y[4], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { y[i] = v[i] * scale_d; top = fmax_nan(top, fabsf(y[i])); }
+    const bool over = Fmt<FMT>::nosat_limit_inclusive ? top >= Fmt<FMT>::nosat_limit : top > Fmt<FMT>::nosat_limit;
+    if (top <= 3.402823466e38f && !(nosat && over)) return cvt_quad<FMT>(y[0], y[1], y[2], y[3]);
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t code;
+        if (y[i] != y[i]) code = ((__float_as_uint(v[i]) >> 24) & 0x80u) | 0x7Fu;
+        else code = nosat ? encode_scalar<FMT, true>(y[i]) : encode_scalar<FMT, false>(y[i]);
+        word |= code << (8 * i);
+    }
+    return word;
+}
+
+// Stores a group as p.store says and folds its magnitudes into `top` (NaN once any is NaN): of the stored values for
+// the wide types, of v before scaling for FP8.
+__device__ __forceinline__ void store4(const Params& p, void* base, int64_t at, int count, float (&v)[4], float scale_d, float& top) {
+    if (p.store == FP8_STORE_BF16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(pack_bf16(v[i], 0.0f) << 16);
+        store4_wide(base, true, at, count, v);
+    } else if (p.store == FP8_STORE_F32) {
+        store4_wide(base, false, at, count, v);
+    } else {
+        const uint32_t w = p.store == FP8_STORE_E4M3 ? encode4<kE4M3>(v, scale_d, p.nosat != 0) : encode4<kE5M2>(v, scale_d, p.nosat != 0);
+        uint8_t* d = reinterpret_cast<uint8_t*>(base) + at;
+        if (count == 4) *reinterpret_cast<uint32_t*>(d) = w;
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) d[i] = (uint8_t)(w >> (8 * i));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < count) top = fmax_nan(top, fabsf(v[i]));
+}
+
+// ---- products with few rows ---------------------------------------------------
+
+constexpr int ROWS_THREADS = 192;                  // loader warp, MMA warp, four accumulator warps
+constexpr int ROWS_BN = 128;                       // columns of D per tile = the tensor core's M
+constexpr int ROWS_SPLIT_BLOCKS = 4;               // the tensor core's accumulator is drained every 512 of K
+constexpr uint32_t ROWS_TMEM_COLS = 256;           // half of an SM's TMEM: two CTAs share an SM
+constexpr uint32_t ROWS_SMEM = 112 * 1024;
+
+template <int MODE, int T> struct RowsGeo {
+    static constexpr int NB = MODE == MODE_GATED ? 2 : 1;                          // weight operands
+    static constexpr uint32_t W_BYTES = ROWS_BN * BK;
+    static constexpr uint32_t X_BYTES = T * BK;
+    static constexpr uint32_t STAGE_BYTES = NB * W_BYTES + X_BYTES;
+    static constexpr int STAGES = (int)((ROWS_SMEM - 2048) / STAGE_BYTES) < 8 ? (int)((ROWS_SMEM - 2048) / STAGE_BYTES) : 8;
+    static constexpr int ACCS = ROWS_TMEM_COLS / (T * NB) < 16 ? ROWS_TMEM_COLS / (T * NB) : 16;
+    static constexpr uint32_t EXCHANGE_BYTES = (uint32_t)NB * T * ROWS_BN * 4;
+    static_assert(STAGES >= 2 && ACCS >= 2 && EXCHANGE_BYTES <= STAGES * STAGE_BYTES, "shared memory budget");
+};
+
+struct alignas(8) RowsBarriers {
+    uint64_t full[8], empty[8], acc_full[16], acc_empty[16];
+    uint32_t tmem_base, abort_flag;
+};
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+
+template <int MODE, int T>
+__global__ void __launch_bounds__(ROWS_THREADS, 2)
+k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1,
+             const __grid_constant__ CUtensorMap map_x, const Params p) {
+    using G = RowsGeo<MODE, T>;
+    constexpr int NB = G::NB, STAGES = G::STAGES, ACCS = G::ACCS;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ RowsBarriers bars;
+    __shared__ uint32_t red[32];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;
+    volatile uint32_t* abort_flag = &bars.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n0 = blockIdx.x * ROWS_BN, t0 = blockIdx.y * T;
+    const uint32_t slices = gridDim.z, slice = blockIdx.z;                     // the cluster spans z
+    const int k_blocks = (int)((p.K + BK - 1) / BK);
+    const int kb_lo = (int)((int64_t)k_blocks * slice / slices), kb_hi = (int)((int64_t)k_blocks * (slice + 1) / slices);
+    const int kb_n = kb_hi - kb_lo;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
+        for (int a = 0; a < ACCS; ++a) { mbar_init(smem_u32(&bars.acc_full[a]), 1); mbar_init(smem_u32(&bars.acc_empty[a]), 4); }
+        bars.abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem_base)), "r"(ROWS_TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars.tmem_base;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ loader
+        bool ok = true;
+        int issued = 0;
+        const uint64_t keep = policy_evict_last(), once = policy_evict_first();
+        for (int i = 0; i < kb_n; ++i) {
+            const int st = i % STAGES;
+            ok = mbar_wait(smem_u32(&bars.empty[st]), ((uint32_t)(i / STAGES) & 1u) ^ 1u, abort_flag, F_WAIT_EMPTY);
+            if (!ok) break;
+            if (lane == 0) {
+                const uint32_t sw = ring + (uint32_t)st * G::STAGE_BYTES, full = smem_u32(&bars.full[st]);
+                const int k0 = (kb_lo + i) * BK;
+                // the weights are read once (by this tile alone when one tile holds all tokens); the tokens by every tile
+                mbar_arrive_expect_tx(full, G::STAGE_BYTES);
+                tma_load_3d(sw, &map_w0, p.w_mn ? n0 : k0, p.w_mn ? k0 : n0, 0, full, gridDim.y == 1 ? once : keep);
+                if (NB == 2) tma_load_3d(sw + G::W_BYTES, &map_w1, p.w_mn ? n0 : k0, p.w_mn ? k0 : n0, 0, full, gridDim.y == 1 ? once : keep);
+                tma_load_3d(sw + NB * G::W_BYTES, &map_x, k0, t0, 0, full, keep);
+            }
+            __syncwarp();
+            issued = i + 1;
+        }
+        if (!ok) {                                          // given up: no copy may be in flight when the CTA leaves
+            for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i) {
+                const uint32_t bar = smem_u32(&bars.full[i % STAGES]);
+                for (int spin = 0; spin < (1 << 20) && !mbar_try_wait(bar, (uint32_t)(i / STAGES) & 1u); ++spin) {}
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer
+        const uint32_t a_kstep = p.w_mn ? UMMA_K * 128 : UMMA_K, a_lbo = p.w_mn ? BK * 128 : 16;
+        bool ok = true;
+        for (int i = 0; i < kb_n; ++i) {
+            const int st = i % STAGES, chunk = i / ROWS_SPLIT_BLOCKS, acc = chunk % ACCS;
+            if (i % ROWS_SPLIT_BLOCKS == 0) {
+                ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), ((uint32_t)(chunk / ACCS) & 1u) ^ 1u, abort_flag, F_WAIT_ACC_EMPTY);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            ok = mbar_wait(smem_u32(&bars.full[st]), (uint32_t)(i / STAGES) & 1u, abort_flag, F_WAIT_FULL);
+            if (!ok) break;
+            tc_fence_after();
+            if (lane == 0) {
+                const uint32_t sw = ring + (uint32_t)st * G::STAGE_BYTES, sx = sw + NB * G::W_BYTES;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int k = 0; k < BK / UMMA_K; ++k)
+                        tc_mma_f8(tmem + (uint32_t)((acc * NB + b) * T), smem_desc(sw + b * G::W_BYTES + k * a_kstep, a_lbo, 1024),
+                                  smem_desc(sx + k * UMMA_K, 16, 1024), p.idesc, ((i % ROWS_SPLIT_BLOCKS) | k) != 0 ? 1u : 0u);
+                tc_commit(smem_u32(&bars.empty[st]));
+                if (i == kb_n - 1 || (i + 1) % ROWS_SPLIT_BLOCKS == 0) tc_commit(smem_u32(&bars.acc_full[acc]));
+            }
+            __syncwarp();
+        }
+    } else {
+        // ------------------------------------------------------------ accumulators: lane = column of D, TMEM column = token
+        const int q = warp & 3;
+        float part[NB * T];
+#pragma unroll
+        for (int i = 0; i < NB * T; ++i) part[i] = 0.0f;
+        bool ok = true;
+        const int chunks = (kb_n + ROWS_SPLIT_BLOCKS - 1) / ROWS_SPLIT_BLOCKS;
+        for (int c = 0; c < chunks; ++c) {
+            const int acc = c % ACCS;
+            ok = mbar_wait(smem_u32(&bars.acc_full[acc]), (uint32_t)(c / ACCS) & 1u, abort_flag, F_WAIT_ACC_FULL);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t taddr = tmem + (uint32_t)(acc * NB * T) + ((uint32_t)(q * 32) << 16);
+#pragma unroll
+            for (int j = 0; j < NB * T / 16; ++j) {
+                uint32_t r[16];
+                tc_ld16(taddr + j * 16, r);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[j * 16 + i] += __uint_as_float(r[i]);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.acc_empty[acc]));
+        }
+        // the last accumulator is complete, so every staged tile has been consumed: the ring becomes the exchange buffer
+        if (ok) {
+            const uint32_t mine = ring + (uint32_t)(q * 32 + lane) * 4;
+#pragma unroll
+            for (int i = 0; i < NB * T; ++i)
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)i * ROWS_BN * 4), "f"(part[i]) : "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (slices > 1) cluster_sync_all();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(ROWS_TMEM_COLS) : "memory");
+
+    // ---------------------------------------------------------------- epilogue: each slice finishes its share of the tile
+    float top = 0.0f;
+    bool whole = bars.abort_flag == 0u;
+    if (slices > 1) {
+        for (uint32_t s = 0; s < slices; ++s) {
+            uint32_t flag;
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(flag) : "r"(map_to_cta(smem_u32(&bars.abort_flag), s)) : "memory");
+            whole = whole && flag == 0u;
+        }
+    }
+    if (whole) {
+        const int rows = (int)min((int64_t)T, p.M - t0);
+        const int items = rows * (ROWS_BN / 4);
+        const int lo = (int)((int64_t)items * slice / slices), hi = (int)((int64_t)items * (slice + 1) / slices);
+        const float sa = __ldg(p.sa_inv);
+        const float scale_d = p.store >= FP8_STORE_E4M3 ? __ldg(p.scale_d) : 1.0f;
+        const float alpha0 = p.sb_inv_vec ? 0.0f : sa * __ldg(p.sb_inv[0]);
+        const float alpha1 = NB == 2 ? sa * __ldg(p.sb_inv[1]) : 0.0f;
+        for (int item = lo + (int)threadIdx.x; item < hi; item += ROWS_THREADS) {
+            const int tr = item >> 5, quad = item & 31;
+            const int64_t t = t0 + tr, n = n0 + quad * 4;
+            const int count = (int)min((int64_t)4, p.N - n);
+            if (count <= 0) continue;
+            float a[NB][4];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t at = ring + (uint32_t)((b * T + tr) * ROWS_BN + quad * 4) * 4;
+                a[b][0] = a[b][1] = a[b][2] = a[b][3] = 0.0f;
+                for (uint32_t s = 0; s < slices; ++s) {
+                    const float4 v = ld_cluster_f4(slices > 1 ? map_to_cta(at, s) : at);
+                    a[b][0] += v.x; a[b][1] += v.y; a[b][2] += v.z; a[b][3] += v.w;
+                }
+            }
+            if (MODE == MODE_EPILOGUE) {
+                float z[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (p.bias) load4_any(p.bias, p.bias_bf16 != 0, n, count, bias);
+                if (p.sb_inv_vec) {
+                    float sb[4];
+                    load4_any(p.sb_inv_vec, false, n, count, sb);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = fmaf(a[0][i], sa * sb[i], bias[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = fmaf(a[0][i], alpha0, bias[i]);
+                }
+                if (p.keep[0]) store4_wide(p.keep[0], p.keep_bf16 != 0, t * p.ld_keep + n, count, z);
+                with_activation(p.act, [&](auto tag) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = activate<decltype(tag)::value>(z[i]);
+                });
+                if (p.in[0]) {
+                    float r[4];
+                    load4(p.in[0], p.in_bf16 != 0, t * p.ld_in + n, count, r);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] += r[i];
+                }
+                store4(p, p.D[0], t * p.ldd + n, count, z, scale_d, top);
+            } else if (MODE == MODE_GATED) {
+                float g[4], u[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { g[i] = a[0][i] * alpha0; u[i] = a[NB - 1][i] * alpha1; }
+                if (p.keep[0]) {
+                    store4_wide(p.keep[0], p.keep_bf16 != 0, t * p.ld_keep + n, count, g);
+                    store4_wide(p.keep[1], p.keep_bf16 != 0, t * p.ld_keep + n, count, u);
+                }
+                with_activation(p.act, [&](auto tag) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) g[i] = activate<decltype(tag)::value>(g[i]) * u[i];
+                });
+                store4(p, p.D[0], t * p.ldd + n, count, g, scale_d, top);
+            } else {
+                float g[4], u[4], dg[4], du[4];
+                load4(p.in[0], p.in_bf16 != 0, t * p.ld_in + n, count, g);
+                load4(p.in[1], p.in_bf16 != 0, t * p.ld_in + n, count, u);
+                with_activation(p.act, [&](auto tag) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float value, slope;
+                        activate_with_slope<decltype(tag)::value>(g[i], value, slope);
+                        const float dh = a[0][i] * alpha0;
+                        dg[i] = dh * u[i] * slope;
+                        du[i] = dh * value;
+                    }
+                });
+                store4(p, p.D[0], t * p.ldd + n, count, dg, scale_d, top);
+                store4(p, p.D[1], t * p.ldd + n, count, du, scale_d, top);
+            }
+        }
+        if (p.amax_bits) block_atomic_max_bits(canonical_nan_bits(__float_as_uint(top)), red, p.amax_bits);
+    } else if (p.amax_bits) {
+        block_atomic_max_bits(0u, red, p.amax_bits);
+    }
+    if (slices > 1) cluster_sync_all();                     // no CTA leaves while another still reads its partial sums
+}
+
+// ---- host ------------------------------------------------------------------
+
+static fp8_status launch_cluster(const void* kernel, dim3 grid, dim3 cluster, int threads, uint32_t smem, cudaStream_t st, void** args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster.x;
+    attr[0].val.clusterDim.y = cluster.y;
+    attr[0].val.clusterDim.z = cluster.z;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
+    count_launches(1);
+    return launch_status();
+}
+
+// A kernel's dynamic shared memory limit is raised once per (kernel, device).
+static bool allow_smem(const void* kernel, uint32_t bytes) {
+    static std::mutex mu;
+    static const void* done[64][32] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    std::lock_guard<std::mutex> lock(mu);
+    int i = 0;
+    while (i < 32 && done[dev][i] && done[dev][i] != kernel) ++i;
+    if (i < 32 && done[dev][i] == kernel) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) { (void)cudaGetLastError(); return false; }
+    if (i < 32) done[dev][i] = kernel;
+    return true;
+}
+
+template <int MODE, int T>
+static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
+    using G = RowsGeo<MODE, T>;
+    const bool w_mn = d->mb == FP8_MAJOR_MN;
+    CUtensorMap w0 = {}, w1 = {}, x = {};
+    if (d->K > 0) {
+        bool ok = make_map(&x, A, (uint64_t)d->K, (uint64_t)d->M, (uint64_t)d->lda, 1, 0, BK, T);
+        const uint64_t inner = (uint64_t)(w_mn ? d->N : d->K), outer = (uint64_t)(w_mn ? d->K : d->N);
+        ok = ok && make_map(&w0, B0, inner, outer, (uint64_t)d->ldb, 1, 0, 128, 128);
+        ok = ok && (!B1 || make_map(&w1, B1, inner, outer, (uint64_t)d->ldb, 1, 0, 128, 128));
+        if (!ok) return FP8_ERR_CUDA;
+    }
+    p.w_mn = w_mn ? 1 : 0;
+    // instruction descriptor: fp32 accumulate; the weights are the tensor core's A operand (M = 128), the tokens its B (N = T)
+    p.idesc = (1u << 4) | ((uint32_t)d->fb << 7) | ((uint32_t)d->fa << 10) | ((w_mn ? 1u : 0u) << 15) |
+              ((uint32_t)(T >> 3) << 17) | ((uint32_t)(ROWS_BN >> 4) << 24);
+    const int64_t tiles_n = (d->N + ROWS_BN - 1) / ROWS_BN, tiles_t = (d->M + T - 1) / T;
+    if (tiles_t > 65535) return FP8_ERR_UNSUPPORTED;
+    const int64_t k_blocks = (d->K + BK - 1) / BK;
+    unsigned slices = 1;
+    while (slices < 8 && tiles_n * tiles_t * slices * 2 <= 2 * (int64_t)sm_count() && k_blocks >= 8 * (int64_t)slices) slices *= 2;
+    const void* k = reinterpret_cast<const void*>(&k_fused_rows<MODE, T>);
+    constexpr uint32_t smem = G::STAGES * G::STAGE_BYTES + 1024;
+    if (!allow_smem(k, smem)) return FP8_ERR_CUDA;
+    void* args[] = {&w0, &w1, &x, &p};
+    return launch_cluster(k, dim3((unsigned)tiles_n, (unsigned)tiles_t, slices), dim3(1, 1, slices), ROWS_THREADS, smem, st, args);
+}
+
+template <int MODE>
+static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
+    if (d->ma == FP8_MAJOR_MN) return FP8_ERR_UNSUPPORTED;
+    if (d->M <= 16) return launch_rows<MODE, 16>(d, A, B0, B1, p, st);
+    if (d->M <= 32) return launch_rows<MODE, 32>(d, A, B0, B1, p, st);
+    return launch_rows<MODE, 64>(d, A, B0, B1, p, st);
+}
+
+// ---- validation shared by the three entry points: nothing is enqueued before every check has passed ----------------
+
+static bool enums_ok(const fp8_gemm_desc* d, int act, int store, int overflow) {
+    return (d->fa == FP8_E4M3 || d->fa == FP8_E5M2) && (d->fb == FP8_E4M3 || d->fb == FP8_E5M2) &&
+           (d->ma == FP8_MAJOR_K || d->ma == FP8_MAJOR_MN) && (d->mb == FP8_MAJOR_K || d->mb == FP8_MAJOR_MN) &&
+           (d->acc == FP8_ACC_FAST || d->acc == FP8_ACC_SPLIT) && act >= FP8_ACT_NONE && act <= FP8_ACT_SILU &&
+           store >= FP8_STORE_F32 && store <= FP8_STORE_E5M2 && (overflow == FP8_SATURATE || overflow == FP8_NOSAT);
+}
+static bool wide_ok(int t) { return t == FP8_F32 || t == FP8_BF16; }
+static int64_t store_bytes(int store) { return store == FP8_STORE_F32 ? 4 : store == FP8_STORE_BF16 ? 2 : 1; }
+static bool misaligned(const void* p, int64_t pitch_bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0 || (pitch_bytes & 15) != 0; }
+
+// operands and D; `B1` only where the mode has it
+static fp8_status check_product(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, bool two,
+                                const void* D0, const void* D1, bool two_out, int store) {
+    if (d->M < 0 || d->N < 0 || d->K < 0) return FP8_ERR_SHAPE;
+    if (d->M == 0 || d->N == 0) return FP8_OK;
+    if (!D0 || (two_out && !D1)) return FP8_ERR_NULL;
+    if (d->ldd < d->N) return FP8_ERR_SHAPE;
+    if (d->K > 0) {
+        if (!A || !B0 || (two && !B1)) return FP8_ERR_NULL;
+        if (d->lda < (d->ma == FP8_MAJOR_MN ? d->M : d->K) || d->ldb < (d->mb == FP8_MAJOR_MN ? d->N : d->K)) return FP8_ERR_SHAPE;
+        if (misaligned(A, d->lda) || misaligned(B0, d->ldb) || (two && misaligned(B1, d->ldb))) return FP8_ERR_ALIGN;
+    }
+    if (misaligned(D0, d->ldd * store_bytes(store)) || (two_out && misaligned(D1, d->ldd * store_bytes(store)))) return FP8_ERR_ALIGN;
+    const int64_t most = ((int64_t)1 << 31) - 512;
+    if (d->M > most || d->N > most || d->K > most || ((d->M + 127) / 128) * ((d->N + 127) / 128) > (int64_t)1 << 30) return FP8_ERR_UNSUPPORTED;
+    return FP8_OK;
+}
+
+static fp8_status zero_amax(float* amax, cudaStream_t st) {
+    if (!amax) return FP8_OK;
+    if (cudaMemsetAsync(amax, 0, 4, st) != cudaSuccess) return FP8_ERR_CUDA;
+    count_launches(1);
+    return FP8_OK;
+}
+
+static Params common_params(const fp8_gemm_desc* d, int act, int store, int overflow, const float* scale_d, float* amax) {
+    Params p = {};
+    p.M = d->M; p.N = d->N; p.K = d->K; p.ldd = d->ldd;
+    p.act = act; p.store = store; p.nosat = overflow == FP8_NOSAT ? 1 : 0;
+    p.scale_d = scale_d;
+    p.amax_bits = reinterpret_cast<uint32_t*>(amax);
+    return p;
+}
+
+}  // namespace fused
+
+// Reads and clears this file's error latch.
+void fused_read_clear_latch(unsigned int out2[2]) {
+    out2[0] = out2[1] = 0u;
+    if (cudaMemcpyFromSymbol(out2, g_async_latch, 2 * sizeof(unsigned int)) != cudaSuccess || out2[0] == 0u) return;
+    const unsigned int zero[2] = {0u, 0u};
+    (void)cudaMemcpyToSymbol(g_async_latch, zero, sizeof(zero));
+}
+
+}  // namespace fp8b200
+
+using namespace fp8b200;
+
+extern "C" {
+
+fp8_status fp8_gemm_epilogue(const fp8_gemm_desc* d, const fp8_epilogue* e, const uint8_t* A, const uint8_t* B, void* D,
+                             const float* scale_inv_a_dev, const float* scale_inv_b_dev, const float* scale_d_dev,
+                             float* amax_d_dev, void* stream) {
+    using namespace fp8b200::fused;
+    if (!d || !e || !scale_inv_a_dev || (!scale_inv_b_dev && !e->scale_inv_b_vec_dev)) return FP8_ERR_NULL;
+    if (!enums_ok(d, e->act, e->store, e->overflow) || !wide_ok(e->bias_t) || !wide_ok(e->residual_t) || !wide_ok(e->pre_t)) return FP8_ERR_ENUM;
+    if (e->store >= FP8_STORE_E4M3 && !scale_d_dev) return FP8_ERR_NULL;
+    fp8_status rc = check_product(d, A, B, nullptr, false, D, nullptr, false, e->store);
+    if (rc != FP8_OK) return rc;
+    const int64_t r_size = e->residual_t == FP8_BF16 ? 2 : 4, p_size = e->pre_t == FP8_BF16 ? 2 : 4;
+    if (d->M > 0 && d->N > 0) {
+        if ((e->residual && e->ldr < d->N) || (e->pre && e->ldp < d->N)) return FP8_ERR_SHAPE;
+        if ((e->residual && misaligned(e->residual, e->ldr * r_size)) || (e->pre && misaligned(e->pre, e->ldp * p_size))) return FP8_ERR_ALIGN;
+        if (e->bias && (reinterpret_cast<uintptr_t>(e->bias) & (e->bias_t == FP8_BF16 ? 1u : 3u))) return FP8_ERR_ALIGN;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = zero_amax(amax_d_dev, st)) != FP8_OK || d->M == 0 || d->N == 0) return rc;
+    Params p = common_params(d, e->act, e->store, e->overflow, scale_d_dev, amax_d_dev);
+    p.sa_inv = scale_inv_a_dev; p.sb_inv[0] = scale_inv_b_dev; p.sb_inv_vec = e->scale_inv_b_vec_dev;
+    p.bias = e->bias; p.bias_bf16 = e->bias_t == FP8_BF16;
+    p.in[0] = e->residual; p.in_bf16 = e->residual_t == FP8_BF16; p.ld_in = e->ldr;
+    p.keep[0] = e->pre; p.keep_bf16 = e->pre_t == FP8_BF16; p.ld_keep = e->ldp;
+    p.D[0] = D;
+    return dispatch<MODE_EPILOGUE>(d, A, B, nullptr, p, st);
+}
+
+static fp8_status check_gate(const fp8_gemm_desc* d, const fp8_gated* w) {
+    if (d->M == 0 || d->N == 0 || !w->gate) return FP8_OK;
+    if (w->ldg < d->N) return FP8_ERR_SHAPE;
+    const int64_t size = w->gate_t == FP8_BF16 ? 2 : 4;
+    return fp8b200::fused::misaligned(w->gate, w->ldg * size) || fp8b200::fused::misaligned(w->up, w->ldg * size) ? FP8_ERR_ALIGN : FP8_OK;
+}
+
+fp8_status fp8_gemm_gated(const fp8_gemm_desc* d, const fp8_gated* w, const uint8_t* A, const uint8_t* Bg, const uint8_t* Bu, void* H,
+                          const float* scale_inv_a_dev, const float* scale_inv_bg_dev, const float* scale_inv_bu_dev,
+                          const float* scale_h_dev, float* amax_h_dev, void* stream) {
+    using namespace fp8b200::fused;
+    if (!d || !w || !scale_inv_a_dev || !scale_inv_bg_dev || !scale_inv_bu_dev || !w->gate != !w->up) return FP8_ERR_NULL;
+    if (!enums_ok(d, w->act, w->store, w->overflow) || !wide_ok(w->gate_t)) return FP8_ERR_ENUM;
+    if (w->store >= FP8_STORE_E4M3 && !scale_h_dev) return FP8_ERR_NULL;
+    fp8_status rc = check_product(d, A, Bg, Bu, true, H, nullptr, false, w->store);
+    if (rc != FP8_OK || (rc = check_gate(d, w)) != FP8_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = zero_amax(amax_h_dev, st)) != FP8_OK || d->M == 0 || d->N == 0) return rc;
+    Params p = common_params(d, w->act, w->store, w->overflow, scale_h_dev, amax_h_dev);
+    p.sa_inv = scale_inv_a_dev; p.sb_inv[0] = scale_inv_bg_dev; p.sb_inv[1] = scale_inv_bu_dev;
+    p.keep[0] = w->gate; p.keep[1] = w->up; p.keep_bf16 = w->gate_t == FP8_BF16; p.ld_keep = w->ldg;
+    p.D[0] = H;
+    return dispatch<MODE_GATED>(d, A, Bg, Bu, p, st);
+}
+
+fp8_status fp8_gemm_gated_backward(const fp8_gemm_desc* d, const fp8_gated* w, const uint8_t* A, const uint8_t* B, void* dG, void* dU,
+                                   const float* scale_inv_a_dev, const float* scale_inv_b_dev, const float* scale_d_dev,
+                                   float* amax_dev, void* stream) {
+    using namespace fp8b200::fused;
+    if (!d || !w || !scale_inv_a_dev || !scale_inv_b_dev) return FP8_ERR_NULL;
+    if (!enums_ok(d, w->act, w->store, w->overflow) || !wide_ok(w->gate_t)) return FP8_ERR_ENUM;
+    if (w->store >= FP8_STORE_E4M3 && !scale_d_dev) return FP8_ERR_NULL;
+    if (d->M > 0 && d->N > 0 && (!w->gate || !w->up)) return FP8_ERR_NULL;
+    fp8_status rc = check_product(d, A, B, nullptr, false, dG, dU, true, w->store);
+    if (rc != FP8_OK || (rc = check_gate(d, w)) != FP8_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = zero_amax(amax_dev, st)) != FP8_OK || d->M == 0 || d->N == 0) return rc;
+    Params p = common_params(d, w->act, w->store, w->overflow, scale_d_dev, amax_dev);
+    p.sa_inv = scale_inv_a_dev; p.sb_inv[0] = scale_inv_b_dev;
+    p.in[0] = w->gate; p.in[1] = w->up; p.in_bf16 = w->gate_t == FP8_BF16; p.ld_in = w->ldg;
+    p.D[0] = dG; p.D[1] = dU;
+    return dispatch<MODE_GATED_BWD>(d, A, B, nullptr, p, st);
+}
+
+}  // extern "C"
