@@ -43,7 +43,7 @@ struct Params {
     int store, nosat, act;
     uint32_t* amax_bits;                // may be null
     uint32_t idesc;
-    int w_mn;                           // weights stored with their N index contiguous
+    int a_mn, w_mn;                     // rows stored with M contiguous; weights stored with N contiguous
 };
 
 // codes written to the error latch (those of the plain products end at 9, the grid barrier's is 16)
@@ -402,7 +402,474 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
     if (slices > 1) cluster_sync_all();                     // no CTA leaves while another still reads its partial sums
 }
 
+// ---- products with many rows --------------------------------------------------
+//
+// Persistent CTA pairs on 256 x 256 accumulator tiles (each CTA holds 128 rows), organised as the plain product kernel: a
+// loader warp, an MMA warp in the leader, eight epilogue warps.  The accumulator is moved into the epilogue warps'
+// registers chunk by chunk of K and handed back at once, so the epilogue of a tile runs beside the matrix instructions of
+// the next one.  Matrices that the epilogue reads (residual; gate and up) and writes move as boxes of 32 rows x 32 columns
+// between global and shared memory by TMA: every warp has its own staging slots, a tile's reads are issued while its
+// products are still being accumulated, and the TMA unit clips rows and columns past the edges.
+// The gated block puts 128 columns of the gate projection and the same 128 of the up projection into one accumulator
+// tile (each CTA of the pair stages the weights of one of the two), so that both factors of h meet in one thread.
+
+constexpr int BM = 128;
+constexpr int TILE_M = 2 * BM;
+constexpr int ACC_COLS = 256;
+constexpr int TILES_STAGES = 4, TILES_FG = 2;                          // ring depth; stages consumed per barrier wait
+constexpr uint32_t TILES_A_BYTES = BM * BK, TILES_B_BYTES = 128 * BK;
+constexpr uint32_t TILES_STAGE_BYTES = TILES_A_BYTES + TILES_B_BYTES;
+constexpr int TILES_EPI_WARPS = 8, TILES_EPI_BASE = 4;
+constexpr int TILES_THREADS = 32 * (TILES_EPI_BASE + TILES_EPI_WARPS);
+constexpr int TILES_REGS_FRONT = 56, TILES_REGS_EPILOGUE = 224;        // 4 x 32 x 56 + 8 x 32 x 224 = 64512 <= 384 x 168
+constexpr int TILES_SPLIT_BLOCKS = 16;                                 // split accumulation: a chunk is 2048 of K
+constexpr int TILES_GROUP_M = 16;
+constexpr int MAX_SLOTS = 4;
+constexpr uint32_t TILES_WARP_BYTES = 12 * 1024;                       // staging of one epilogue warp
+constexpr uint32_t TILES_SMEM = TILES_STAGES * TILES_STAGE_BYTES + TILES_EPI_WARPS * TILES_WARP_BYTES + 1024;
+constexpr uint32_t TILES_TMEM_COLS = 512;
+
+// tile index -> (row-tile, column-tile): GROUP_M row-tiles advance together over the columns, sharing panels in L2
+__device__ __forceinline__ void fused_tile_coords(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int per_group = TILES_GROUP_M * tiles_n, g = t / per_group, first_m = g * TILES_GROUP_M;
+    const int rows = min(TILES_GROUP_M, tiles_m - first_m), r = t - g * per_group;
+    tm = first_m + r % rows;
+    tn = r / rows;
+}
+
+struct alignas(8) TilesBarriers {
+    uint64_t full[TILES_STAGES], empty[TILES_STAGES], acc_full[2], acc_empty[2];
+    uint64_t in[TILES_EPI_WARPS][MAX_SLOTS];
+    uint32_t tmem_base, abort_flag;
+};
+
+// Where the pieces of a staging slot lie: byte offsets of the boxes read and written.
+struct Staging {
+    uint32_t in[2], out[2], keep[2];
+    uint32_t slot_bytes;
+    int slots;
+    uint32_t in_tx;                     // bytes that arrive per slot
+};
+
+struct TilesParams {
+    Params p;
+    Staging s;
+    int tiles_m, tiles_n, chunk_blocks;
+};
+
+struct TilesMaps {
+    CUtensorMap a, b[2], in[2], out[2], keep[2];
+};
+
+// byte offset of 16-byte unit `unit` of row `row` in a box whose rows are 32 << LOG2 bytes long, as the TMA unit swizzles it
+__device__ __forceinline__ uint32_t box_offset(int row_bytes, int row, int unit) {
+    const int mask = row_bytes >> 4;                                   // units per row: 2, 4, 8
+    const int turn = row_bytes == 128 ? row : row_bytes == 64 ? row >> 1 : row >> 2;
+    return (uint32_t)(row * row_bytes + ((unit ^ (turn & (mask - 1))) << 4));
+}
+
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// Eight consecutive columns (octet `o` of four) of this thread's row in a staged box.
+__device__ __forceinline__ void box_load8(uint32_t box, bool bf16, int row, int o, float (&v)[8]) {
+    if (bf16) {
+        const uint4 w = ld_shared_v4(box + box_offset(64, row, o));
+        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        v[4] = __uint_as_float(w.z << 16); v[5] = __uint_as_float(w.z & 0xFFFF0000u);
+        v[6] = __uint_as_float(w.w << 16); v[7] = __uint_as_float(w.w & 0xFFFF0000u);
+    } else {
+        const uint4 w = ld_shared_v4(box + box_offset(128, row, 2 * o)), x = ld_shared_v4(box + box_offset(128, row, 2 * o + 1));
+        v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+        v[4] = __uint_as_float(x.x); v[5] = __uint_as_float(x.y); v[6] = __uint_as_float(x.z); v[7] = __uint_as_float(x.w);
+    }
+}
+
+__device__ __forceinline__ void box_store8_wide(uint32_t box, bool bf16, int row, int o, const float (&v)[8]) {
+    if (bf16) {
+        st_shared_v4(box + box_offset(64, row, o), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    } else {
+        st_shared_v4(box + box_offset(128, row, 2 * o), __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        st_shared_v4(box + box_offset(128, row, 2 * o + 1), __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    }
+}
+
+// Eight values of a row written to global memory one by one: where a box crosses the right edge of rows whose length is
+// not a multiple of 16 bytes (the TMA unit clips in such units).
+__device__ __forceinline__ void direct_store8_wide(void* base, bool bf16, int64_t at, int count, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= count) break;
+        if (bf16) reinterpret_cast<uint16_t*>(base)[at + i] = (uint16_t)pack_bf16(v[i], 0.0f);
+        else reinterpret_cast<float*>(base)[at + i] = v[i];
+    }
+}
+
+// One output of the epilogue: conversion, amax, staging (or the direct form).
+__device__ __forceinline__ void emit8(const Params& p, void* D, uint32_t box, bool direct, bool row_ok, int row, int o, int64_t grow, int64_t col,
+                                      float (&v)[8], float scale_d, float& top) {
+    const int count = row_ok ? (int)max((int64_t)0, min((int64_t)8, p.N - col)) : 0;
+    if (p.store == FP8_STORE_BF16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(pack_bf16(v[i], 0.0f) << 16);
+    }
+    if (count == 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmax_nan(top, fabsf(v[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) top = fmax_nan(top, fabsf(v[i]));
+    }
+    if (p.store <= FP8_STORE_BF16) {
+        if (direct) direct_store8_wide(D, p.store == FP8_STORE_BF16, grow * p.ldd + col, count, v);
+        else box_store8_wide(box, p.store == FP8_STORE_BF16, row, o, v);
+        return;
+    }
+    const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+    uint32_t w0, w1;
+    if (p.store == FP8_STORE_E4M3) { w0 = encode4<kE4M3>(lo, scale_d, p.nosat != 0); w1 = encode4<kE4M3>(hi, scale_d, p.nosat != 0); }
+    else                           { w0 = encode4<kE5M2>(lo, scale_d, p.nosat != 0); w1 = encode4<kE5M2>(hi, scale_d, p.nosat != 0); }
+    if (direct) {
+        uint8_t* d = reinterpret_cast<uint8_t*>(D) + grow * p.ldd + col;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) d[i] = (uint8_t)((i < 4 ? w0 : w1) >> (8 * (i & 3)));
+    } else {
+        const uint32_t at = box + box_offset(32, row, o >> 1) + (uint32_t)(o & 1) * 8;
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w0), "r"(w1) : "memory");
+    }
+}
+
+template <int MODE>
+__global__ void __launch_bounds__(TILES_THREADS, 1)
+k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ TilesParams tp) {
+    const Params& p = tp.p;
+    constexpr int OUT_COLS = MODE == MODE_GATED ? 128 : 256;           // columns of D per tile
+    constexpr int WARP_COLS = OUT_COLS / 2;                            // two warps share a lane quarter
+    constexpr int STEPS = WARP_COLS / 32;
+    constexpr int NIN = MODE == MODE_GATED_BWD ? 2 : 1, NOUT = MODE == MODE_GATED_BWD ? 2 : 1;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ TilesBarriers bars;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    volatile uint32_t* abort_flag = &bars.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t cta_rank = cluster_ctarank();
+    const int worker = blockIdx.x / 2, num_workers = gridDim.x / 2;
+    const int num_tiles = tp.tiles_m * tp.tiles_n;
+    const int k_blocks = (int)((p.K + BK - 1) / BK);
+    const int k_pad = (k_blocks + TILES_FG - 1) / TILES_FG * TILES_FG;
+    const int chunk = tp.chunk_blocks;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < TILES_STAGES; ++s) { mbar_init(smem_u32(&bars.full[s]), TILES_FG * 2); mbar_init(smem_u32(&bars.empty[s]), 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars.acc_full[a]), 1); mbar_init(smem_u32(&bars.acc_empty[a]), TILES_EPI_WARPS * 2); }
+        for (int w = 0; w < TILES_EPI_WARPS; ++w)
+            for (int s = 0; s < MAX_SLOTS; ++s) mbar_init(smem_u32(&bars.in[w][s]), 1);
+        bars.abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem_base)), "r"(TILES_TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = bars.tmem_base;
+
+    if (warp < TILES_EPI_BASE) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TILES_REGS_FRONT));
+        if (warp == 0) {
+            // -------------------------------------------------------- loader: each CTA its rows of A and its half of B
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            const uint64_t keep = policy_evict_last();
+            const CUtensorMap* map_b = &maps.b[MODE == MODE_GATED ? cta_rank : 0];
+            const bool a_mn = p.a_mn != 0, b_mn = p.w_mn != 0;
+            int tile_no = 0;
+            for (int t = worker; t < num_tiles && ok; t += num_workers) {
+                int tm, tn;
+                fused_tile_coords(t, tp.tiles_m, tp.tiles_n, tm, tn);
+                const int m0 = tm * TILE_M + (int)cta_rank * BM;
+                const int n0 = MODE == MODE_GATED ? tn * OUT_COLS : tn * OUT_COLS + (int)cta_rank * 128;
+                const bool backwards = (tile_no++ & 1) != 0;           // K from its end: the wave meets again in L2
+                for (int kb = 0; kb < k_pad; ++kb) {
+                    ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag, F_WAIT_EMPTY);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        const uint32_t sa = ring + stage * TILES_STAGE_BYTES, sb = sa + TILES_A_BYTES;
+                        const int k0 = (backwards && kb < k_blocks ? k_blocks - 1 - kb : kb) * BK;
+                        const uint32_t full = map_to_cta(smem_u32(&bars.full[stage / TILES_FG]), 0);
+                        if (kb < k_blocks) {
+                            mbar_arrive_expect_tx_cluster(full, TILES_STAGE_BYTES);
+                            tma_load_3d_pair(sa, &maps.a, a_mn ? m0 : k0, a_mn ? k0 : m0, 0, full, keep);
+                            tma_load_3d_pair(sb, map_b, b_mn ? n0 : k0, b_mn ? k0 : n0, 0, full, keep);
+                        } else {
+                            mbar_arrive_cluster(full);                 // padding block
+                        }
+                    }
+                    __syncwarp();
+                    if (++stage == TILES_STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok)                                                   // given up: a millisecond for copies still in flight (their
+                for (const long long t0 = clock64(); clock64() - t0 < 2000000ll;) {}     // barrier may be in the other CTA)
+        } else if (warp == 1) {
+            // -------------------------------------------------------- MMA issuer (leader only)
+            uint32_t stage = 0, phase = 0;
+            bool ok = cta_rank == 0;
+            int it = 0;
+            const uint32_t a_kstep = p.a_mn ? UMMA_K * 128 : UMMA_K, a_lbo = p.a_mn ? BK * 128 : 16;
+            const uint32_t b_kstep = p.w_mn ? UMMA_K * 128 : UMMA_K, b_lbo = p.w_mn ? BK * 128 : 16;
+            for (int t = worker; t < num_tiles && ok; t += num_workers) {
+                for (int kc = 0; kc < k_pad && ok; kc += chunk, ++it) {
+                    const uint32_t acc = (uint32_t)it & 1u;
+                    ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), (((uint32_t)it >> 1) & 1u) ^ 1u, abort_flag, F_WAIT_ACC_EMPTY);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int kend = min(k_pad, kc + chunk), last_real = min(k_blocks, kend) - 1;
+                    for (int kb = kc; kb < kend; kb += TILES_FG) {
+                        ok = mbar_wait(smem_u32(&bars.full[stage / TILES_FG]), phase, abort_flag, F_WAIT_FULL);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (lane == 0) {
+#pragma unroll
+                            for (int h = 0; h < TILES_FG; ++h) {
+                                const uint32_t st = stage + h;
+                                if (kb + h < k_blocks) {
+                                    const uint32_t sa = ring + st * TILES_STAGE_BYTES, sb = sa + TILES_A_BYTES;
+#pragma unroll
+                                    for (int k = 0; k < BK / UMMA_K; ++k)
+                                        tc_mma_f8_pair(tmem + acc * ACC_COLS, smem_desc(sa + k * a_kstep, a_lbo, 1024), smem_desc(sb + k * b_kstep, b_lbo, 1024),
+                                                       p.idesc, ((kb - kc) | h | k) != 0 ? 1u : 0u);
+                                }
+                                tc_commit_pair(smem_u32(&bars.empty[st]));
+                                if (kb + h == last_real) tc_commit_pair(smem_u32(&bars.acc_full[acc]));
+                            }
+                        }
+                        __syncwarp();
+                        stage += TILES_FG;
+                        if (stage == TILES_STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ epilogue: each CTA its own 128 rows
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TILES_REGS_EPILOGUE));
+        const int ew = warp - TILES_EPI_BASE, q = warp & 3, part_no = ew >> 2;
+        const float sa_inv = __ldg(p.sa_inv);
+        const float alpha0 = p.sb_inv_vec ? 0.0f : sa_inv * __ldg(p.sb_inv[0]);
+        const float alpha1 = MODE == MODE_GATED ? sa_inv * __ldg(p.sb_inv[1]) : 0.0f;
+        const float scale_d = p.store >= FP8_STORE_E4M3 ? __ldg(p.scale_d) : 1.0f;
+        const uint32_t staging = ring + TILES_STAGES * TILES_STAGE_BYTES + (uint32_t)ew * TILES_WARP_BYTES;
+        const uint64_t stream = policy_evict_first();
+        const bool has_in = tp.s.in_tx != 0u;
+        const int64_t row_out = p.N * (p.store == FP8_STORE_F32 ? 4 : p.store == FP8_STORE_BF16 ? 2 : 1);
+        const int64_t row_keep = p.N * (p.keep_bf16 ? 2 : 4);
+        const int out_size = p.store == FP8_STORE_F32 ? 4 : p.store == FP8_STORE_BF16 ? 2 : 1;
+        const int keep_size = p.keep_bf16 ? 2 : 4, in_size = p.in_bf16 ? 2 : 4;
+        uint32_t in_phase = 0;                                         // bit s: parity of slot s
+        uint32_t issued = 0;                                           // bit s: a read into slot s has not been waited for
+        float top = 0.0f;
+        float part[128];
+        bool ok = true;
+        int it = 0;
+        const int slots = tp.s.slots;
+        int slot = 0;                                                  // of the current step; every step takes the next one
+        // lane 0: issue the reads of step `st` of a tile into a slot
+        auto issue = [&](int slot, int st, int64_t row0, int64_t col0) {
+            if (lane == 0) {
+                const uint32_t bar = smem_u32(&bars.in[ew][slot]), at = staging + (uint32_t)slot * tp.s.slot_bytes;
+                const int x = (int)((col0 + st * 32) * in_size);
+                mbar_arrive_expect_tx(bar, tp.s.in_tx);
+#pragma unroll
+                for (int i = 0; i < NIN; ++i) tma_load_3d(at + tp.s.in[i], &maps.in[i], x, (int)row0, 0, bar, stream);
+            }
+            issued |= 1u << slot;
+        };
+        for (int t = worker; t < num_tiles && ok; t += num_workers) {
+            int tm, tn;
+            fused_tile_coords(t, tp.tiles_m, tp.tiles_n, tm, tn);
+            const int64_t row0 = (int64_t)tm * TILE_M + (int)cta_rank * BM + q * 32;
+            const int64_t col0 = (int64_t)tn * OUT_COLS + part_no * WARP_COLS;
+            const bool row_ok = row0 + lane < p.M;
+            // steps with something inside D
+            const int steps = row0 < p.M && col0 < p.N ? (int)min((int64_t)STEPS, (p.N - col0 + 31) / 32) : 0;
+            if (has_in && steps > 0) {
+                if (lane == 0) bulk_wait_read<0>();                    // the previous tile's boxes have left the slots
+                __syncwarp();
+                for (int st = 0; st < min(steps, slots); ++st) issue(slot + st < slots ? slot + st : slot + st - slots, st, row0, col0);
+            }
+            for (int kc = 0; kc < k_pad && ok; kc += chunk, ++it) {
+                const uint32_t acc = (uint32_t)it & 1u;
+                ok = mbar_wait(smem_u32(&bars.acc_full[acc]), ((uint32_t)it >> 1) & 1u, abort_flag, F_WAIT_ACC_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t taddr = tmem + acc * ACC_COLS + ((uint32_t)(q * 32) << 16);
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    uint32_t r[2][32];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        // gated: 64 columns of the gate half, then the same 64 of the up half
+                        const int c = MODE == MODE_GATED ? s2 * 128 + part_no * 64 + h * 32 : part_no * 128 + (2 * s2 + h) * 32;
+                        tc_ld32(taddr + c, r[h]);
+                    }
+                    tc_wait_ld();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            float& s = part[(2 * s2 + h) * 32 + i];
+                            s = (kc != 0 ? s : 0.0f) + __uint_as_float(r[h][i]);
+                        }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bars.acc_empty[acc]), 0));
+            }
+            if (!ok) break;
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                if (st >= steps) break;
+                const uint32_t at = staging + (uint32_t)slot * tp.s.slot_bytes;
+                const int64_t col = col0 + st * 32;
+                const bool ragged = col + 32 > p.N;
+                const bool direct = ragged && (row_out & 15) != 0, direct_keep = ragged && (row_keep & 15) != 0;
+                if (has_in) {
+                    ok = mbar_wait(smem_u32(&bars.in[ew][slot]), (in_phase >> slot) & 1u, abort_flag, F_WAIT_IN);
+                    if (!ok) break;
+                    in_phase ^= 1u << slot;
+                    issued &= ~(1u << slot);
+                } else {
+                    if (lane == 0) {                                   // the boxes last stored from this slot have left it
+                        if (slots >= 4) bulk_wait_read<3>();
+                        else if (slots == 3) bulk_wait_read<2>();
+                        else if (slots == 2) bulk_wait_read<1>();
+                        else bulk_wait_read<0>();
+                    }
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int o = 0; o < 4; ++o) {
+                    const int64_t c = col + o * 8;
+                    if (MODE == MODE_EPILOGUE) {
+                        float z[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const bool in = c + i < p.N;
+                            float bias = 0.0f;
+                            if (p.bias && in) bias = p.bias_bf16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p.bias) + c + i) << 16)
+                                                                 : __ldg(reinterpret_cast<const float*>(p.bias) + c + i);
+                            const float alpha = p.sb_inv_vec ? (in ? sa_inv * __ldg(p.sb_inv_vec + c + i) : 0.0f) : alpha0;
+                            z[i] = fmaf(part[st * 32 + o * 8 + i], alpha, bias);
+                        }
+                        if (p.keep[0]) {
+                            if (direct_keep) { if (row_ok) direct_store8_wide(p.keep[0], p.keep_bf16 != 0, (row0 + lane) * p.ld_keep + c, (int)max((int64_t)0, min((int64_t)8, p.N - c)), z); }
+                            else box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, z);
+                        }
+                        with_activation(p.act, [&](auto tag) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) z[i] = activate<decltype(tag)::value>(z[i]);
+                        });
+                        if (has_in) {
+                            float r[8];
+                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, r);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) z[i] += r[i];
+                        }
+                        emit8(p, p.D[0], at + tp.s.out[0], direct, row_ok, lane, o, row0 + lane, c, z, scale_d, top);
+                    } else if (MODE == MODE_GATED) {
+                        float g[8], u[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { g[i] = part[st * 32 + o * 8 + i] * alpha0; u[i] = part[(64 + st * 32 + o * 8 + i) & 127] * alpha1; }
+                        if (p.keep[0]) {
+                            if (direct_keep) {
+                                const int count = row_ok ? (int)max((int64_t)0, min((int64_t)8, p.N - c)) : 0;
+                                direct_store8_wide(p.keep[0], p.keep_bf16 != 0, (row0 + lane) * p.ld_keep + c, count, g);
+                                direct_store8_wide(p.keep[1], p.keep_bf16 != 0, (row0 + lane) * p.ld_keep + c, count, u);
+                            } else {
+                                box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, g);
+                                box_store8_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, o, u);
+                            }
+                        }
+                        with_activation(p.act, [&](auto tag) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) g[i] = activate<decltype(tag)::value>(g[i]) * u[i];
+                        });
+                        emit8(p, p.D[0], at + tp.s.out[0], direct, row_ok, lane, o, row0 + lane, c, g, scale_d, top);
+                    } else {
+                        float g[8], u[8];
+                        box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, g);
+                        box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, u);
+                        with_activation(p.act, [&](auto tag) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float value, slope;
+                                activate_with_slope<decltype(tag)::value>(g[i], value, slope);
+                                const float dh = part[st * 32 + o * 8 + i] * alpha0;
+                                g[i] = dh * u[i] * slope;
+                                u[i] = dh * value;
+                            }
+                        });
+                        emit8(p, p.D[0], at + tp.s.out[0], direct, row_ok, lane, o, row0 + lane, c, g, scale_d, top);
+                        emit8(p, p.D[NOUT - 1], at + tp.s.out[NOUT - 1], direct, row_ok, lane, o, row0 + lane, c, u, scale_d, top);
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (!direct) {
+#pragma unroll
+                        for (int i = 0; i < NOUT; ++i) tma_store_3d(&maps.out[i], at + tp.s.out[i], (int)(col * out_size), (int)row0, 0, stream);
+                    }
+                    if (MODE != MODE_GATED_BWD && p.keep[0] && !direct_keep) {
+#pragma unroll
+                        for (int i = 0; i < (MODE == MODE_GATED ? 2 : 1); ++i) tma_store_3d(&maps.keep[i], at + tp.s.keep[i], (int)(col * keep_size), (int)row0, 0, stream);
+                    }
+                    bulk_commit();
+                }
+                if (has_in && st + slots < steps) {                    // the slot's next read, once these boxes have left it
+                    if (lane == 0) bulk_wait_read<0>();
+                    __syncwarp();
+                    issue(slot, st + slots, row0, col0);
+                }
+                if (++slot == slots) slot = 0;
+            }
+        }
+        if (!ok) {                                                     // given up: wait (bounded) for reads still in flight
+            for (int s = 0; s < MAX_SLOTS; ++s)
+                if ((issued >> s) & 1u)
+                    for (int spin = 0; spin < (1 << 20) && !mbar_try_wait(smem_u32(&bars.in[ew][s]), (in_phase >> s) & 1u); ++spin) {}
+        }
+        if (lane == 0) bulk_wait_all();                                // every store has reached global memory before exit
+        if (p.amax_bits) {
+            const uint32_t bits = warp_max_u32(canonical_nan_bits(__float_as_uint(top)));
+            if (lane == 0 && bits != 0u) atomicMax(p.amax_bits, bits);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                     // neither CTA leaves while the other may still touch its smem, barriers or TMEM
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TILES_TMEM_COLS) : "memory");
+    }
+}
+
 // ---- host ------------------------------------------------------------------
+
+static bool wide_ok(int t) { return t == FP8_F32 || t == FP8_BF16; }
+static int64_t store_bytes(int store) { return store == FP8_STORE_F32 ? 4 : store == FP8_STORE_BF16 ? 2 : 1; }
+static bool misaligned(const void* p, int64_t pitch_bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0 || (pitch_bytes & 15) != 0; }
 
 static fp8_status launch_cluster(const void* kernel, dim3 grid, dim3 cluster, int threads, uint32_t smem, cudaStream_t st, void** args) {
     cudaLaunchConfig_t cfg = {};
@@ -437,6 +904,32 @@ static bool allow_smem(const void* kernel, uint32_t bytes) {
     return true;
 }
 
+// CTA pairs of a tiles kernel that can be resident at once on the current device (looked up once per kernel and device).
+static int pair_workers(const void* kernel) {
+    static std::mutex mu;
+    static struct { const void* k; int n; } known[64][4] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / 2;
+    std::lock_guard<std::mutex> lock(mu);
+    int i = 0;
+    while (i < 4 && known[dev][i].k && known[dev][i].k != kernel) ++i;
+    if (i < 4 && known[dev][i].k == kernel) return known[dev][i].n;
+    int n = sm_count() / 2, clusters = 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * n), 1, 1);
+    cfg.blockDim = dim3(TILES_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = TILES_SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0 && clusters < n) n = clusters;
+    if (i < 4) { known[dev][i].k = kernel; known[dev][i].n = n; }
+    return n;
+}
+
 template <int MODE, int T>
 static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
     using G = RowsGeo<MODE, T>;
@@ -465,9 +958,71 @@ static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const ui
     return launch_cluster(k, dim3((unsigned)tiles_n, (unsigned)tiles_t, slices), dim3(1, 1, slices), ROWS_THREADS, smem, st, args);
 }
 
+// Tensor map of a wide or FP8 matrix in boxes of 32 rows x 32 columns (`size` bytes per element).
+static bool make_box_map(CUtensorMap* map, const void* base, const Params& p, int64_t ld, int size) {
+    const CUtensorMapSwizzle swizzle = size == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : size == 2 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
+    return make_map(map, base, (uint64_t)(p.N * size), (uint64_t)p.M, (uint64_t)(ld * size), 1, 0, (uint32_t)(32 * size), 32, swizzle);
+}
+
+template <int MODE>
+static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
+    const bool a_mn = d->ma == FP8_MAJOR_MN, w_mn = d->mb == FP8_MAJOR_MN;
+    TilesMaps m = {};
+    TilesParams tp = {};
+    bool ok = a_mn ? make_map(&m.a, A, (uint64_t)d->M, (uint64_t)d->K, (uint64_t)d->lda, 1, 0, 128, BK)
+                   : make_map(&m.a, A, (uint64_t)d->K, (uint64_t)d->M, (uint64_t)d->lda, 1, 0, BK, BM);
+    const uint64_t inner = (uint64_t)(w_mn ? d->N : d->K), outer = (uint64_t)(w_mn ? d->K : d->N);
+    ok = ok && make_map(&m.b[0], B0, inner, outer, (uint64_t)d->ldb, 1, 0, 128, 128);
+    ok = ok && (!B1 || make_map(&m.b[1], B1, inner, outer, (uint64_t)d->ldb, 1, 0, 128, 128));
+    // boxes of the epilogue and their places in a staging slot; an output of the size of an input takes its place
+    const int out_size = (int)store_bytes(p.store), in_size = p.in_bf16 ? 2 : 4, keep_size = p.keep_bf16 ? 2 : 4;
+    uint32_t at = 0;
+    for (int i = 0; i < 2; ++i) {
+        if (p.in[i]) {
+            ok = ok && make_box_map(&m.in[i], p.in[i], p, p.ld_in, in_size);
+            tp.s.in[i] = at;
+            at += 1024u * in_size;
+            tp.s.in_tx += 1024u * in_size;
+        }
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (p.D[i]) {
+            ok = ok && make_box_map(&m.out[i], p.D[i], p, p.ldd, out_size);
+            if (p.in[i] && in_size == out_size) tp.s.out[i] = tp.s.in[i];
+            else { tp.s.out[i] = at; at += 1024u * out_size; }
+        }
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (p.keep[i]) {
+            ok = ok && make_box_map(&m.keep[i], p.keep[i], p, p.ld_keep, keep_size);
+            tp.s.keep[i] = at;
+            at += 1024u * keep_size;
+        }
+    }
+    if (!ok) return FP8_ERR_CUDA;
+    tp.s.slot_bytes = at;
+    tp.s.slots = (int)(TILES_WARP_BYTES / at) < MAX_SLOTS ? (int)(TILES_WARP_BYTES / at) : MAX_SLOTS;
+    p.a_mn = a_mn ? 1 : 0; p.w_mn = w_mn ? 1 : 0;
+    p.idesc = (1u << 4) | ((uint32_t)d->fa << 7) | ((uint32_t)d->fb << 10) | ((a_mn ? 1u : 0u) << 15) | ((w_mn ? 1u : 0u) << 16) |
+              ((uint32_t)(ACC_COLS >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
+    const int out_cols = MODE == MODE_GATED ? 128 : 256;
+    const int64_t tiles_m = (d->M + TILE_M - 1) / TILE_M, tiles_n = (d->N + out_cols - 1) / out_cols;
+    if (tiles_m * tiles_n > (int64_t)1 << 30) return FP8_ERR_UNSUPPORTED;
+    const int k_pad = (int)((d->K + BK - 1) / BK + TILES_FG - 1) / TILES_FG * TILES_FG;
+    tp.p = p;
+    tp.tiles_m = (int)tiles_m; tp.tiles_n = (int)tiles_n;
+    tp.chunk_blocks = d->acc == FP8_ACC_SPLIT ? TILES_SPLIT_BLOCKS : k_pad;
+    const void* k = reinterpret_cast<const void*>(&k_fused_tiles<MODE>);
+    if (!allow_smem(k, TILES_SMEM)) return FP8_ERR_CUDA;
+    const int workers = pair_workers(k);
+    const int64_t use = tiles_m * tiles_n < workers ? tiles_m * tiles_n : workers;
+    void* args[] = {&m, &tp};
+    return launch_cluster(k, dim3((unsigned)(2 * use), 1, 1), dim3(2, 1, 1), TILES_THREADS, TILES_SMEM, st, args);
+}
+
 template <int MODE>
 static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
-    if (d->ma == FP8_MAJOR_MN) return FP8_ERR_UNSUPPORTED;
+    if (d->K > 0 && (d->M > 64 || d->ma == FP8_MAJOR_MN)) return launch_tiles<MODE>(d, A, B0, B1, p, st);
     if (d->M <= 16) return launch_rows<MODE, 16>(d, A, B0, B1, p, st);
     if (d->M <= 32) return launch_rows<MODE, 32>(d, A, B0, B1, p, st);
     return launch_rows<MODE, 64>(d, A, B0, B1, p, st);
@@ -481,10 +1036,6 @@ static bool enums_ok(const fp8_gemm_desc* d, int act, int store, int overflow) {
            (d->acc == FP8_ACC_FAST || d->acc == FP8_ACC_SPLIT) && act >= FP8_ACT_NONE && act <= FP8_ACT_SILU &&
            store >= FP8_STORE_F32 && store <= FP8_STORE_E5M2 && (overflow == FP8_SATURATE || overflow == FP8_NOSAT);
 }
-static bool wide_ok(int t) { return t == FP8_F32 || t == FP8_BF16; }
-static int64_t store_bytes(int store) { return store == FP8_STORE_F32 ? 4 : store == FP8_STORE_BF16 ? 2 : 1; }
-static bool misaligned(const void* p, int64_t pitch_bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0 || (pitch_bytes & 15) != 0; }
-
 // operands and D; `B1` only where the mode has it
 static fp8_status check_product(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, bool two,
                                 const void* D0, const void* D1, bool two_out, int store) {

@@ -180,7 +180,7 @@ def _run_epilogue(M, N, K, ma, mb, act, bias_t, res_t, pre_t, out, channel, fa=E
     return D, v, amax
 
 
-@pytest.mark.parametrize("case", [c for c in EPILOGUES if c[3] == K_], ids=lambda c: "%dx%dx%d_%s" % (c[0], c[1], c[2], c[5]))
+@pytest.mark.parametrize("case", EPILOGUES, ids=lambda c: "%dx%dx%d_%s" % (c[0], c[1], c[2], c[5]))
 def test_epilogue(case):
     _run_epilogue(*case)
 
@@ -284,7 +284,7 @@ GATED = [
 ]
 
 
-@pytest.mark.parametrize("case", [c for c in GATED if c[3] == K_], ids=lambda c: "%dx%dx%d_%s" % (c[0], c[1], c[2], c[5]))
+@pytest.mark.parametrize("case", GATED, ids=lambda c: "%dx%dx%d_%s" % (c[0], c[1], c[2], c[5]))
 @pytest.mark.parametrize("packed", [False, True])
 def test_gated(case, packed):
     M, N, K, ma, mb, act, save, out = case
@@ -345,7 +345,7 @@ GATED_BWD = [
 ]
 
 
-@pytest.mark.parametrize("case", [c for c in GATED_BWD if c[3] == K_], ids=lambda c: "%dx%dx%d_%s" % (c[0], c[1], c[2], c[5]))
+@pytest.mark.parametrize("case", GATED_BWD, ids=lambda c: "%dx%dx%d_%s" % (c[0], c[1], c[2], c[5]))
 def test_gated_backward(case):
     M, N, K, ma, mb, act, gate_t, out = case
     g = _gen(M * 3 + N + K)
@@ -465,7 +465,7 @@ def test_seeded_shapes():
         M, N, K = (int(2 ** r.uniform(0, 9.5)) for _ in range(3))
         out = r.choice([BF, F32, E4, E5])
         pick = lambda: r.choice([None, BF, F32])  # noqa: E731
-        _run_epilogue(M, N, K, K_, r.choice([K_, MN]), r.choice(list(ACTS)), pick(), pick(), pick(), out, r.random() < 0.3, seed=i)
+        _run_epilogue(M, N, K, r.choice([K_, MN]), r.choice([K_, MN]), r.choice(list(ACTS)), pick(), pick(), pick(), out, r.random() < 0.3, seed=i)
 
 
 def test_refusals():
