@@ -498,54 +498,82 @@ __device__ __forceinline__ void box_store8_wide(uint32_t box, bool bf16, int row
     }
 }
 
-// Eight values of a row written to global memory one by one: where a box crosses the right edge of rows whose length is
-// not a multiple of 16 bytes (the TMA unit clips in such units).
-__device__ __forceinline__ void direct_store8_wide(void* base, bool bf16, int64_t at, int count, const float (&v)[8]) {
+// FP8 codes of eight values of which one is special (or, non-saturating, too large): one at a time, kept small.
+__device__ __forceinline__ uint2 encode8_special(const float (&v)[8], float scale_d, bool e4m3, bool nosat) {
+    uint64_t codes = 0;
+#pragma unroll 1
+    for (int i = 7; i >= 0; --i) {
+        float x = v[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= count) break;
-        if (bf16) reinterpret_cast<uint16_t*>(base)[at + i] = (uint16_t)pack_bf16(v[i], 0.0f);
-        else reinterpret_cast<float*>(base)[at + i] = v[i];
+        for (int j = 1; j < 8; ++j) x = i == j ? v[j] : x;
+        const float y = x * scale_d;
+        uint32_t code;
+        if (y != y) code = ((__float_as_uint(x) >> 24) & 0x80u) | 0x7Fu;
+        else if (e4m3) code = nosat ? encode_scalar<kE4M3, true>(y) : encode_scalar<kE4M3, false>(y);
+        else code = nosat ? encode_scalar<kE5M2, true>(y) : encode_scalar<kE5M2, false>(y);
+        codes = codes << 8 | code;
     }
+    return make_uint2((uint32_t)codes, (uint32_t)(codes >> 32));
 }
 
-// One output of the epilogue: conversion, amax, staging (or the direct form).
-__device__ __forceinline__ void emit8(const Params& p, void* D, uint32_t box, bool direct, bool row_ok, int row, int o, int64_t grow, int64_t col,
-                                      float (&v)[8], float scale_d, float& top) {
-    const int count = row_ok ? (int)max((int64_t)0, min((int64_t)8, p.N - col)) : 0;
-    if (p.store == FP8_STORE_BF16) {
+// One octet of an output: its magnitudes (NaN once any is NaN), conversion, staging.  Rounding and scaling are monotonic,
+// so the largest magnitude before them decides the amax after rounding and whether a conversion can overflow.
+__device__ __forceinline__ float emit8(const Params& p, uint32_t box, int row, int o, const float (&v)[8], float scale_d) {
+    float most = fabsf(v[0]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(pack_bf16(v[i], 0.0f) << 16);
-    }
-    if (count == 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmax_nan(top, fabsf(v[i]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) top = fmax_nan(top, fabsf(v[i]));
-    }
+    for (int i = 1; i < 8; ++i) most = fmax_nan(most, fabsf(v[i]));
     if (p.store <= FP8_STORE_BF16) {
-        if (direct) direct_store8_wide(D, p.store == FP8_STORE_BF16, grow * p.ldd + col, count, v);
-        else box_store8_wide(box, p.store == FP8_STORE_BF16, row, o, v);
-        return;
+        box_store8_wide(box, p.store == FP8_STORE_BF16, row, o, v);
+        return most;
     }
-    const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-    uint32_t w0, w1;
-    if (p.store == FP8_STORE_E4M3) { w0 = encode4<kE4M3>(lo, scale_d, p.nosat != 0); w1 = encode4<kE4M3>(hi, scale_d, p.nosat != 0); }
-    else                           { w0 = encode4<kE5M2>(lo, scale_d, p.nosat != 0); w1 = encode4<kE5M2>(hi, scale_d, p.nosat != 0); }
-    if (direct) {
-        uint8_t* d = reinterpret_cast<uint8_t*>(D) + grow * p.ldd + col;
+    const bool e4m3 = p.store == FP8_STORE_E4M3;
+    const float far = most * fabsf(scale_d);
+    const bool over = e4m3 ? far > Fmt<kE4M3>::nosat_limit : far >= Fmt<kE5M2>::nosat_limit;
+    uint2 w;
+    if (far <= 3.402823466e38f && !(p.nosat && over)) {
+        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) d[i] = (uint8_t)((i < 4 ? w0 : w1) >> (8 * (i & 3)));
+        for (int i = 0; i < 8; ++i) y[i] = v[i] * scale_d;
+        w = e4m3 ? make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7]))
+                 : make_uint2(cvt_quad<kE5M2>(y[0], y[1], y[2], y[3]), cvt_quad<kE5M2>(y[4], y[5], y[6], y[7]));
     } else {
-        const uint32_t at = box + box_offset(32, row, o >> 1) + (uint32_t)(o & 1) * 8;
-        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w0), "r"(w1) : "memory");
+        w = encode8_special(v, scale_d, e4m3, p.nosat != 0);
+    }
+    const uint32_t at = box + box_offset(32, row, o >> 1) + (uint32_t)(o & 1) * 8;
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w.x), "r"(w.y) : "memory");
+    return most;
+}
+
+// A staged box written to global memory element by element: where it crosses the right edge of rows whose length is not a
+// multiple of 16 bytes (the TMA unit clips in such units).  Lane = column.
+__device__ __forceinline__ void copy_box_out(void* base, int size, uint32_t box, int64_t row0, int rows, int64_t col, int64_t ld, int lane, bool inside) {
+    __syncwarp();
+    const int byte = lane * size;
+#pragma unroll 1
+    for (int r = 0; r < rows && inside; ++r) {
+        const uint32_t at = box + box_offset(32 * size, r, byte >> 4) + (uint32_t)(byte & 15);
+        uint8_t* to = reinterpret_cast<uint8_t*>(base) + ((row0 + r) * ld + col + lane) * size;
+        uint32_t w;
+        if (size == 4) {
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+            *reinterpret_cast<uint32_t*>(to) = w;
+        } else if (size == 2) {
+            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+            *reinterpret_cast<uint16_t*>(to) = (uint16_t)w;
+        } else {
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+            *to = (uint8_t)w;
+        }
     }
 }
 
-template <int MODE>
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+template <int MODE, int ACT>
 __global__ void __launch_bounds__(TILES_THREADS, 1)
 k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ TilesParams tp) {
     const Params& p = tp.p;
@@ -671,10 +699,10 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
         const uint32_t staging = ring + TILES_STAGES * TILES_STAGE_BYTES + (uint32_t)ew * TILES_WARP_BYTES;
         const uint64_t stream = policy_evict_first();
         const bool has_in = tp.s.in_tx != 0u;
-        const int64_t row_out = p.N * (p.store == FP8_STORE_F32 ? 4 : p.store == FP8_STORE_BF16 ? 2 : 1);
-        const int64_t row_keep = p.N * (p.keep_bf16 ? 2 : 4);
         const int out_size = p.store == FP8_STORE_F32 ? 4 : p.store == FP8_STORE_BF16 ? 2 : 1;
         const int keep_size = p.keep_bf16 ? 2 : 4, in_size = p.in_bf16 ? 2 : 4;
+        const bool clip_out = ((p.N * out_size) & 15) != 0, clip_keep = ((p.N * keep_size) & 15) != 0;
+        const uint32_t columns = staging + TILES_WARP_BYTES - 1024;    // 128 factors, 128 biases of this warp's columns
         uint32_t in_phase = 0;                                         // bit s: parity of slot s
         uint32_t issued = 0;                                           // bit s: a read into slot s has not been waited for
         float top = 0.0f;
@@ -702,6 +730,21 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
             const bool row_ok = row0 + lane < p.M;
             // steps with something inside D
             const int steps = row0 < p.M && col0 < p.N ? (int)min((int64_t)STEPS, (p.N - col0 + 31) / 32) : 0;
+            if (MODE == MODE_EPILOGUE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t c = col0 + i * 32 + lane;
+                    float factor = alpha0, bias = 0.0f;
+                    if (c < p.N) {
+                        if (p.sb_inv_vec) factor = sa_inv * __ldg(p.sb_inv_vec + c);
+                        if (p.bias) bias = p.bias_bf16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p.bias) + c) << 16)
+                                                       : __ldg(reinterpret_cast<const float*>(p.bias) + c);
+                    }
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(columns + (uint32_t)(i * 32 + lane) * 4), "f"(factor) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(columns + 512 + (uint32_t)(i * 32 + lane) * 4), "f"(bias) : "memory");
+                }
+                __syncwarp();
+            }
             if (has_in && steps > 0) {
                 if (lane == 0) bulk_wait_read<0>();                    // the previous tile's boxes have left the slots
                 __syncwarp();
@@ -736,13 +779,13 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bars.acc_empty[acc]), 0));
             }
             if (!ok) break;
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                if (st >= steps) break;
+            // The loop over steps is rolled (its body alone is hundreds of instructions; unrolled, the epilogue warps wait
+            // for instruction fetches): each round works on the first 32 sums and then moves the others down.
+#pragma unroll 1
+            for (int st = 0; st < steps; ++st) {
                 const uint32_t at = staging + (uint32_t)slot * tp.s.slot_bytes;
                 const int64_t col = col0 + st * 32;
                 const bool ragged = col + 32 > p.N;
-                const bool direct = ragged && (row_out & 15) != 0, direct_keep = ragged && (row_keep & 15) != 0;
                 if (has_in) {
                     ok = mbar_wait(smem_u32(&bars.in[ew][slot]), (in_phase >> slot) & 1u, abort_flag, F_WAIT_IN);
                     if (!ok) break;
@@ -757,80 +800,79 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                     }
                     __syncwarp();
                 }
+                float most = 0.0f;
 #pragma unroll
                 for (int o = 0; o < 4; ++o) {
-                    const int64_t c = col + o * 8;
+                    float x[8], y[8];
                     if (MODE == MODE_EPILOGUE) {
-                        float z[8];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float4 f = ld_shared_f4(columns + (uint32_t)(st * 32 + o * 8 + h * 4) * 4);
+                            const float4 b = ld_shared_f4(columns + 512 + (uint32_t)(st * 32 + o * 8 + h * 4) * 4);
+                            x[h * 4 + 0] = fmaf(part[o * 8 + h * 4 + 0], f.x, b.x);
+                            x[h * 4 + 1] = fmaf(part[o * 8 + h * 4 + 1], f.y, b.y);
+                            x[h * 4 + 2] = fmaf(part[o * 8 + h * 4 + 2], f.z, b.z);
+                            x[h * 4 + 3] = fmaf(part[o * 8 + h * 4 + 3], f.w, b.w);
+                        }
+                        if (p.keep[0]) box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, x);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = activate<ACT>(x[i]);
+                        if (has_in) {
+                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, y);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] += y[i];
+                        }
+                    } else if (MODE == MODE_GATED) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { x[i] = part[o * 8 + i] * alpha0; y[i] = part[64 + o * 8 + i] * alpha1; }
+                        if (p.keep[0]) {
+                            box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, x);
+                            box_store8_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, o, y);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = activate<ACT>(x[i]) * y[i];
+                    } else {
+                        box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, x);
+                        box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, y);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const bool in = c + i < p.N;
-                            float bias = 0.0f;
-                            if (p.bias && in) bias = p.bias_bf16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p.bias) + c + i) << 16)
-                                                                 : __ldg(reinterpret_cast<const float*>(p.bias) + c + i);
-                            const float alpha = p.sb_inv_vec ? (in ? sa_inv * __ldg(p.sb_inv_vec + c + i) : 0.0f) : alpha0;
-                            z[i] = fmaf(part[st * 32 + o * 8 + i], alpha, bias);
+                            float value, slope;
+                            activate_with_slope<ACT>(x[i], value, slope);
+                            const float dh = part[o * 8 + i] * alpha0;
+                            x[i] = dh * y[i] * slope;
+                            y[i] = dh * value;
                         }
-                        if (p.keep[0]) {
-                            if (direct_keep) { if (row_ok) direct_store8_wide(p.keep[0], p.keep_bf16 != 0, (row0 + lane) * p.ld_keep + c, (int)max((int64_t)0, min((int64_t)8, p.N - c)), z); }
-                            else box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, z);
-                        }
-                        with_activation(p.act, [&](auto tag) {
+                    }
+                    if (ragged) {                                      // columns past N count for nothing
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) z[i] = activate<decltype(tag)::value>(z[i]);
-                        });
-                        if (has_in) {
-                            float r[8];
-                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, r);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) z[i] += r[i];
-                        }
-                        emit8(p, p.D[0], at + tp.s.out[0], direct, row_ok, lane, o, row0 + lane, c, z, scale_d, top);
-                    } else if (MODE == MODE_GATED) {
-                        float g[8], u[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { g[i] = part[st * 32 + o * 8 + i] * alpha0; u[i] = part[(64 + st * 32 + o * 8 + i) & 127] * alpha1; }
-                        if (p.keep[0]) {
-                            if (direct_keep) {
-                                const int count = row_ok ? (int)max((int64_t)0, min((int64_t)8, p.N - c)) : 0;
-                                direct_store8_wide(p.keep[0], p.keep_bf16 != 0, (row0 + lane) * p.ld_keep + c, count, g);
-                                direct_store8_wide(p.keep[1], p.keep_bf16 != 0, (row0 + lane) * p.ld_keep + c, count, u);
-                            } else {
-                                box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, g);
-                                box_store8_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, o, u);
-                            }
-                        }
-                        with_activation(p.act, [&](auto tag) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) g[i] = activate<decltype(tag)::value>(g[i]) * u[i];
-                        });
-                        emit8(p, p.D[0], at + tp.s.out[0], direct, row_ok, lane, o, row0 + lane, c, g, scale_d, top);
-                    } else {
-                        float g[8], u[8];
-                        box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, g);
-                        box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, u);
-                        with_activation(p.act, [&](auto tag) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                float value, slope;
-                                activate_with_slope<decltype(tag)::value>(g[i], value, slope);
-                                const float dh = part[st * 32 + o * 8 + i] * alpha0;
-                                g[i] = dh * u[i] * slope;
-                                u[i] = dh * value;
-                            }
-                        });
-                        emit8(p, p.D[0], at + tp.s.out[0], direct, row_ok, lane, o, row0 + lane, c, g, scale_d, top);
-                        emit8(p, p.D[NOUT - 1], at + tp.s.out[NOUT - 1], direct, row_ok, lane, o, row0 + lane, c, u, scale_d, top);
+                        for (int i = 0; i < 8; ++i)
+                            if (col + o * 8 + i >= p.N) x[i] = y[i] = 0.0f;
+                    }
+                    most = fmax_nan(most, emit8(p, at + tp.s.out[0], lane, o, x, scale_d));
+                    if (MODE == MODE_GATED_BWD) most = fmax_nan(most, emit8(p, at + tp.s.out[NOUT - 1], lane, o, y, scale_d));
+                }
+                if (row_ok) top = fmax_nan(top, most);
+                const bool by_hand = ragged && clip_out, keep_by_hand = ragged && clip_keep;
+                if (ragged) {
+                    const int rows = (int)min((int64_t)32, p.M - row0);
+                    const bool inside = col + lane < p.N;
+                    if (by_hand) {
+                        copy_box_out(p.D[0], out_size, at + tp.s.out[0], row0, rows, col, p.ldd, lane, inside);
+                        if (MODE == MODE_GATED_BWD) copy_box_out(p.D[1], out_size, at + tp.s.out[NOUT - 1], row0, rows, col, p.ldd, lane, inside);
+                    }
+                    if (MODE != MODE_GATED_BWD && keep_by_hand && p.keep[0]) {
+                        copy_box_out(p.keep[0], keep_size, at + tp.s.keep[0], row0, rows, col, p.ld_keep, lane, inside);
+                        if (MODE == MODE_GATED) copy_box_out(p.keep[1], keep_size, at + tp.s.keep[1], row0, rows, col, p.ld_keep, lane, inside);
                     }
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (!direct) {
+                    if (!by_hand) {
 #pragma unroll
                         for (int i = 0; i < NOUT; ++i) tma_store_3d(&maps.out[i], at + tp.s.out[i], (int)(col * out_size), (int)row0, 0, stream);
                     }
-                    if (MODE != MODE_GATED_BWD && p.keep[0] && !direct_keep) {
+                    if (MODE != MODE_GATED_BWD && p.keep[0] && !keep_by_hand) {
 #pragma unroll
                         for (int i = 0; i < (MODE == MODE_GATED ? 2 : 1); ++i) tma_store_3d(&maps.keep[i], at + tp.s.keep[i], (int)(col * keep_size), (int)row0, 0, stream);
                     }
@@ -842,6 +884,13 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                     issue(slot, st + slots, row0, col0);
                 }
                 if (++slot == slots) slot = 0;
+                if (MODE == MODE_GATED) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) { part[i] = part[32 + i]; part[64 + i] = part[96 + i]; }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 96; ++i) part[i] = part[32 + i];
+                }
             }
         }
         if (!ok) {                                                     // given up: wait (bounded) for reads still in flight
@@ -851,6 +900,7 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
         }
         if (lane == 0) bulk_wait_all();                                // every store has reached global memory before exit
         if (p.amax_bits) {
+            if (p.store == FP8_STORE_BF16) top = __uint_as_float(pack_bf16(top, 0.0f) << 16);      // of the values as stored
             const uint32_t bits = warp_max_u32(canonical_nan_bits(__float_as_uint(top)));
             if (lane == 0 && bits != 0u) atomicMax(p.amax_bits, bits);
         }
@@ -907,13 +957,13 @@ static bool allow_smem(const void* kernel, uint32_t bytes) {
 // CTA pairs of a tiles kernel that can be resident at once on the current device (looked up once per kernel and device).
 static int pair_workers(const void* kernel) {
     static std::mutex mu;
-    static struct { const void* k; int n; } known[64][4] = {};
+    static struct { const void* k; int n; } known[64][16] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / 2;
     std::lock_guard<std::mutex> lock(mu);
     int i = 0;
-    while (i < 4 && known[dev][i].k && known[dev][i].k != kernel) ++i;
-    if (i < 4 && known[dev][i].k == kernel) return known[dev][i].n;
+    while (i < 16 && known[dev][i].k && known[dev][i].k != kernel) ++i;
+    if (i < 16 && known[dev][i].k == kernel) return known[dev][i].n;
     int n = sm_count() / 2, clusters = 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * n), 1, 1);
@@ -926,7 +976,7 @@ static int pair_workers(const void* kernel) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0 && clusters < n) n = clusters;
-    if (i < 4) { known[dev][i].k = kernel; known[dev][i].n = n; }
+    if (i < 16) { known[dev][i].k = kernel; known[dev][i].n = n; }
     return n;
 }
 
@@ -964,7 +1014,7 @@ static bool make_box_map(CUtensorMap* map, const void* base, const Params& p, in
     return make_map(map, base, (uint64_t)(p.N * size), (uint64_t)p.M, (uint64_t)(ld * size), 1, 0, (uint32_t)(32 * size), 32, swizzle);
 }
 
-template <int MODE>
+template <int MODE, int ACT>
 static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
     const bool a_mn = d->ma == FP8_MAJOR_MN, w_mn = d->mb == FP8_MAJOR_MN;
     TilesMaps m = {};
@@ -1001,7 +1051,8 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
     }
     if (!ok) return FP8_ERR_CUDA;
     tp.s.slot_bytes = at;
-    tp.s.slots = (int)(TILES_WARP_BYTES / at) < MAX_SLOTS ? (int)(TILES_WARP_BYTES / at) : MAX_SLOTS;
+    const uint32_t room = MODE == MODE_EPILOGUE ? TILES_WARP_BYTES - 1024 : TILES_WARP_BYTES;      // 8 KB + column values, 12 KB, 12 KB at most
+    tp.s.slots = (int)(room / at) < MAX_SLOTS ? (int)(room / at) : MAX_SLOTS;
     p.a_mn = a_mn ? 1 : 0; p.w_mn = w_mn ? 1 : 0;
     p.idesc = (1u << 4) | ((uint32_t)d->fa << 7) | ((uint32_t)d->fb << 10) | ((a_mn ? 1u : 0u) << 15) | ((w_mn ? 1u : 0u) << 16) |
               ((uint32_t)(ACC_COLS >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
@@ -1012,7 +1063,7 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
     tp.p = p;
     tp.tiles_m = (int)tiles_m; tp.tiles_n = (int)tiles_n;
     tp.chunk_blocks = d->acc == FP8_ACC_SPLIT ? TILES_SPLIT_BLOCKS : k_pad;
-    const void* k = reinterpret_cast<const void*>(&k_fused_tiles<MODE>);
+    const void* k = reinterpret_cast<const void*>(&k_fused_tiles<MODE, ACT>);
     if (!allow_smem(k, TILES_SMEM)) return FP8_ERR_CUDA;
     const int workers = pair_workers(k);
     const int64_t use = tiles_m * tiles_n < workers ? tiles_m * tiles_n : workers;
@@ -1022,7 +1073,15 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
 
 template <int MODE>
 static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
-    if (d->K > 0 && (d->M > 64 || d->ma == FP8_MAJOR_MN)) return launch_tiles<MODE>(d, A, B0, B1, p, st);
+    if (d->K > 0 && (d->M > 64 || d->ma == FP8_MAJOR_MN)) {
+        switch (p.act) {
+            case FP8_ACT_RELU: return launch_tiles<MODE, FP8_ACT_RELU>(d, A, B0, B1, p, st);
+            case FP8_ACT_GELU: return launch_tiles<MODE, FP8_ACT_GELU>(d, A, B0, B1, p, st);
+            case FP8_ACT_GELU_TANH: return launch_tiles<MODE, FP8_ACT_GELU_TANH>(d, A, B0, B1, p, st);
+            case FP8_ACT_SILU: return launch_tiles<MODE, FP8_ACT_SILU>(d, A, B0, B1, p, st);
+            default: return launch_tiles<MODE, FP8_ACT_NONE>(d, A, B0, B1, p, st);
+        }
+    }
     if (d->M <= 16) return launch_rows<MODE, 16>(d, A, B0, B1, p, st);
     if (d->M <= 32) return launch_rows<MODE, 32>(d, A, B0, B1, p, st);
     return launch_rows<MODE, 64>(d, A, B0, B1, p, st);
