@@ -422,6 +422,60 @@ fp8_status fp8_gemm_gated_backward(const fp8_gemm_desc* d, const fp8_gated* w, c
                                    float* amax_dev, void* stream);
 
 /*
+ * fp8_epilogue_backward — the backward pass of fp8_gemm_epilogue up to its product, in one pass over the output gradient:
+ *   dz[i,j] = dy[i,j] * act'(pre[i,j])                          (binary32)
+ *   out[i,j] = dz rounded to the wide type, or encode(dz * scale_dz): the E5M2 operand of the data and weight gradients
+ *   dbias[j] = sum_i dz[i,j]                                    (binary32, from dz before its conversion; OVERWRITTEN)
+ *   *amax_dev = amax of out as stored (wide types), of dz before scaling and conversion (FP8)
+ * (the gradient of the residual is dy itself).  dy, pre: M x N wide, pitches ldy, ldp; pre may be NULL when act is
+ * FP8_ACT_NONE.  dbias_dev (N floats) and amax_dev may be NULL.  M == 0 gives dbias = 0.  The sums are added in an order
+ * that depends on the shape alone: repeated calls give the same bits.
+ * Alignment: dy, pre and out 16-byte aligned with pitches that are multiples of 16 bytes (FP8_ERR_ALIGN).  out may be dy
+ * itself (same address, pitch and type).
+ *   workspace  needed when dbias_dev is given: fp8_epilogue_backward_workspace_bytes(M, N) bytes, 16-byte aligned.  It must
+ *              hold zeros before its first use; every call leaves the part that matters zeroed again, so one buffer of the
+ *              largest size serves any number of calls on one stream.  Calls that may overlap need different workspaces.
+ */
+size_t fp8_epilogue_backward_workspace_bytes(int64_t M, int64_t N);
+fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const void* dy, fp8_wide dy_t, int64_t ldy,
+                                 const void* pre, fp8_wide pre_t, int64_t ldp, fp8_store store, fp8_overflow overflow,
+                                 const float* scale_dz_dev, void* out, int64_t ldo, float* dbias_dev, float* amax_dev,
+                                 void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * Global gradient norm and clipping over many tensors — Section 4.1 trains with the recipes of the higher-precision
+ * baselines, of which norm clipping is a part; weight gradients are wide tensors.
+ *   norm = sqrt(sum over all tensors of x^2);   coef = norm <= max_norm ? 1 : max_norm / norm;   out = round(x * coef)
+ * The squares are binary32 (a magnitude above 1.8e19 overflows to an infinite norm, one below 1e-23 counts as 0); sums of
+ * 64 and more of them are carried on in binary64.  The order of the additions depends on the plan alone.  A NaN anywhere
+ * gives a NaN norm and NaN everywhere in out; an infinite norm gives coef = 0 (0 for finite x, NaN for infinite x).
+ *
+ * A plan is made once for a list of tensors (their addresses, sizes and types):
+ *   fp8_clip_plan_size   fills *plan with the sizes of the table and of the workspace for these items.
+ *   fp8_clip_plan_fill   writes the table (plan->table_bytes) to HOST memory; the caller copies it to the device.
+ * fp8_grad_norm writes *norm_dev.  fp8_grad_clip writes *norm_dev and every out (out == x clips in place; then nothing is
+ * written when coef is 1).  The workspace: device, plan->workspace_bytes, 16-byte aligned, zero before its first use; every
+ * call leaves the part that matters zeroed.  Items need the alignment of their elements only (16 bytes are faster); x_t and
+ * out_t may differ, and out may overlap nothing but its own x.  max_norm below 0 or NaN: FP8_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    const void* x;
+    void* out;                  /* NULL: counted in the norm, not written */
+    int64_t n;
+    fp8_wide x_t, out_t;
+} fp8_clip_item;
+typedef struct {
+    int64_t count, chunks;
+    size_t table_bytes, workspace_bytes;
+} fp8_clip_plan;
+
+fp8_status fp8_clip_plan_size(const fp8_clip_item* items, int64_t count, fp8_clip_plan* plan);
+fp8_status fp8_clip_plan_fill(const fp8_clip_item* items, const fp8_clip_plan* plan, void* table_host);
+fp8_status fp8_grad_norm(const fp8_clip_plan* plan, const void* table_dev, void* workspace_dev, float* norm_dev, void* stream);
+fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void* workspace_dev, float max_norm,
+                         float* norm_dev, void* stream);
+
+/*
  * fp8_async_status — reads and clears the device-side error latch of the
  * current device (synchronises the device).  FP8_OK, or FP8_ERR_TIMEOUT if a
  * kernel gave up on a bounded wait since the last call; *detail (optional, host

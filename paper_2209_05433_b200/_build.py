@@ -8,8 +8,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfp8_b200.so")
-SOURCES = ["cast.cu", "gemm.cu", "fused.cu"]
-HEADERS = ["common.cuh", "codec.cuh", "umma.cuh", "activation.cuh", os.path.join("..", "..", "include", "fp8_b200.h")]
+SOURCES = ["cast.cu", "gemm.cu", "fused.cu", "grads.cu"]
+HEADERS = ["common.cuh", "codec.cuh", "umma.cuh", "activation.cuh", "octet.cuh", os.path.join("..", "..", "include", "fp8_b200.h")]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",

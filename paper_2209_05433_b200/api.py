@@ -28,6 +28,8 @@ EXPORTS = ["fp8_amax", "fp8_scale_from_amax", "fp8_quantize", "fp8_quantize_curr
            "fp8_quantize_channels", "fp8_quantize_transpose", "fp8_gemm_channel_scales", "fp8_gemm_batched",
            "fp8_gemm_splitk", "fp8_gemm_splitk_workspace",
            "fp8_gemm_epilogue", "fp8_gemm_gated", "fp8_gemm_gated_backward",
+           "fp8_epilogue_backward", "fp8_epilogue_backward_workspace_bytes",
+           "fp8_clip_plan_size", "fp8_clip_plan_fill", "fp8_grad_norm", "fp8_grad_clip",
            "fp8_async_status", "fp8_self_test_expire_wait", "fp8_sm_clock_probe", "fp8_status_string", "fp8_launch_count"]
 
 
@@ -50,6 +52,15 @@ class Epilogue(ctypes.Structure):
 class Gated(ctypes.Structure):
     _fields_ = [("act", ctypes.c_int), ("store", ctypes.c_int), ("overflow", ctypes.c_int), ("gate_t", ctypes.c_int),
                 ("gate", ctypes.c_void_p), ("up", ctypes.c_void_p), ("ldg", ctypes.c_int64)]
+
+
+class ClipItem(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("x_t", ctypes.c_int), ("out_t", ctypes.c_int)]
+
+
+class ClipSizes(ctypes.Structure):
+    """fp8_clip_plan of the header"""
+    _fields_ = [("count", ctypes.c_int64), ("chunks", ctypes.c_int64), ("table_bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t)]
 
 
 _lib = None
@@ -120,6 +131,18 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.fp8_gemm_gated.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Gated), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.fp8_gemm_gated_backward.restype = i32
     lib.fp8_gemm_gated_backward.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Gated), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fp8_epilogue_backward_workspace_bytes.restype = sz
+    lib.fp8_epilogue_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.fp8_epilogue_backward.restype = i32
+    lib.fp8_epilogue_backward.argtypes = [i64, i64, i32, vp, i32, i64, vp, i32, i64, i32, i32, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.fp8_clip_plan_size.restype = i32
+    lib.fp8_clip_plan_size.argtypes = [ctypes.POINTER(ClipItem), i64, ctypes.POINTER(ClipSizes)]
+    lib.fp8_clip_plan_fill.restype = i32
+    lib.fp8_clip_plan_fill.argtypes = [ctypes.POINTER(ClipItem), ctypes.POINTER(ClipSizes), vp]
+    lib.fp8_grad_norm.restype = i32
+    lib.fp8_grad_norm.argtypes = [ctypes.POINTER(ClipSizes), vp, vp, vp, vp]
+    lib.fp8_grad_clip.restype = i32
+    lib.fp8_grad_clip.argtypes = [ctypes.POINTER(ClipSizes), vp, vp, ctypes.c_float, vp, vp]
     lib.fp8_async_status.restype = i32
     lib.fp8_async_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     lib.fp8_self_test_expire_wait.restype = i32
@@ -490,6 +513,79 @@ def fp8_gemm_gated_backward(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, 
                                           _scalar(scale_inv_a, "scale_inv_a"), _scalar(scale_inv_b, "scale_inv_b"), scale_d_ptr,
                                           None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()),
            "fp8_gemm_gated_backward")
+
+
+_backward_workspaces: dict = {}
+
+
+def epilogue_backward_workspace(device: torch.device, M: int, N: int) -> torch.Tensor:
+    """A workspace for fp8_epilogue_backward on `device`, kept per (device, stream) and grown as needed."""
+    key = (device.index if device.index is not None else torch.cuda.current_device(), _stream())
+    need = int(load().fp8_epilogue_backward_workspace_bytes(M, N))
+    ws = _backward_workspaces.get(key)
+    if ws is None or ws.numel() < need:
+        ws = torch.zeros(need, dtype=torch.uint8, device=device)
+        _backward_workspaces[key] = ws
+    return ws
+
+
+def fp8_epilogue_backward(dy: torch.Tensor, pre: torch.Tensor | None, out: torch.Tensor, act: int = ACT_NONE, fd: int | None = None,
+                          scale_d: torch.Tensor | None = None, dbias: torch.Tensor | None = None, amax_out: torch.Tensor | None = None,
+                          overflow: int = SATURATE, workspace: torch.Tensor | None = None) -> None:
+    """out = dy * act'(pre), wide or as codes of format ``fd`` made with ``scale_d``; ``dbias`` (float32, one element per
+    column) receives its column sums.  ``pre`` is what fp8_gemm_epilogue kept (None goes with ACT_NONE)."""
+    if dy.dim() != 2 or out.dim() != 2:
+        raise ValueError("dy and out must be 2-D tensors")
+    M, N = dy.shape
+    dy_t = _wide2d(dy, (M, N), "dy")
+    if tuple(out.shape) != (M, N) or not out.is_cuda or out.stride(1) != 1:
+        raise ValueError("out must be a CUDA tensor of the shape of dy with unit inner stride")
+    store, scale_ptr = _store_of(out, fd, scale_d)
+    pre_t, pre_ptr, ldp = (BF16, None, N) if pre is None else (_wide2d(pre, (M, N), "pre"), pre.data_ptr(), pre.stride(0))
+    ws_ptr, ws_bytes, dbias_ptr = None, 0, None
+    if dbias is not None:
+        dbias_ptr = _vec(dbias, N, "dbias")
+        ws = epilogue_backward_workspace(dy.device, M, N) if workspace is None else workspace
+        ws_ptr, ws_bytes = _dev(ws, "workspace"), ws.numel() * ws.element_size()
+    _check(load().fp8_epilogue_backward(M, N, act, dy.data_ptr(), dy_t, dy.stride(0), pre_ptr, pre_t, ldp, store, overflow, scale_ptr,
+                                        out.data_ptr(), out.stride(0), dbias_ptr,
+                                        None if amax_out is None else _scalar(amax_out, "amax_out"), ws_ptr, ws_bytes, _stream()),
+           "fp8_epilogue_backward")
+
+
+class ClipPlan:
+    """The tensors that fp8_grad_norm and fp8_grad_clip go over, laid out once: their table and workspace on the device.
+    ``outs`` (same sizes, float32 or bfloat16 each) receive the clipped gradients; None clips in place.  The plan keeps its
+    tensors alive; calls that may overlap on the GPU need plans of their own."""
+
+    def __init__(self, grads: list[torch.Tensor], outs: list[torch.Tensor] | None = None):
+        self.grads, self.outs = list(grads), list(grads if outs is None else outs)
+        if len(self.grads) != len(self.outs):
+            raise ValueError("grads and outs must have one length")
+        items = (ClipItem * max(1, len(self.grads)))()
+        for it, x, o in zip(items, self.grads, self.outs):
+            if x.numel() != o.numel() or x.device != o.device or x.device != self.grads[0].device:
+                raise ValueError("each output must have the size of its gradient, and all tensors one device")
+            it.x, it.x_t, it.n = _dev(x, "gradient"), _wide_of(x), x.numel()
+            it.out, it.out_t = _dev(o, "output"), _wide_of(o)
+        self.sizes = ClipSizes()
+        _check(load().fp8_clip_plan_size(items, len(self.grads), ctypes.byref(self.sizes)), "fp8_clip_plan_size")
+        device = self.grads[0].device if self.grads else torch.device("cuda", torch.cuda.current_device())
+        host = torch.zeros(max(16, self.sizes.table_bytes), dtype=torch.uint8)
+        _check(load().fp8_clip_plan_fill(items, ctypes.byref(self.sizes), host.data_ptr()), "fp8_clip_plan_fill")
+        self.table = host.to(device)
+        self.workspace = torch.zeros(self.sizes.workspace_bytes, dtype=torch.uint8, device=device)
+        self._call = (ctypes.byref(self.sizes), self.table.data_ptr(), self.workspace.data_ptr())
+
+
+def fp8_grad_norm(plan: ClipPlan, norm_out: torch.Tensor) -> None:
+    """Global 2-norm of the plan's gradients."""
+    _check(load().fp8_grad_norm(*plan._call, _scalar(norm_out, "norm_out"), _stream()), "fp8_grad_norm")
+
+
+def fp8_grad_clip(plan: ClipPlan, max_norm: float, norm_out: torch.Tensor) -> None:
+    """Global 2-norm of the plan's gradients, and outs = grads * min(1, max_norm / norm)."""
+    _check(load().fp8_grad_clip(*plan._call, max_norm, _scalar(norm_out, "norm_out"), _stream()), "fp8_grad_clip")
 
 
 TIMEOUT = 7                                   # FP8_ERR_TIMEOUT

@@ -14,6 +14,7 @@
 #include "activation.cuh"
 #include "codec.cuh"
 #include "common.cuh"
+#include "octet.cuh"
 #include "umma.cuh"
 
 namespace fp8b200 {
@@ -498,24 +499,6 @@ __device__ __forceinline__ void box_store8_wide(uint32_t box, bool bf16, int row
     }
 }
 
-// FP8 codes of eight values of which one is special (or, non-saturating, too large): one at a time, kept small.
-__device__ __forceinline__ uint2 encode8_special(const float (&v)[8], float scale_d, bool e4m3, bool nosat) {
-    uint64_t codes = 0;
-#pragma unroll 1
-    for (int i = 7; i >= 0; --i) {
-        float x = v[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) x = i == j ? v[j] : x;
-        const float y = x * scale_d;
-        uint32_t code;
-        if (y != y) code = ((__float_as_uint(x) >> 24) & 0x80u) | 0x7Fu;
-        else if (e4m3) code = nosat ? encode_scalar<kE4M3, true>(y) : encode_scalar<kE4M3, false>(y);
-        else code = nosat ? encode_scalar<kE5M2, true>(y) : encode_scalar<kE5M2, false>(y);
-        codes = codes << 8 | code;
-    }
-    return make_uint2((uint32_t)codes, (uint32_t)(codes >> 32));
-}
-
 // One octet of an output: its magnitudes (NaN once any is NaN), conversion, staging.  Rounding and scaling are monotonic,
 // so the largest magnitude before them decides the amax after rounding and whether a conversion can overflow.
 __device__ __forceinline__ float emit8(const Params& p, uint32_t box, int row, int o, const float (&v)[8], float scale_d) {
@@ -526,19 +509,7 @@ __device__ __forceinline__ float emit8(const Params& p, uint32_t box, int row, i
         box_store8_wide(box, p.store == FP8_STORE_BF16, row, o, v);
         return most;
     }
-    const bool e4m3 = p.store == FP8_STORE_E4M3;
-    const float far = most * fabsf(scale_d);
-    const bool over = e4m3 ? far > Fmt<kE4M3>::nosat_limit : far >= Fmt<kE5M2>::nosat_limit;
-    uint2 w;
-    if (far <= 3.402823466e38f && !(p.nosat && over)) {
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = v[i] * scale_d;
-        w = e4m3 ? make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7]))
-                 : make_uint2(cvt_quad<kE5M2>(y[0], y[1], y[2], y[3]), cvt_quad<kE5M2>(y[4], y[5], y[6], y[7]));
-    } else {
-        w = encode8_special(v, scale_d, e4m3, p.nosat != 0);
-    }
+    const uint2 w = encode8(v, most, scale_d, p.store == FP8_STORE_E4M3, p.nosat != 0);
     const uint32_t at = box + box_offset(32, row, o >> 1) + (uint32_t)(o & 1) * 8;
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w.x), "r"(w.y) : "memory");
     return most;

@@ -1,0 +1,55 @@
+// Eight consecutive values at a time: magnitudes and FP8 conversion, shared by the fused epilogues and the backward pass.
+#pragma once
+
+#include <stdint.h>
+
+#include "codec.cuh"
+
+namespace fp8b200 {
+
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either operand is NaN
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// Largest magnitude, NaN once any value is NaN.
+__device__ __forceinline__ float most8(const float (&v)[8]) {
+    float most = fabsf(v[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) most = max_nan(most, fabsf(v[i]));
+    return most;
+}
+
+// FP8 codes of eight values of which one is special (or, non-saturating, too large): one at a time, kept small.
+__device__ __forceinline__ uint2 encode8_special(const float (&v)[8], float scale_d, bool e4m3, bool nosat) {
+    uint64_t codes = 0;
+#pragma unroll 1
+    for (int i = 7; i >= 0; --i) {
+        float x = v[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) x = i == j ? v[j] : x;
+        const float y = x * scale_d;
+        uint32_t code;
+        if (y != y) code = ((__float_as_uint(x) >> 24) & 0x80u) | 0x7Fu;
+        else if (e4m3) code = nosat ? encode_scalar<kE4M3, true>(y) : encode_scalar<kE4M3, false>(y);
+        else code = nosat ? encode_scalar<kE5M2, true>(y) : encode_scalar<kE5M2, false>(y);
+        codes = codes << 8 | code;
+    }
+    return make_uint2((uint32_t)codes, (uint32_t)(codes >> 32));
+}
+
+// Codes of v * scale_d; `most` is most8(v).  Scaling is monotonic, so the largest magnitude decides for all eight whether
+// the packed hardware convert may be used.
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], float most, float scale_d, bool e4m3, bool nosat) {
+    const float far = most * fabsf(scale_d);
+    const bool over = e4m3 ? far > Fmt<kE4M3>::nosat_limit : far >= Fmt<kE5M2>::nosat_limit;
+    if (!(far <= 3.402823466e38f) || (nosat && over)) return encode8_special(v, scale_d, e4m3, nosat);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = v[i] * scale_d;
+    return e4m3 ? make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7]))
+                : make_uint2(cvt_quad<kE5M2>(y[0], y[1], y[2], y[3]), cvt_quad<kE5M2>(y[4], y[5], y[6], y[7]));
+}
+
+}  // namespace fp8b200
