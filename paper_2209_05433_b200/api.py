@@ -163,15 +163,17 @@ def _check(status: int, what: str) -> None:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """handle of torch's current stream on the current device (the raw form: no Stream object is made per call)"""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _wide_of(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
+    dtype = t.dtype
+    if dtype is torch.bfloat16:
         return BF16
-    raise TypeError("wide tensors must be float32 or bfloat16, got %s" % t.dtype)
+    if dtype is torch.float32:
+        return F32
+    raise TypeError("wide tensors must be float32 or bfloat16, got %s" % dtype)
 
 
 def _dev(t: torch.Tensor, name: str) -> int:
@@ -183,9 +185,11 @@ def _dev(t: torch.Tensor, name: str) -> int:
 
 
 def _scalar(t: torch.Tensor, name: str) -> int:
-    if t.dtype != torch.float32 or t.numel() != 1:
+    if t.dtype is not torch.float32 or t.numel() != 1:
         raise TypeError("%s must be a one-element float32 CUDA tensor" % name)
-    return _dev(t, name)
+    if not t.is_cuda:                       # one element is always contiguous
+        raise ValueError("%s must be a CUDA tensor" % name)
+    return t.data_ptr()
 
 
 def fp8_amax(x: torch.Tensor, amax_out: torch.Tensor) -> None:
@@ -284,16 +288,27 @@ def fp8_gemm(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int, mb: in
 
 def _gemm_desc_2d(A, ma, B, mb, D, fa, fb, acc, codes_out=False):
     """descriptor of a 2-D product from the tensors' shapes and strides; D is a wide tensor, or uint8 codes"""
-    if A.dtype != torch.uint8 or B.dtype != torch.uint8 or A.dim() != 2 or B.dim() != 2 or D.dim() != 2 or (codes_out and D.dtype != torch.uint8):
+    if A.dtype is not torch.uint8 or B.dtype is not torch.uint8 or A.dim() != 2 or B.dim() != 2 or D.dim() != 2 or (codes_out and D.dtype is not torch.uint8):
         raise TypeError("A and B must be 2-D uint8 tensors and D a 2-D %s tensor" % ("uint8" if codes_out else "float32 or bfloat16"))
-    for t, name in ((A, "A"), (B, "B"), (D, "D")):
-        if not t.is_cuda or t.stride(1) != 1:
-            raise ValueError("%s must be a CUDA tensor with unit inner stride" % name)
-    M, K = (A.shape[0], A.shape[1]) if ma == MAJOR_K else (A.shape[1], A.shape[0])
-    Kb, N = (B.shape[1], B.shape[0]) if mb == MAJOR_K else (B.shape[0], B.shape[1])
-    if K != Kb or tuple(D.shape) != (M, N):
+    lda, ia = A.stride()
+    ldb, ib = B.stride()
+    ldd, idd = D.stride()
+    if ia != 1 or ib != 1 or idd != 1 or not (A.is_cuda and B.is_cuda and D.is_cuda):
+        for t, name in ((A, "A"), (B, "B"), (D, "D")):
+            if not t.is_cuda or t.stride(1) != 1:
+                raise ValueError("%s must be a CUDA tensor with unit inner stride" % name)
+    if ma == MAJOR_K:
+        M, K = A.shape
+    else:
+        K, M = A.shape
+    if mb == MAJOR_K:
+        N, Kb = B.shape
+    else:
+        Kb, N = B.shape
+    rows, cols = D.shape
+    if K != Kb or rows != M or cols != N:
         raise ValueError("shape mismatch: A gives M=%d K=%d, B gives K=%d N=%d, D is %s" % (M, K, Kb, N, tuple(D.shape)))
-    return GemmDesc(M, N, K, fa, fb, ma, mb, A.stride(0), B.stride(0), D.stride(0), BF16 if codes_out else _wide_of(D), acc)
+    return GemmDesc(M, N, K, fa, fb, ma, mb, lda, ldb, ldd, BF16 if codes_out else _wide_of(D), acc)
 
 
 def fp8_gemm_splitk_workspace(M: int, N: int, K: int) -> tuple[int, int]:
@@ -416,7 +431,7 @@ def fp8_gemm_batched(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int
 
 def _wide2d(t: torch.Tensor, shape, name: str) -> int:
     """fp8_wide of a 2-D float32 or bfloat16 CUDA tensor of the given shape with unit inner stride"""
-    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must be a 2-D tensor of shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     if not t.is_cuda or t.stride(1) != 1:
         raise ValueError("%s must be a CUDA tensor with unit inner stride" % name)
