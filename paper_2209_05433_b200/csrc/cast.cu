@@ -1250,6 +1250,7 @@ static fp8_status zero_word(void* p, cudaStream_t st) {
     count_launches(1);
     return FP8_OK;
 }
+fp8_status launch_zero_word(uint32_t* p, cudaStream_t st) { return zero_word(p, st); }
 
 template <int WIDE, int FMT, bool NOSAT>
 static fp8_status launch_current(const void* x, size_t n, float fmax, uint8_t* out, float* amax, float* scale, float* scale_inv,

@@ -22,6 +22,10 @@ inline fp8_status launch_status() {
     return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
 }
 
+// Enqueues the one-thread kernel that zeroes a device word, with programmatic stream serialization: the start value of an
+// amax accumulator (a memset node in its place costs the kernel behind it its early launch, 3.5 us on a 16 us kernel).
+fp8_status launch_zero_word(uint32_t* p, cudaStream_t st);
+
 // Launch with programmatic stream serialization: the kernel may be scheduled while its predecessor in the
 // stream is still draining (once every block of the predecessor has signalled or exited).  Such a kernel must
 // execute grid_dependency_wait() before it touches memory an earlier kernel may still be writing.

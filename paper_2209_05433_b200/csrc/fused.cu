@@ -213,6 +213,10 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars.tmem_base;
+    // The next kernel of the stream may be scheduled from here on (this CTA holds its TMEM already); nothing that an
+    // earlier kernel may still be writing is touched above this line.
+    grid_launch_dependents();
+    grid_dependency_wait();
 
     if (warp == 0) {
         // ------------------------------------------------------------ loader
@@ -581,6 +585,8 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = bars.tmem_base;
+    grid_launch_dependents();               // as in the kernel for few rows
+    grid_dependency_wait();
 
     if (warp < TILES_EPI_BASE) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TILES_REGS_FRONT));
@@ -898,13 +904,15 @@ static fp8_status launch_cluster(const void* kernel, dim3 grid, dim3 cluster, in
     cfg.blockDim = dim3((unsigned)threads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster.x;
     attr[0].val.clusterDim.y = cluster.y;
     attr[0].val.clusterDim.z = cluster.z;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
     count_launches(1);
     return launch_status();
@@ -1085,10 +1093,7 @@ static fp8_status check_product(const fp8_gemm_desc* d, const uint8_t* A, const 
 }
 
 static fp8_status zero_amax(float* amax, cudaStream_t st) {
-    if (!amax) return FP8_OK;
-    if (cudaMemsetAsync(amax, 0, 4, st) != cudaSuccess) return FP8_ERR_CUDA;
-    count_launches(1);
-    return FP8_OK;
+    return amax ? launch_zero_word(reinterpret_cast<uint32_t*>(amax), st) : FP8_OK;
 }
 
 static Params common_params(const fp8_gemm_desc* d, int act, int store, int overflow, const float* scale_d, float* amax) {

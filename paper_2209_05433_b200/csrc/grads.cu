@@ -447,8 +447,8 @@ fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const
     }
     cudaStream_t st = (cudaStream_t)stream;
     if (amax_dev) {
-        if (cudaMemsetAsync(amax_dev, 0, 4, st) != cudaSuccess) return FP8_ERR_CUDA;
-        count_launches(1);
+        const fp8_status rc = launch_zero_word(reinterpret_cast<uint32_t*>(amax_dev), st);
+        if (rc != FP8_OK) return rc;
     }
     if (!some) {
         if (dbias_dev && N > 0) {
