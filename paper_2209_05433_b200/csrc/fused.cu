@@ -148,27 +148,35 @@ constexpr int ROWS_THREADS = 192;                  // loader warp, MMA warp, fou
 constexpr int ROWS_BN = 128;                       // columns of D per tile = the tensor core's M
 constexpr int ROWS_SPLIT_BLOCKS = 4;               // the tensor core's accumulator is drained every 512 of K
 constexpr uint32_t ROWS_TMEM_COLS = 256;           // half of an SM's TMEM: two CTAs share an SM
-constexpr uint32_t ROWS_SMEM = 112 * 1024;
+constexpr uint32_t ROWS_SMEM = 112 * 1024;         // dynamic shared memory of a CTA: two fit an SM
+constexpr int ROWS_MAX_STAGES = 8;
 
 template <int MODE, int T> struct RowsGeo {
     static constexpr int NB = MODE == MODE_GATED ? 2 : 1;                          // weight operands
     static constexpr uint32_t W_BYTES = ROWS_BN * BK;
     static constexpr uint32_t X_BYTES = T * BK;
     static constexpr uint32_t STAGE_BYTES = NB * W_BYTES + X_BYTES;
-    static constexpr int STAGES = (int)((ROWS_SMEM - 2048) / STAGE_BYTES) < 8 ? (int)((ROWS_SMEM - 2048) / STAGE_BYTES) : 8;
     static constexpr int ACCS = ROWS_TMEM_COLS / (T * NB) < 16 ? ROWS_TMEM_COLS / (T * NB) : 16;
-    static constexpr uint32_t EXCHANGE_BYTES = (uint32_t)NB * T * ROWS_BN * 4;
-    static_assert(STAGES >= 2 && ACCS >= 2 && EXCHANGE_BYTES <= STAGES * STAGE_BYTES, "shared memory budget");
+    // partial sums of `rows` tokens that a CTA receives from the slices, and what is left for the ring
+    static constexpr uint32_t exchange_bytes(int rows) { return (uint32_t)(NB * rows * ROWS_BN * 4); }
+    static constexpr int stages(int rows) {
+        const int n = (int)((ROWS_SMEM - 1024 - exchange_bytes(rows)) / STAGE_BYTES);
+        return n < ROWS_MAX_STAGES ? n : ROWS_MAX_STAGES;
+    }
+    static_assert(ACCS >= 2 && (ROWS_SMEM - 1024 - NB * T * ROWS_BN * 4) / STAGE_BYTES >= 2, "TMEM and shared memory budgets");
 };
 
 struct alignas(8) RowsBarriers {
-    uint64_t full[8], empty[8], acc_full[16], acc_empty[16];
+    uint64_t full[ROWS_MAX_STAGES], empty[ROWS_MAX_STAGES], acc_full[16], acc_empty[16];
     uint32_t tmem_base, abort_flag;
 };
 
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
     float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
 
@@ -183,14 +191,14 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 template <int MODE, int T>
 __global__ void __launch_bounds__(ROWS_THREADS, 2)
 k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1,
-             const __grid_constant__ CUtensorMap map_x, const Params p) {
+             const __grid_constant__ CUtensorMap map_x, const Params p, const int stages) {
     using G = RowsGeo<MODE, T>;
-    constexpr int NB = G::NB, STAGES = G::STAGES, ACCS = G::ACCS;
+    constexpr int NB = G::NB, ACCS = G::ACCS;
     extern __shared__ uint8_t smem_raw[];
     __shared__ RowsBarriers bars;
     __shared__ uint32_t red[32];
-    const uint32_t raw = smem_u32(smem_raw);
-    const uint32_t ring = (raw + 1023u) & ~1023u;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t exchange = ring + (uint32_t)stages * G::STAGE_BYTES;
     volatile uint32_t* abort_flag = &bars.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n0 = blockIdx.x * ROWS_BN, t0 = blockIdx.y * T;
@@ -200,10 +208,13 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
     const int kb_n = kb_hi - kb_lo;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
+        for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
         for (int a = 0; a < ACCS; ++a) { mbar_init(smem_u32(&bars.acc_full[a]), 1); mbar_init(smem_u32(&bars.acc_empty[a]), 4); }
         bars.abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&map_w0);
+        if (NB == 2) prefetch_map(&map_w1);
+        prefetch_map(&map_x);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem_base)), "r"(ROWS_TMEM_COLS) : "memory");
@@ -212,20 +223,46 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (slices > 1) cluster_arrive();                       // first phase: every CTA of the cluster runs
     const uint32_t tmem = bars.tmem_base;
     // The next kernel of the stream may be scheduled from here on (this CTA holds its TMEM already); nothing that an
     // earlier kernel may still be writing is touched above this line.
     grid_launch_dependents();
     grid_dependency_wait();
 
+    // The epilogue's items are groups of four columns of a token; each slice of the cluster finishes a contiguous share of
+    // the tile's items.  A thread's items lie THREADS apart, a multiple of 32, so its columns are always the same ones.
+    const int rows = (int)min((int64_t)T, p.M - t0);
+    const int share = rows * (ROWS_BN / 4) / (int)slices;   // 32 items per token, at most 8 slices: always whole
+    const int lo = share * (int)slice;
+    const int quad = (lo + (int)threadIdx.x) & 31;
+    const int64_t n = n0 + quad * 4;
+    const int count = (int)max((int64_t)0, min((int64_t)4, p.N - n));
+    float factor[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f}, alpha1 = 0.0f, scale_d = 1.0f;
+    auto fetch_columns = [&] {
+        const float sa = __ldg(p.sa_inv);
+        if (MODE == MODE_EPILOGUE && p.sb_inv_vec) {
+            load4_any(p.sb_inv_vec, false, n, count, factor);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) factor[i] *= sa;
+        } else {
+            const float f = sa * __ldg(p.sb_inv[0]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) factor[i] = f;
+        }
+        if (MODE == MODE_EPILOGUE && p.bias) load4_any(p.bias, p.bias_bf16 != 0, n, count, bias);
+        if (NB == 2) alpha1 = sa * __ldg(p.sb_inv[1]);
+        if (p.store >= FP8_STORE_E4M3) scale_d = __ldg(p.scale_d);
+    };
+
     if (warp == 0) {
         // ------------------------------------------------------------ loader
         bool ok = true;
-        int issued = 0;
+        int issued = 0, st = 0;
+        uint32_t phase = 1;
         const uint64_t keep = policy_evict_last(), once = policy_evict_first();
         for (int i = 0; i < kb_n; ++i) {
-            const int st = i % STAGES;
-            ok = mbar_wait(smem_u32(&bars.empty[st]), ((uint32_t)(i / STAGES) & 1u) ^ 1u, abort_flag, F_WAIT_EMPTY);
+            ok = mbar_wait(smem_u32(&bars.empty[st]), phase, abort_flag, F_WAIT_EMPTY);
             if (!ok) break;
             if (lane == 0) {
                 const uint32_t sw = ring + (uint32_t)st * G::STAGE_BYTES, full = smem_u32(&bars.full[st]);
@@ -238,25 +275,30 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
             }
             __syncwarp();
             issued = i + 1;
+            if (++st == stages) { st = 0; phase ^= 1u; }
         }
         if (!ok) {                                          // given up: no copy may be in flight when the CTA leaves
-            for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i) {
-                const uint32_t bar = smem_u32(&bars.full[i % STAGES]);
-                for (int spin = 0; spin < (1 << 20) && !mbar_try_wait(bar, (uint32_t)(i / STAGES) & 1u); ++spin) {}
+            for (int i = issued > stages ? issued - stages : 0; i < issued; ++i) {
+                const uint32_t bar = smem_u32(&bars.full[i % stages]);
+                for (int spin = 0; spin < (1 << 20) && !mbar_try_wait(bar, (uint32_t)(i / stages) & 1u); ++spin) {}
             }
         }
+        fetch_columns();
+        if (slices > 1) cluster_wait();
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer
         const uint32_t a_kstep = p.w_mn ? UMMA_K * 128 : UMMA_K, a_lbo = p.w_mn ? BK * 128 : 16;
         bool ok = true;
+        int st = 0;
+        uint32_t phase = 0;
         for (int i = 0; i < kb_n; ++i) {
-            const int st = i % STAGES, chunk = i / ROWS_SPLIT_BLOCKS, acc = chunk % ACCS;
+            const int chunk = i / ROWS_SPLIT_BLOCKS, acc = chunk % ACCS;
             if (i % ROWS_SPLIT_BLOCKS == 0) {
                 ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), ((uint32_t)(chunk / ACCS) & 1u) ^ 1u, abort_flag, F_WAIT_ACC_EMPTY);
                 if (!ok) break;
                 tc_fence_after();
             }
-            ok = mbar_wait(smem_u32(&bars.full[st]), (uint32_t)(i / STAGES) & 1u, abort_flag, F_WAIT_FULL);
+            ok = mbar_wait(smem_u32(&bars.full[st]), phase, abort_flag, F_WAIT_FULL);
             if (!ok) break;
             tc_fence_after();
             if (lane == 0) {
@@ -271,10 +313,14 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
                 if (i == kb_n - 1 || (i + 1) % ROWS_SPLIT_BLOCKS == 0) tc_commit(smem_u32(&bars.acc_full[acc]));
             }
             __syncwarp();
+            if (++st == stages) { st = 0; phase ^= 1u; }
         }
+        fetch_columns();
+        if (slices > 1) cluster_wait();
     } else {
         // ------------------------------------------------------------ accumulators: lane = column of D, TMEM column = token
         const int q = warp & 3;
+        fetch_columns();
         float part[NB * T];
 #pragma unroll
         for (int i = 0; i < NB * T; ++i) part[i] = 0.0f;
@@ -298,81 +344,82 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.acc_empty[acc]));
         }
-        // the last accumulator is complete, so every staged tile has been consumed: the ring becomes the exchange buffer
+        // every partial sum goes to the slice that finishes its item: [from slice][operand][item][4]
+        if (slices > 1) cluster_wait();
+        const float inv_share = 1.0f / (float)share;
         if (ok) {
-            const uint32_t mine = ring + (uint32_t)(q * 32 + lane) * 4;
 #pragma unroll
-            for (int i = 0; i < NB * T; ++i)
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + (uint32_t)i * ROWS_BN * 4), "f"(part[i]) : "memory");
+            for (int t = 0; t < T; ++t) {
+                if (t < rows) {
+                    const int item = t * 32 + q * 8 + (lane >> 2);
+                    const int owner = (int)(((float)item + 0.5f) * inv_share);      // item / share: both below 2^11
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const uint32_t at = exchange + (uint32_t)((((int)slice * NB + b) * share + item - owner * share) * 16 + (lane & 3) * 4);
+                        if (slices > 1)
+                            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(at, (uint32_t)owner)), "f"(part[b * T + t]) : "memory");
+                        else
+                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(part[b * T + t]) : "memory");
+                    }
+                }
+            }
+        } else if (lane == 0) {                             // given up: the other slices must not use this one's sums
+            for (uint32_t s = 0; s < slices; ++s)
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cta(smem_u32(&bars.abort_flag), s)), "r"(1u) : "memory");
         }
     }
+    // the first items' inputs, on their way while the slices meet
+    const int first = (int)threadIdx.x;
+    constexpr int NIN = MODE == MODE_GATED_BWD ? 2 : 1;
+    float in[NIN][4];
+    const bool has_in = MODE == MODE_GATED_BWD || (MODE == MODE_EPILOGUE && p.in[0]);
+    if (has_in && first < share && count > 0) {
+        const int64_t at = (t0 + ((lo + first) >> 5)) * p.ld_in + n;
+#pragma unroll
+        for (int i = 0; i < NIN; ++i) load4(p.in[i], p.in_bf16 != 0, at, count, in[i]);
+    }
     tc_fence_before();
-    __syncthreads();
-    if (slices > 1) cluster_sync_all();
+    if (slices > 1) { cluster_arrive(); cluster_wait(); }
+    else __syncthreads();
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(ROWS_TMEM_COLS) : "memory");
 
-    // ---------------------------------------------------------------- epilogue: each slice finishes its share of the tile
+    // ---------------------------------------------------------------- epilogue: nothing below reaches into another CTA
     float top = 0.0f;
-    bool whole = bars.abort_flag == 0u;
-    if (slices > 1) {
-        for (uint32_t s = 0; s < slices; ++s) {
-            uint32_t flag;
-            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(flag) : "r"(map_to_cta(smem_u32(&bars.abort_flag), s)) : "memory");
-            whole = whole && flag == 0u;
-        }
-    }
-    if (whole) {
-        const int rows = (int)min((int64_t)T, p.M - t0);
-        const int items = rows * (ROWS_BN / 4);
-        const int lo = (int)((int64_t)items * slice / slices), hi = (int)((int64_t)items * (slice + 1) / slices);
-        const float sa = __ldg(p.sa_inv);
-        const float scale_d = p.store >= FP8_STORE_E4M3 ? __ldg(p.scale_d) : 1.0f;
-        const float alpha0 = p.sb_inv_vec ? 0.0f : sa * __ldg(p.sb_inv[0]);
-        const float alpha1 = NB == 2 ? sa * __ldg(p.sb_inv[1]) : 0.0f;
-        for (int item = lo + (int)threadIdx.x; item < hi; item += ROWS_THREADS) {
-            const int tr = item >> 5, quad = item & 31;
-            const int64_t t = t0 + tr, n = n0 + quad * 4;
-            const int count = (int)min((int64_t)4, p.N - n);
-            if (count <= 0) continue;
+    if (bars.abort_flag == 0u && count > 0) {
+        for (int j = first; j < share; j += ROWS_THREADS) {
+            const int64_t t = t0 + ((lo + j) >> 5);
             float a[NB][4];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const uint32_t at = ring + (uint32_t)((b * T + tr) * ROWS_BN + quad * 4) * 4;
                 a[b][0] = a[b][1] = a[b][2] = a[b][3] = 0.0f;
                 for (uint32_t s = 0; s < slices; ++s) {
-                    const float4 v = ld_cluster_f4(slices > 1 ? map_to_cta(at, s) : at);
+                    const float4 v = ld_shared_f4(exchange + (uint32_t)((((int)s * NB + b) * share + j) * 16));
                     a[b][0] += v.x; a[b][1] += v.y; a[b][2] += v.z; a[b][3] += v.w;
                 }
             }
+            if (has_in && j != first) {
+#pragma unroll
+                for (int i = 0; i < NIN; ++i) load4(p.in[i], p.in_bf16 != 0, t * p.ld_in + n, count, in[i]);
+            }
             if (MODE == MODE_EPILOGUE) {
-                float z[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (p.bias) load4_any(p.bias, p.bias_bf16 != 0, n, count, bias);
-                if (p.sb_inv_vec) {
-                    float sb[4];
-                    load4_any(p.sb_inv_vec, false, n, count, sb);
+                float z[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = fmaf(a[0][i], sa * sb[i], bias[i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = fmaf(a[0][i], alpha0, bias[i]);
-                }
+                for (int i = 0; i < 4; ++i) z[i] = fmaf(a[0][i], factor[i], bias[i]);
                 if (p.keep[0]) store4_wide(p.keep[0], p.keep_bf16 != 0, t * p.ld_keep + n, count, z);
                 with_activation(p.act, [&](auto tag) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[i] = activate<decltype(tag)::value>(z[i]);
                 });
-                if (p.in[0]) {
-                    float r[4];
-                    load4(p.in[0], p.in_bf16 != 0, t * p.ld_in + n, count, r);
+                if (has_in) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] += r[i];
+                    for (int i = 0; i < 4; ++i) z[i] += in[0][i];
                 }
                 store4(p, p.D[0], t * p.ldd + n, count, z, scale_d, top);
             } else if (MODE == MODE_GATED) {
                 float g[4], u[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { g[i] = a[0][i] * alpha0; u[i] = a[NB - 1][i] * alpha1; }
+                for (int i = 0; i < 4; ++i) { g[i] = a[0][i] * factor[0]; u[i] = a[NB - 1][i] * alpha1; }
                 if (p.keep[0]) {
                     store4_wide(p.keep[0], p.keep_bf16 != 0, t * p.ld_keep + n, count, g);
                     store4_wide(p.keep[1], p.keep_bf16 != 0, t * p.ld_keep + n, count, u);
@@ -383,16 +430,14 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
                 });
                 store4(p, p.D[0], t * p.ldd + n, count, g, scale_d, top);
             } else {
-                float g[4], u[4], dg[4], du[4];
-                load4(p.in[0], p.in_bf16 != 0, t * p.ld_in + n, count, g);
-                load4(p.in[1], p.in_bf16 != 0, t * p.ld_in + n, count, u);
+                float dg[4], du[4];
                 with_activation(p.act, [&](auto tag) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         float value, slope;
-                        activate_with_slope<decltype(tag)::value>(g[i], value, slope);
-                        const float dh = a[0][i] * alpha0;
-                        dg[i] = dh * u[i] * slope;
+                        activate_with_slope<decltype(tag)::value>(in[0][i], value, slope);
+                        const float dh = a[0][i] * factor[0];
+                        dg[i] = dh * in[NIN - 1][i] * slope;
                         du[i] = dh * value;
                     }
                 });
@@ -400,11 +445,8 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
                 store4(p, p.D[1], t * p.ldd + n, count, du, scale_d, top);
             }
         }
-        if (p.amax_bits) block_atomic_max_bits(canonical_nan_bits(__float_as_uint(top)), red, p.amax_bits);
-    } else if (p.amax_bits) {
-        block_atomic_max_bits(0u, red, p.amax_bits);
     }
-    if (slices > 1) cluster_sync_all();                     // no CTA leaves while another still reads its partial sums
+    if (p.amax_bits) block_atomic_max_bits(canonical_nan_bits(__float_as_uint(top)), red, p.amax_bits);
 }
 
 // ---- products with many rows --------------------------------------------------
@@ -540,12 +582,6 @@ __device__ __forceinline__ void copy_box_out(void* base, int size, uint32_t box,
             *to = (uint8_t)w;
         }
     }
-}
-
-__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
 }
 
 template <int MODE, int ACT>
@@ -981,9 +1017,11 @@ static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const ui
     unsigned slices = 1;
     while (slices < 8 && tiles_n * tiles_t * slices * 2 <= 2 * (int64_t)sm_count() && k_blocks >= 8 * (int64_t)slices) slices *= 2;
     const void* k = reinterpret_cast<const void*>(&k_fused_rows<MODE, T>);
-    constexpr uint32_t smem = G::STAGES * G::STAGE_BYTES + 1024;
-    if (!allow_smem(k, smem)) return FP8_ERR_CUDA;
-    void* args[] = {&w0, &w1, &x, &p};
+    const int rows = d->M < T ? (int)d->M : T;
+    int stages = G::stages(rows);
+    const uint32_t smem = (uint32_t)stages * G::STAGE_BYTES + G::exchange_bytes(rows) + 1024;
+    if (!allow_smem(k, ROWS_SMEM)) return FP8_ERR_CUDA;
+    void* args[] = {&w0, &w1, &x, &p, &stages};
     return launch_cluster(k, dim3((unsigned)tiles_n, (unsigned)tiles_t, slices), dim3(1, 1, slices), ROWS_THREADS, smem, st, args);
 }
 
@@ -1063,7 +1101,8 @@ static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8
     }
     if (d->M <= 16) return launch_rows<MODE, 16>(d, A, B0, B1, p, st);
     if (d->M <= 32) return launch_rows<MODE, 32>(d, A, B0, B1, p, st);
-    return launch_rows<MODE, 64>(d, A, B0, B1, p, st);
+    // (the two operands of the gated block leave no room for the sums of 64 rows)
+    return launch_rows<MODE, MODE == MODE_GATED ? 32 : 64>(d, A, B0, B1, p, st);
 }
 
 // ---- validation shared by the three entry points: nothing is enqueued before every check has passed ----------------
