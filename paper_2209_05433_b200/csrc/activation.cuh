@@ -21,13 +21,30 @@ __device__ __forceinline__ float gated_by(float z, float weight) { return weight
 
 constexpr float kGeluTwoC = 1.5957691216057308f;      // 2 sqrt(2/pi)
 constexpr float kGeluCubic = 0.044715f;
-constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrtTwoPi = 0.39894228040143268f;
+
+// Phi(z), the normal distribution function, and density_scaled = exp(-z^2/2).  Rational approximation 7.1.26 of Abramowitz
+// and Stegun, Handbook of Mathematical Functions (absolute error of erf below 1.5e-7, half of that for Phi):
+//   erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) exp(-x^2),  t = 1 / (1 + 0.3275911 x),  x = |z| / sqrt 2.
+// No branches, one exponential that the derivative uses too (the library's erff takes two paths of a dozen terms).
+__device__ __forceinline__ float normal_cdf(float z, float& density_scaled) {
+    const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
+    density_scaled = __expf(-0.5f * z * z);
+    float q = fmaf(1.061405429f, t, -1.453152027f);
+    q = fmaf(q, t, 1.421413741f);
+    q = fmaf(q, t, -0.284496736f);
+    q = fmaf(q, t, 0.254829592f);
+    const float tail = 0.5f * q * t * density_scaled;             // Phi(-|z|)
+    return z < 0.0f ? tail : 1.0f - tail;                         // NaN: tail is NaN
+}
 
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
     if (ACT == FP8_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == FP8_ACT_GELU) return gated_by(z, fmaf(0.5f, erff(z * kSqrtHalf), 0.5f));
+    if (ACT == FP8_ACT_GELU) {
+        float e;
+        return gated_by(z, normal_cdf(z, e));
+    }
     if (ACT == FP8_ACT_GELU_TANH) return gated_by(z, logistic(kGeluTwoC * z * fmaf(kGeluCubic * z, z, 1.0f)));
     if (ACT == FP8_ACT_SILU) return gated_by(z, logistic(z));
     return z;
@@ -41,10 +58,11 @@ __device__ __forceinline__ void activate_with_slope(float z, float& value, float
         value = z < 0.0f ? 0.0f : z;
         slope = z > 0.0f ? 1.0f : 0.0f;
     } else if (ACT == FP8_ACT_GELU) {
-        const float c = fminf(fmaxf(z, -16.0f), 16.0f);
-        const float w = fmaf(0.5f, erff(z * kSqrtHalf), 0.5f);
+        const float c = fminf(fmaxf(z, -16.0f), 16.0f);           // the density has long vanished there
+        float e;
+        const float w = normal_cdf(z, e);
         value = gated_by(z, w);
-        slope = fmaf(c * kInvSqrtTwoPi, __expf(-0.5f * c * c), w);
+        slope = fmaf(c * kInvSqrtTwoPi, e, w);
     } else if (ACT == FP8_ACT_GELU_TANH) {
         const float c = fminf(fmaxf(z, -16.0f), 16.0f);
         const float w = logistic(kGeluTwoC * z * fmaf(kGeluCubic * z, z, 1.0f));

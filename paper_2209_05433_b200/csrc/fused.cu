@@ -146,7 +146,7 @@ __device__ __forceinline__ void store4(const Params& p, void* base, int64_t at, 
 
 constexpr int ROWS_THREADS = 192;                  // loader warp, MMA warp, four accumulator warps
 constexpr int ROWS_BN = 128;                       // columns of D per tile = the tensor core's M
-constexpr int ROWS_SPLIT_BLOCKS = 4;               // the tensor core's accumulator is drained every 512 of K
+constexpr int ROWS_SPLIT_BLOCKS = 8;               // the tensor core's accumulator is drained every 1024 of K
 constexpr uint32_t ROWS_TMEM_COLS = 256;           // half of an SM's TMEM: two CTAs share an SM
 constexpr uint32_t ROWS_SMEM = 112 * 1024;         // dynamic shared memory of a CTA: two fit an SM
 constexpr int ROWS_MAX_STAGES = 8;
@@ -155,7 +155,10 @@ template <int MODE, int T> struct RowsGeo {
     static constexpr int NB = MODE == MODE_GATED ? 2 : 1;                          // weight operands
     static constexpr uint32_t W_BYTES = ROWS_BN * BK;
     static constexpr uint32_t X_BYTES = T * BK;
-    static constexpr uint32_t STAGE_BYTES = NB * W_BYTES + X_BYTES;
+    // K-blocks per stage: a stage costs the loader and the MMA warp a fixed number of barrier operations, so one holds
+    // two weight tiles of either kind (two K-blocks of one operand, or one of both) where shared memory allows it
+    static constexpr int KB = NB == 2 || T > 32 ? 1 : 2;
+    static constexpr uint32_t STAGE_BYTES = KB * (NB * W_BYTES + X_BYTES);
     static constexpr int ACCS = ROWS_TMEM_COLS / (T * NB) < 16 ? ROWS_TMEM_COLS / (T * NB) : 16;
     // partial sums of `rows` tokens that a CTA receives from the slices, and what is left for the ring
     static constexpr uint32_t exchange_bytes(int rows) { return (uint32_t)(NB * rows * ROWS_BN * 4); }
@@ -173,6 +176,9 @@ struct alignas(8) RowsBarriers {
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
     float4 v;
@@ -225,6 +231,17 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
     tc_fence_after();
     if (slices > 1) cluster_arrive();                       // first phase: every CTA of the cluster runs
     const uint32_t tmem = bars.tmem_base;
+    // The first ring's worth of weights is on its way to L2 while the stream's earlier kernels finish (L2 is where all of
+    // this GPU's writes meet, so a weight that one of them still writes is read as written): 14.7 -> 13.0 us for one token,
+    // 16384 -> 4096; prefetching twice as much or the whole slice gains less.
+    if (threadIdx.x == 0) {
+        const int ahead = min(stages * G::KB, kb_n);
+        for (int i = 0; i < ahead; ++i) {
+            const int k0 = (kb_lo + i) * BK, x = p.w_mn ? n0 : k0, y = p.w_mn ? k0 : n0;
+            tma_prefetch_3d(&map_w0, x, y, 0);
+            if (NB == 2) tma_prefetch_3d(&map_w1, x, y, 0);
+        }
+    }
     // The next kernel of the stream may be scheduled from here on (this CTA holds its TMEM already); nothing that an
     // earlier kernel may still be writing is touched above this line.
     grid_launch_dependents();
@@ -255,66 +272,84 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
         if (p.store >= FP8_STORE_E4M3) scale_d = __ldg(p.scale_d);
     };
 
+    constexpr int KB = G::KB;
+    const int groups = (kb_n + KB - 1) / KB;                // stages' worth of K
     if (warp == 0) {
-        // ------------------------------------------------------------ loader
-        bool ok = true;
-        int issued = 0, st = 0;
-        uint32_t phase = 1;
-        const uint64_t keep = policy_evict_last(), once = policy_evict_first();
-        for (int i = 0; i < kb_n; ++i) {
-            ok = mbar_wait(smem_u32(&bars.empty[st]), phase, abort_flag, F_WAIT_EMPTY);
-            if (!ok) break;
-            if (lane == 0) {
-                const uint32_t sw = ring + (uint32_t)st * G::STAGE_BYTES, full = smem_u32(&bars.full[st]);
-                const int k0 = (kb_lo + i) * BK;
-                // the weights are read once (by this tile alone when one tile holds all tokens); the tokens by every tile
-                mbar_arrive_expect_tx(full, G::STAGE_BYTES);
-                tma_load_3d(sw, &map_w0, p.w_mn ? n0 : k0, p.w_mn ? k0 : n0, 0, full, gridDim.y == 1 ? once : keep);
-                if (NB == 2) tma_load_3d(sw + G::W_BYTES, &map_w1, p.w_mn ? n0 : k0, p.w_mn ? k0 : n0, 0, full, gridDim.y == 1 ? once : keep);
-                tma_load_3d(sw + NB * G::W_BYTES, &map_x, k0, t0, 0, full, keep);
+        // ------------------------------------------------------------ loader (one lane)
+        if (lane == 0) {
+            bool ok = true;
+            int st = 0, issued = 0;
+            uint32_t phase = 1;
+            const uint64_t keep = policy_evict_last(), weights = gridDim.y == 1 ? policy_evict_first() : keep;
+            // the weights are read once (by this tile alone when one tile holds all tokens); the tokens by every tile
+            for (int g = 0; g < groups; ++g) {
+                ok = mbar_wait(smem_u32(&bars.empty[st]), phase, abort_flag, F_WAIT_EMPTY);
+                if (!ok) break;
+                const uint32_t sw = ring + (uint32_t)st * G::STAGE_BYTES, sx = sw + KB * NB * G::W_BYTES, full = smem_u32(&bars.full[st]);
+                const int blocks = min(KB, kb_n - g * KB);
+                mbar_arrive_expect_tx(full, (uint32_t)blocks * (NB * G::W_BYTES + G::X_BYTES));
+#pragma unroll
+                for (int h = 0; h < KB; ++h) {
+                    if (h < blocks) {
+                        const int k0 = (kb_lo + g * KB + h) * BK, x = p.w_mn ? n0 : k0, y = p.w_mn ? k0 : n0;
+                        tma_load_3d(sw + h * NB * G::W_BYTES, &map_w0, x, y, 0, full, weights);
+                        if (NB == 2) tma_load_3d(sw + G::W_BYTES, &map_w1, x, y, 0, full, weights);
+                        tma_load_3d(sx + h * G::X_BYTES, &map_x, k0, t0, 0, full, keep);
+                    }
+                }
+                issued = g + 1;
+                if (++st == stages) { st = 0; phase ^= 1u; }
             }
-            __syncwarp();
-            issued = i + 1;
-            if (++st == stages) { st = 0; phase ^= 1u; }
-        }
-        if (!ok) {                                          // given up: no copy may be in flight when the CTA leaves
-            for (int i = issued > stages ? issued - stages : 0; i < issued; ++i) {
-                const uint32_t bar = smem_u32(&bars.full[i % stages]);
-                for (int spin = 0; spin < (1 << 20) && !mbar_try_wait(bar, (uint32_t)(i / stages) & 1u); ++spin) {}
+            if (!ok) {                                      // given up: no copy may be in flight when the CTA leaves
+                for (int g = issued > stages ? issued - stages : 0; g < issued; ++g) {
+                    const uint32_t bar = smem_u32(&bars.full[g % stages]);
+                    for (int spin = 0; spin < (1 << 20) && !mbar_try_wait(bar, (uint32_t)(g / stages) & 1u); ++spin) {}
+                }
             }
         }
+        __syncwarp();
         fetch_columns();
         if (slices > 1) cluster_wait();
     } else if (warp == 1) {
-        // ------------------------------------------------------------ MMA issuer
-        const uint32_t a_kstep = p.w_mn ? UMMA_K * 128 : UMMA_K, a_lbo = p.w_mn ? BK * 128 : 16;
-        bool ok = true;
-        int st = 0;
-        uint32_t phase = 0;
-        for (int i = 0; i < kb_n; ++i) {
-            const int chunk = i / ROWS_SPLIT_BLOCKS, acc = chunk % ACCS;
-            if (i % ROWS_SPLIT_BLOCKS == 0) {
-                ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), ((uint32_t)(chunk / ACCS) & 1u) ^ 1u, abort_flag, F_WAIT_ACC_EMPTY);
+        // ------------------------------------------------------------ MMA issuer (one lane)
+        if (lane == 0) {
+            const uint32_t a_kstep = (p.w_mn ? UMMA_K * 128 : UMMA_K) >> 4;                  // in descriptor units of 16 bytes
+            const uint64_t dw0 = smem_desc(ring, p.w_mn ? BK * 128 : 16, 1024), dx0 = smem_desc(ring + KB * NB * G::W_BYTES, 16, 1024);
+            bool ok = true;
+            int st = 0, acc = 0, in_chunk = 0;
+            uint32_t phase = 0, acc_phase = 1;
+            for (int g = 0; g < groups; ++g) {
+                if (in_chunk == 0) {
+                    ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), acc_phase, abort_flag, F_WAIT_ACC_EMPTY);
+                    if (!ok) break;
+                }
+                ok = mbar_wait(smem_u32(&bars.full[st]), phase, abort_flag, F_WAIT_FULL);
                 if (!ok) break;
                 tc_fence_after();
-            }
-            ok = mbar_wait(smem_u32(&bars.full[st]), phase, abort_flag, F_WAIT_FULL);
-            if (!ok) break;
-            tc_fence_after();
-            if (lane == 0) {
-                const uint32_t sw = ring + (uint32_t)st * G::STAGE_BYTES, sx = sw + NB * G::W_BYTES;
+                const uint32_t at = (uint32_t)st * (G::STAGE_BYTES >> 4);
+                const int blocks = min(KB, kb_n - g * KB);
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                for (int h = 0; h < KB; ++h) {
+                    if (h < blocks) {
 #pragma unroll
-                    for (int k = 0; k < BK / UMMA_K; ++k)
-                        tc_mma_f8(tmem + (uint32_t)((acc * NB + b) * T), smem_desc(sw + b * G::W_BYTES + k * a_kstep, a_lbo, 1024),
-                                  smem_desc(sx + k * UMMA_K, 16, 1024), p.idesc, ((i % ROWS_SPLIT_BLOCKS) | k) != 0 ? 1u : 0u);
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int k = 0; k < BK / UMMA_K; ++k)
+                                tc_mma_f8(tmem + (uint32_t)((acc * NB + b) * T), dw0 + (at + (h * NB + b) * (G::W_BYTES >> 4) + k * a_kstep),
+                                          dx0 + (at + h * (G::X_BYTES >> 4) + k * (UMMA_K >> 4)), p.idesc, (in_chunk | h | k) != 0 ? 1u : 0u);
+                    }
+                }
                 tc_commit(smem_u32(&bars.empty[st]));
-                if (i == kb_n - 1 || (i + 1) % ROWS_SPLIT_BLOCKS == 0) tc_commit(smem_u32(&bars.acc_full[acc]));
+                in_chunk += KB;
+                if (in_chunk == ROWS_SPLIT_BLOCKS || g == groups - 1) {
+                    tc_commit(smem_u32(&bars.acc_full[acc]));
+                    in_chunk = 0;
+                    if (++acc == ACCS) { acc = 0; acc_phase ^= 1u; }
+                }
+                if (++st == stages) { st = 0; phase ^= 1u; }
             }
-            __syncwarp();
-            if (++st == stages) { st = 0; phase ^= 1u; }
         }
+        __syncwarp();
         fetch_columns();
         if (slices > 1) cluster_wait();
     } else {
@@ -1101,6 +1136,7 @@ static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8
     }
     if (d->M <= 16) return launch_rows<MODE, 16>(d, A, B0, B1, p, st);
     if (d->M <= 32) return launch_rows<MODE, 32>(d, A, B0, B1, p, st);
+    if (MODE != MODE_GATED && d->M <= 48) return launch_rows<MODE, MODE == MODE_GATED ? 32 : 48>(d, A, B0, B1, p, st);
     // (the two operands of the gated block leave no room for the sums of 64 rows)
     return launch_rows<MODE, MODE == MODE_GATED ? 32 : 64>(d, A, B0, B1, p, st);
 }
