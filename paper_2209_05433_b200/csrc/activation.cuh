@@ -13,69 +13,85 @@
 
 namespace fp8b200 {
 
-// 1 / (1 + exp(-x)): exp overflows to infinity below -88, where the quotient is 0 and so is the limit.
-__device__ __forceinline__ float logistic(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
+// 2^x and 1/x by the hardware's approximations (2 and 1 ulp).  Results below the normal range become 0, which is what the
+// callers want of a vanishing weight; the library forms that keep subnormals cost four more instructions each.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
-// z times a weight that vanishes towards -inf
-__device__ __forceinline__ float gated_by(float z, float weight) { return weight == 0.0f ? 0.0f : z * weight; }
+// 1 / (1 + 2^y); 2^y overflows to infinity, where the quotient is 0 and so is the limit.
+__device__ __forceinline__ float logistic2(float y) { return reciprocal_fast(1.0f + exp2_fast(y)); }
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGeluTwoC = 1.5957691216057308f;      // 2 sqrt(2/pi)
 constexpr float kGeluCubic = 0.044715f;
 constexpr float kInvSqrtTwoPi = 0.39894228040143268f;
 
-// Phi(z), the normal distribution function, and density_scaled = exp(-z^2/2).  Rational approximation 7.1.26 of Abramowitz
-// and Stegun, Handbook of Mathematical Functions (absolute error of erf below 1.5e-7, half of that for Phi):
+// Phi(z), the normal distribution function, and bell = exp(-z^2/2).  Rational approximation 7.1.26 of Abramowitz and
+// Stegun, Handbook of Mathematical Functions (absolute error of erf below 1.5e-7, half of that for Phi):
 //   erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) exp(-x^2),  t = 1 / (1 + 0.3275911 x),  x = |z| / sqrt 2.
 // No branches, one exponential that the derivative uses too (the library's erff takes two paths of a dozen terms).
-__device__ __forceinline__ float normal_cdf(float z, float& density_scaled) {
-    const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
-    density_scaled = __expf(-0.5f * z * z);
-    float q = fmaf(1.061405429f, t, -1.453152027f);
-    q = fmaf(q, t, 1.421413741f);
-    q = fmaf(q, t, -0.284496736f);
-    q = fmaf(q, t, 0.254829592f);
-    const float tail = 0.5f * q * t * density_scaled;             // Phi(-|z|)
+__device__ __forceinline__ float normal_cdf(float z, float& bell) {
+    const float t = reciprocal_fast(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
+    bell = exp2_fast(-0.5f * kLog2e * z * z);
+    float q = fmaf(0.5f * 1.061405429f, t, -0.5f * 1.453152027f);
+    q = fmaf(q, t, 0.5f * 1.421413741f);
+    q = fmaf(q, t, -0.5f * 0.284496736f);
+    q = fmaf(q, t, 0.5f * 0.254829592f);
+    const float tail = q * t * bell;                              // Phi(-|z|)
     return z < 0.0f ? tail : 1.0f - tail;                         // NaN: tail is NaN
 }
+
+// Weight of the smooth activations, act(z) = z * weight(z), at any z.  FAR: where the weight has reached 0 (below -FAR)
+// or 1 (above FAR) in binary32, and its derivative 0.
+template <int ACT> struct Far { static constexpr float value = ACT == FP8_ACT_SILU ? 100.0f : 16.0f; };
 
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
     if (ACT == FP8_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == FP8_ACT_GELU) {
-        float e;
-        return gated_by(z, normal_cdf(z, e));
-    }
-    if (ACT == FP8_ACT_GELU_TANH) return gated_by(z, logistic(kGeluTwoC * z * fmaf(kGeluCubic * z, z, 1.0f)));
-    if (ACT == FP8_ACT_SILU) return gated_by(z, logistic(z));
-    return z;
+    if (ACT == FP8_ACT_NONE) return z;
+    float w, bell;
+    if (ACT == FP8_ACT_GELU) w = normal_cdf(z, bell);
+    else if (ACT == FP8_ACT_GELU_TANH) w = logistic2(z * fmaf(-kLog2e * kGeluTwoC * kGeluCubic * z, z, -kLog2e * kGeluTwoC));
+    else w = logistic2(-kLog2e * z);
+    return fmaxf(z, -Far<ACT>::value) * w;                        // -inf: finite times 0; NaN: the weight is NaN
 }
 
-// act(z) and act'(z).  The second term of the derivative is evaluated at z held within +-LIMIT, where it has long
-// vanished, so that it never multiplies an infinity by a zero.
+// act(z) and act'(z) = weight + z * weight'.  The second term is evaluated at z held within +-FAR, where it has vanished,
+// so that it never multiplies an infinity by a zero.
 template <int ACT>
 __device__ __forceinline__ void activate_with_slope(float z, float& value, float& slope) {
     if (ACT == FP8_ACT_RELU) {
         value = z < 0.0f ? 0.0f : z;
         slope = z > 0.0f ? 1.0f : 0.0f;
-    } else if (ACT == FP8_ACT_GELU) {
-        const float c = fminf(fmaxf(z, -16.0f), 16.0f);           // the density has long vanished there
-        float e;
-        const float w = normal_cdf(z, e);
-        value = gated_by(z, w);
-        slope = fmaf(c * kInvSqrtTwoPi, e, w);
-    } else if (ACT == FP8_ACT_GELU_TANH) {
-        const float c = fminf(fmaxf(z, -16.0f), 16.0f);
-        const float w = logistic(kGeluTwoC * z * fmaf(kGeluCubic * z, z, 1.0f));
-        value = gated_by(z, w);
-        slope = fmaf(c * w * (1.0f - w), kGeluTwoC * fmaf(3.0f * kGeluCubic * c, c, 1.0f), w);
-    } else if (ACT == FP8_ACT_SILU) {
-        const float c = fminf(fmaxf(z, -100.0f), 100.0f);
-        const float w = logistic(z);
-        value = gated_by(z, w);
-        slope = fmaf(c * w, 1.0f - w, w);
-    } else {
+        return;
+    }
+    if (ACT == FP8_ACT_NONE) {
         value = z;
         slope = 1.0f;
+        return;
+    }
+    const float above = fmaxf(z, -Far<ACT>::value), c = fminf(above, Far<ACT>::value);
+    if (ACT == FP8_ACT_GELU) {
+        float bell;
+        const float w = normal_cdf(z, bell);
+        value = above * w;
+        slope = fmaf(c * kInvSqrtTwoPi, bell, w);
+    } else if (ACT == FP8_ACT_GELU_TANH) {
+        const float w = logistic2(z * fmaf(-kLog2e * kGeluTwoC * kGeluCubic * z, z, -kLog2e * kGeluTwoC));
+        value = above * w;
+        slope = fmaf(c * w * (1.0f - w), fmaf(3.0f * kGeluTwoC * kGeluCubic * c, c, kGeluTwoC), w);
+    } else {
+        const float w = logistic2(-kLog2e * z);
+        value = above * w;
+        slope = fmaf(c * w, 1.0f - w, w);
     }
 }
 

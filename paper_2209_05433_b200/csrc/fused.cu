@@ -583,9 +583,7 @@ __device__ __forceinline__ void box_store8_wide(uint32_t box, bool bf16, int row
 // One octet of an output: its magnitudes (NaN once any is NaN), conversion, staging.  Rounding and scaling are monotonic,
 // so the largest magnitude before them decides the amax after rounding and whether a conversion can overflow.
 __device__ __forceinline__ float emit8(const Params& p, uint32_t box, int row, int o, const float (&v)[8], float scale_d) {
-    float most = fabsf(v[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) most = fmax_nan(most, fabsf(v[i]));
+    const float most = most8(v);
     if (p.store <= FP8_STORE_BF16) {
         box_store8_wide(box, p.store == FP8_STORE_BF16, row, o, v);
         return most;
@@ -804,6 +802,10 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem + acc * ACC_COLS + ((uint32_t)(q * 32) << 16);
+                if (kc == 0) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) part[i] = 0.0f;
+                }
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2) {
                     uint32_t r[2][32];
@@ -818,8 +820,7 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            float& s = part[(2 * s2 + h) * 32 + i];
-                            s = (kc != 0 ? s : 0.0f) + __uint_as_float(r[h][i]);
+                            part[(2 * s2 + h) * 32 + i] += __uint_as_float(r[h][i]);
                         }
                 }
                 tc_fence_before();

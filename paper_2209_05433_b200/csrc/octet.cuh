@@ -13,12 +13,15 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if eith
     return d;
 }
 
+// max(|a|, |b|, |c|), NaN if any is NaN
+__device__ __forceinline__ float most3(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 // Largest magnitude, NaN once any value is NaN.
 __device__ __forceinline__ float most8(const float (&v)[8]) {
-    float most = fabsf(v[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) most = max_nan(most, fabsf(v[i]));
-    return most;
+    return most3(most3(v[0], v[1], v[2]), most3(v[3], v[4], v[5]), most3(v[6], v[7], 0.0f));
 }
 
 // FP8 codes of eight values of which one is special (or, non-saturating, too large): one at a time, kept small.
