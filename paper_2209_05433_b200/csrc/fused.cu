@@ -498,7 +498,7 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
 constexpr int BM = 128;
 constexpr int TILE_M = 2 * BM;
 constexpr int ACC_COLS = 256;
-constexpr int TILES_STAGES = 4, TILES_FG = 2;                          // ring depth; stages consumed per barrier wait
+constexpr int TILES_MAX_STAGES = 5, TILES_FG = 2;                      // ring depth; K-blocks per barrier wait
 constexpr uint32_t TILES_A_BYTES = BM * BK, TILES_B_BYTES = 128 * BK;
 constexpr uint32_t TILES_STAGE_BYTES = TILES_A_BYTES + TILES_B_BYTES;
 constexpr int TILES_EPI_WARPS = 8, TILES_EPI_BASE = 4;
@@ -507,8 +507,9 @@ constexpr int TILES_REGS_FRONT = 56, TILES_REGS_EPILOGUE = 224;        // 4 x 32
 constexpr int TILES_SPLIT_BLOCKS = 16;                                 // split accumulation: a chunk is 2048 of K
 constexpr int TILES_GROUP_M = 16;
 constexpr int MAX_SLOTS = 4;
-constexpr uint32_t TILES_WARP_BYTES = 12 * 1024;                       // staging of one epilogue warp
-constexpr uint32_t TILES_SMEM = TILES_STAGES * TILES_STAGE_BYTES + TILES_EPI_WARPS * TILES_WARP_BYTES + 1024;
+// Shared memory holds the ring and the epilogue warps' staging: 5 stages leave 8 KB per warp, 4 leave 12.
+constexpr uint32_t TILES_POOL = 224 * 1024, TILES_SMEM = TILES_POOL + 1024;
+constexpr uint32_t tiles_warp_bytes(int stages) { return (TILES_POOL - (uint32_t)stages * TILES_STAGE_BYTES) / TILES_EPI_WARPS; }
 constexpr uint32_t TILES_TMEM_COLS = 512;
 
 // tile index -> (row-tile, column-tile): GROUP_M row-tiles advance together over the columns, sharing panels in L2
@@ -520,7 +521,7 @@ __device__ __forceinline__ void fused_tile_coords(int t, int tiles_m, int tiles_
 }
 
 struct alignas(8) TilesBarriers {
-    uint64_t full[TILES_STAGES], empty[TILES_STAGES], acc_full[2], acc_empty[2];
+    uint64_t full[TILES_MAX_STAGES], empty[TILES_MAX_STAGES], acc_full[2], acc_empty[2];
     uint64_t in[TILES_EPI_WARPS][MAX_SLOTS];
     uint32_t tmem_base, abort_flag;
 };
@@ -528,8 +529,8 @@ struct alignas(8) TilesBarriers {
 // Where the pieces of a staging slot lie: byte offsets of the boxes read and written.
 struct Staging {
     uint32_t in[2], out[2], keep[2];
-    uint32_t slot_bytes;
-    int slots;
+    uint32_t slot_bytes, warp_bytes;
+    int slots, stages;
     uint32_t in_tx;                     // bytes that arrive per slot
 };
 
@@ -571,27 +572,67 @@ __device__ __forceinline__ void box_load8(uint32_t box, bool bf16, int row, int 
     }
 }
 
-__device__ __forceinline__ void box_store8_wide(uint32_t box, bool bf16, int row, int o, const float (&v)[8]) {
+// All 32 columns of this thread's row written to a staged box.  `v` is a run of the thread's registers.
+__device__ __forceinline__ void box_store32_wide(uint32_t box, bool bf16, int row, const float* v) {
     if (bf16) {
-        st_shared_v4(box + box_offset(64, row, o), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            st_shared_v4(box + box_offset(64, row, u), pack_bf16(v[8 * u], v[8 * u + 1]), pack_bf16(v[8 * u + 2], v[8 * u + 3]),
+                         pack_bf16(v[8 * u + 4], v[8 * u + 5]), pack_bf16(v[8 * u + 6], v[8 * u + 7]));
     } else {
-        st_shared_v4(box + box_offset(128, row, 2 * o), __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        st_shared_v4(box + box_offset(128, row, 2 * o + 1), __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            st_shared_v4(box + box_offset(128, row, u), __float_as_uint(v[4 * u]), __float_as_uint(v[4 * u + 1]), __float_as_uint(v[4 * u + 2]), __float_as_uint(v[4 * u + 3]));
     }
 }
 
-// One octet of an output: its magnitudes (NaN once any is NaN), conversion, staging.  Rounding and scaling are monotonic,
-// so the largest magnitude before them decides the amax after rounding and whether a conversion can overflow.
-__device__ __forceinline__ float emit8(const Params& p, uint32_t box, int row, int o, const float (&v)[8], float scale_d) {
-    const float most = most8(v);
-    if (p.store <= FP8_STORE_BF16) {
-        box_store8_wide(box, p.store == FP8_STORE_BF16, row, o, v);
-        return most;
+// 32 columns of an output: conversion and staging; `most` is their largest magnitude.  One decision for all of them, so
+// that the common path is straight-line code.  STORE: FP8_STORE_E4M3, FP8_STORE_E5M2, or a wide type (which one is p.store).
+template <int STORE>
+__device__ __forceinline__ void emit32(const Params& p, uint32_t box, int row, const float* v, float most, float scale_d) {
+    if (STORE <= FP8_STORE_BF16) {
+        box_store32_wide(box, p.store == FP8_STORE_BF16, row, v);
+        return;
     }
-    const uint2 w = encode8(v, most, scale_d, p.store == FP8_STORE_E4M3, p.nosat != 0);
-    const uint32_t at = box + box_offset(32, row, o >> 1) + (uint32_t)(o & 1) * 8;
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(w.x), "r"(w.y) : "memory");
-    return most;
+    constexpr int FMT = STORE == FP8_STORE_E5M2 ? kE5M2 : kE4M3;
+    uint32_t w[8];
+    if (__builtin_expect(converts_packed(most, scale_d, FMT == kE4M3, p.nosat != 0), 1)) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) w[u] = cvt_quad<FMT>(v[4 * u] * scale_d, v[4 * u + 1] * scale_d, v[4 * u + 2] * scale_d, v[4 * u + 3] * scale_d);
+    } else {
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+            const float x[8] = {v[8 * o], v[8 * o + 1], v[8 * o + 2], v[8 * o + 3], v[8 * o + 4], v[8 * o + 5], v[8 * o + 6], v[8 * o + 7]};
+            const uint2 c = encode8_special(x, scale_d, FMT == kE4M3, p.nosat != 0);
+            w[2 * o] = c.x;
+            w[2 * o + 1] = c.y;
+        }
+    }
+    st_shared_v4(box + box_offset(32, row, 0), w[0], w[1], w[2], w[3]);
+    st_shared_v4(box + box_offset(32, row, 1), w[4], w[5], w[6], w[7]);
+}
+
+__device__ __forceinline__ float most32(const float* v) {
+    float m[4];
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {
+        const float x[8] = {v[8 * o], v[8 * o + 1], v[8 * o + 2], v[8 * o + 3], v[8 * o + 4], v[8 * o + 5], v[8 * o + 6], v[8 * o + 7]};
+        m[o] = most8(x);
+    }
+    return most3(most3(m[0], m[1], m[2]), m[3], 0.0f);
+}
+
+// TMEM columns straight into the partial sums (the first chunk of K)
+__device__ __forceinline__ void tc_ld32_sums(uint32_t taddr, float* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+          "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+        : "r"(taddr) : "memory");
 }
 
 // A staged box written to global memory element by element: where it crosses the right edge of rows whose length is not a
@@ -617,7 +658,7 @@ __device__ __forceinline__ void copy_box_out(void* base, int size, uint32_t box,
     }
 }
 
-template <int MODE, int ACT>
+template <int MODE, int ACT, int STORE>
 __global__ void __launch_bounds__(TILES_THREADS, 1)
 k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ TilesParams tp) {
     const Params& p = tp.p;
@@ -635,10 +676,10 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
     const int num_tiles = tp.tiles_m * tp.tiles_n;
     const int k_blocks = (int)((p.K + BK - 1) / BK);
     const int k_pad = (k_blocks + TILES_FG - 1) / TILES_FG * TILES_FG;
-    const int chunk = tp.chunk_blocks;
+    const int chunk = tp.chunk_blocks, stages = tp.s.stages;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < TILES_STAGES; ++s) { mbar_init(smem_u32(&bars.full[s]), TILES_FG * 2); mbar_init(smem_u32(&bars.empty[s]), 1); }
+        for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars.full[s]), TILES_FG * 2); mbar_init(smem_u32(&bars.empty[s]), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars.acc_full[a]), 1); mbar_init(smem_u32(&bars.acc_empty[a]), TILES_EPI_WARPS * 2); }
         for (int w = 0; w < TILES_EPI_WARPS; ++w)
             for (int s = 0; s < MAX_SLOTS; ++s) mbar_init(smem_u32(&bars.in[w][s]), 1);
@@ -660,8 +701,11 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
     if (warp < TILES_EPI_BASE) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TILES_REGS_FRONT));
         if (warp == 0) {
-            // -------------------------------------------------------- loader: each CTA its rows of A and its half of B
-            uint32_t stage = 0, phase = 0;
+            // -------------------------------------------------------- loader: each CTA its rows of A and its half of B.
+            // K-blocks go through the ring of stages one by one; each pair of them completes on one barrier of the leader,
+            // the pairs' barriers going round on their own.
+            int stage = 0, pair = 0;
+            uint32_t phase = 1;
             bool ok = true;
             const uint64_t keep = policy_evict_last();
             const CUtensorMap* map_b = &maps.b[MODE == MODE_GATED ? cta_rank : 0];
@@ -674,12 +718,12 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                 const int n0 = MODE == MODE_GATED ? tn * OUT_COLS : tn * OUT_COLS + (int)cta_rank * 128;
                 const bool backwards = (tile_no++ & 1) != 0;           // K from its end: the wave meets again in L2
                 for (int kb = 0; kb < k_pad; ++kb) {
-                    ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag, F_WAIT_EMPTY);
+                    ok = mbar_wait(smem_u32(&bars.empty[stage]), phase, abort_flag, F_WAIT_EMPTY);
                     if (!ok) break;
                     if (lane == 0) {
-                        const uint32_t sa = ring + stage * TILES_STAGE_BYTES, sb = sa + TILES_A_BYTES;
+                        const uint32_t sa = ring + (uint32_t)stage * TILES_STAGE_BYTES, sb = sa + TILES_A_BYTES;
                         const int k0 = (backwards && kb < k_blocks ? k_blocks - 1 - kb : kb) * BK;
-                        const uint32_t full = map_to_cta(smem_u32(&bars.full[stage / TILES_FG]), 0);
+                        const uint32_t full = map_to_cta(smem_u32(&bars.full[pair]), 0);
                         if (kb < k_blocks) {
                             mbar_arrive_expect_tx_cluster(full, TILES_STAGE_BYTES);
                             tma_load_3d_pair(sa, &maps.a, a_mn ? m0 : k0, a_mn ? k0 : m0, 0, full, keep);
@@ -689,48 +733,51 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                         }
                     }
                     __syncwarp();
-                    if (++stage == TILES_STAGES) { stage = 0; phase ^= 1u; }
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                    if ((kb & 1) != 0 && ++pair == stages) pair = 0;
                 }
             }
             if (!ok)                                                   // given up: a millisecond for copies still in flight (their
                 for (const long long t0 = clock64(); clock64() - t0 < 2000000ll;) {}     // barrier may be in the other CTA)
         } else if (warp == 1) {
             // -------------------------------------------------------- MMA issuer (leader only)
-            uint32_t stage = 0, phase = 0;
+            int stage = 0, pair = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 1;
             bool ok = cta_rank == 0;
-            int it = 0;
             const uint32_t a_kstep = p.a_mn ? UMMA_K * 128 : UMMA_K, a_lbo = p.a_mn ? BK * 128 : 16;
             const uint32_t b_kstep = p.w_mn ? UMMA_K * 128 : UMMA_K, b_lbo = p.w_mn ? BK * 128 : 16;
             for (int t = worker; t < num_tiles && ok; t += num_workers) {
-                for (int kc = 0; kc < k_pad && ok; kc += chunk, ++it) {
-                    const uint32_t acc = (uint32_t)it & 1u;
-                    ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), (((uint32_t)it >> 1) & 1u) ^ 1u, abort_flag, F_WAIT_ACC_EMPTY);
+                for (int kc = 0; kc < k_pad && ok; kc += chunk) {
+                    ok = mbar_wait(smem_u32(&bars.acc_empty[acc]), acc_phase, abort_flag, F_WAIT_ACC_EMPTY);
                     if (!ok) break;
                     tc_fence_after();
                     const int kend = min(k_pad, kc + chunk), last_real = min(k_blocks, kend) - 1;
                     for (int kb = kc; kb < kend; kb += TILES_FG) {
-                        ok = mbar_wait(smem_u32(&bars.full[stage / TILES_FG]), phase, abort_flag, F_WAIT_FULL);
+                        // one wait per two K-blocks: a barrier query between MMA issues costs about one MMA's time
+                        ok = mbar_wait(smem_u32(&bars.full[pair]), phase, abort_flag, F_WAIT_FULL);
                         if (!ok) break;
                         tc_fence_after();
+                        const int stage1 = stage + 1 == stages ? 0 : stage + 1;
                         if (lane == 0) {
 #pragma unroll
                             for (int h = 0; h < TILES_FG; ++h) {
-                                const uint32_t st = stage + h;
+                                const int st = h == 0 ? stage : stage1;
                                 if (kb + h < k_blocks) {
-                                    const uint32_t sa = ring + st * TILES_STAGE_BYTES, sb = sa + TILES_A_BYTES;
+                                    const uint32_t sa = ring + (uint32_t)st * TILES_STAGE_BYTES, sb = sa + TILES_A_BYTES;
 #pragma unroll
                                     for (int k = 0; k < BK / UMMA_K; ++k)
-                                        tc_mma_f8_pair(tmem + acc * ACC_COLS, smem_desc(sa + k * a_kstep, a_lbo, 1024), smem_desc(sb + k * b_kstep, b_lbo, 1024),
-                                                       p.idesc, ((kb - kc) | h | k) != 0 ? 1u : 0u);
+                                        tc_mma_f8_pair(tmem + (uint32_t)acc * ACC_COLS, smem_desc(sa + k * a_kstep, a_lbo, 1024),
+                                                       smem_desc(sb + k * b_kstep, b_lbo, 1024), p.idesc, ((kb - kc) | h | k) != 0 ? 1u : 0u);
                                 }
                                 tc_commit_pair(smem_u32(&bars.empty[st]));
                                 if (kb + h == last_real) tc_commit_pair(smem_u32(&bars.acc_full[acc]));
                             }
                         }
                         __syncwarp();
-                        stage += TILES_FG;
-                        if (stage == TILES_STAGES) { stage = 0; phase ^= 1u; }
+                        stage = stage1 + 1 == stages ? 0 : stage1 + 1;
+                        if (++pair == stages) { pair = 0; phase ^= 1u; }
                     }
+                    if ((acc ^= 1) == 0) acc_phase ^= 1u;
                 }
             }
         }
@@ -742,15 +789,16 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
         const float alpha0 = p.sb_inv_vec ? 0.0f : sa_inv * __ldg(p.sb_inv[0]);
         const float alpha1 = MODE == MODE_GATED ? sa_inv * __ldg(p.sb_inv[1]) : 0.0f;
         const float scale_d = p.store >= FP8_STORE_E4M3 ? __ldg(p.scale_d) : 1.0f;
-        const uint32_t staging = ring + TILES_STAGES * TILES_STAGE_BYTES + (uint32_t)ew * TILES_WARP_BYTES;
+        const uint32_t staging = ring + (uint32_t)stages * TILES_STAGE_BYTES + (uint32_t)ew * tp.s.warp_bytes;
         const uint64_t stream = policy_evict_first();
-        const bool has_in = tp.s.in_tx != 0u;
+        const bool has_in = tp.s.in_tx != 0u, has_columns = p.bias || p.sb_inv_vec;
         const int out_size = p.store == FP8_STORE_F32 ? 4 : p.store == FP8_STORE_BF16 ? 2 : 1;
         const int keep_size = p.keep_bf16 ? 2 : 4, in_size = p.in_bf16 ? 2 : 4;
         const bool clip_out = ((p.N * out_size) & 15) != 0, clip_keep = ((p.N * keep_size) & 15) != 0;
-        const uint32_t columns = staging + TILES_WARP_BYTES - 1024;    // 128 factors, 128 biases of this warp's columns
+        const uint32_t columns = staging + tp.s.warp_bytes - 1024;     // 128 factors, 128 biases of this warp's columns
         uint32_t in_phase = 0;                                         // bit s: parity of slot s
         uint32_t issued = 0;                                           // bit s: a read into slot s has not been waited for
+        const int M = (int)p.M, N = (int)p.N;                          // below 2^31
         float top = 0.0f;
         float part[128];
         bool ok = true;
@@ -758,30 +806,30 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
         const int slots = tp.s.slots;
         int slot = 0;                                                  // of the current step; every step takes the next one
         // lane 0: issue the reads of step `st` of a tile into a slot
-        auto issue = [&](int slot, int st, int64_t row0, int64_t col0) {
+        auto issue = [&](int slot, int st, int row0, int col0) {
             if (lane == 0) {
                 const uint32_t bar = smem_u32(&bars.in[ew][slot]), at = staging + (uint32_t)slot * tp.s.slot_bytes;
-                const int x = (int)((col0 + st * 32) * in_size);
+                const int x = (col0 + st * 32) * in_size;
                 mbar_arrive_expect_tx(bar, tp.s.in_tx);
 #pragma unroll
-                for (int i = 0; i < NIN; ++i) tma_load_3d(at + tp.s.in[i], &maps.in[i], x, (int)row0, 0, bar, stream);
+                for (int i = 0; i < NIN; ++i) tma_load_3d(at + tp.s.in[i], &maps.in[i], x, row0, 0, bar, stream);
             }
             issued |= 1u << slot;
         };
         for (int t = worker; t < num_tiles && ok; t += num_workers) {
             int tm, tn;
             fused_tile_coords(t, tp.tiles_m, tp.tiles_n, tm, tn);
-            const int64_t row0 = (int64_t)tm * TILE_M + (int)cta_rank * BM + q * 32;
-            const int64_t col0 = (int64_t)tn * OUT_COLS + part_no * WARP_COLS;
-            const bool row_ok = row0 + lane < p.M;
+            const int row0 = tm * TILE_M + (int)cta_rank * BM + q * 32;
+            const int col0 = tn * OUT_COLS + part_no * WARP_COLS;
+            const bool row_ok = row0 + lane < M;
             // steps with something inside D
-            const int steps = row0 < p.M && col0 < p.N ? (int)min((int64_t)STEPS, (p.N - col0 + 31) / 32) : 0;
-            if (MODE == MODE_EPILOGUE) {
+            const int steps = row0 < M && col0 < N ? min(STEPS, (N - col0 + 31) / 32) : 0;
+            if (MODE == MODE_EPILOGUE && has_columns) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int64_t c = col0 + i * 32 + lane;
+                    const int c = col0 + i * 32 + lane;
                     float factor = alpha0, bias = 0.0f;
-                    if (c < p.N) {
+                    if (c < N) {
                         if (p.sb_inv_vec) factor = sa_inv * __ldg(p.sb_inv_vec + c);
                         if (p.bias) bias = p.bias_bf16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p.bias) + c) << 16)
                                                        : __ldg(reinterpret_cast<const float*>(p.bias) + c);
@@ -802,39 +850,39 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem + acc * ACC_COLS + ((uint32_t)(q * 32) << 16);
+                // gated: 64 columns of the gate half, then the same 64 of the up half
+                auto column = [&](int j) { return (uint32_t)(MODE == MODE_GATED ? (j >> 1) * 128 + part_no * 64 + (j & 1) * 32 : part_no * 128 + j * 32); };
                 if (kc == 0) {
 #pragma unroll
-                    for (int i = 0; i < 128; ++i) part[i] = 0.0f;
-                }
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    uint32_t r[2][32];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        // gated: 64 columns of the gate half, then the same 64 of the up half
-                        const int c = MODE == MODE_GATED ? s2 * 128 + part_no * 64 + h * 32 : part_no * 128 + (2 * s2 + h) * 32;
-                        tc_ld32(taddr + c, r[h]);
-                    }
+                    for (int j = 0; j < 4; ++j) tc_ld32_sums(taddr + column(j), part + j * 32);
                     tc_wait_ld();
+                } else {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int s2 = 0; s2 < 2; ++s2) {
+                        uint32_t r[2][32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            part[(2 * s2 + h) * 32 + i] += __uint_as_float(r[h][i]);
-                        }
+                        for (int h = 0; h < 2; ++h) tc_ld32(taddr + column(2 * s2 + h), r[h]);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) part[(2 * s2 + h) * 32 + i] += __uint_as_float(r[h][i]);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bars.acc_empty[acc]), 0));
             }
             if (!ok) break;
-            // The loop over steps is rolled (its body alone is hundreds of instructions; unrolled, the epilogue warps wait
-            // for instruction fetches): each round works on the first 32 sums and then moves the others down.
+            // The loop over steps is rolled: its body is hundreds of instructions, and the warps come through it at different
+            // times, so unrolled they wait for instruction fetches more than for anything else.  Each round works on the
+            // first 32 sums and then moves the others down.  What is rarely needed (special values, ragged edges) is kept
+            // out of the loop's straight line.
 #pragma unroll 1
             for (int st = 0; st < steps; ++st) {
                 const uint32_t at = staging + (uint32_t)slot * tp.s.slot_bytes;
-                const int64_t col = col0 + st * 32;
-                const bool ragged = col + 32 > p.N;
+                const int col = col0 + st * 32;
+                const bool ragged = col + 32 > N;
                 if (has_in) {
                     ok = mbar_wait(smem_u32(&bars.in[ew][slot]), (in_phase >> slot) & 1u, abort_flag, F_WAIT_IN);
                     if (!ok) break;
@@ -849,62 +897,76 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                     }
                     __syncwarp();
                 }
-                float most = 0.0f;
+                float* x = part;                                       // this step's sums become its results in place
+                float y[32];
+                if (MODE == MODE_EPILOGUE) {
+                    if (has_columns) {
 #pragma unroll
-                for (int o = 0; o < 4; ++o) {
-                    float x[8], y[8];
-                    if (MODE == MODE_EPILOGUE) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float4 f = ld_shared_f4(columns + (uint32_t)(st * 32 + o * 8 + h * 4) * 4);
-                            const float4 b = ld_shared_f4(columns + 512 + (uint32_t)(st * 32 + o * 8 + h * 4) * 4);
-                            x[h * 4 + 0] = fmaf(part[o * 8 + h * 4 + 0], f.x, b.x);
-                            x[h * 4 + 1] = fmaf(part[o * 8 + h * 4 + 1], f.y, b.y);
-                            x[h * 4 + 2] = fmaf(part[o * 8 + h * 4 + 2], f.z, b.z);
-                            x[h * 4 + 3] = fmaf(part[o * 8 + h * 4 + 3], f.w, b.w);
+                        for (int u = 0; u < 8; ++u) {
+                            const float4 f = ld_shared_f4(columns + (uint32_t)(st * 32 + u * 4) * 4), b = ld_shared_f4(columns + 512 + (uint32_t)(st * 32 + u * 4) * 4);
+                            x[u * 4 + 0] = fmaf(x[u * 4 + 0], f.x, b.x);
+                            x[u * 4 + 1] = fmaf(x[u * 4 + 1], f.y, b.y);
+                            x[u * 4 + 2] = fmaf(x[u * 4 + 2], f.z, b.z);
+                            x[u * 4 + 3] = fmaf(x[u * 4 + 3], f.w, b.w);
                         }
-                        if (p.keep[0]) box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, x);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = activate<ACT>(x[i]);
-                        if (has_in) {
-                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, y);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] += y[i];
-                        }
-                    } else if (MODE == MODE_GATED) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { x[i] = part[o * 8 + i] * alpha0; y[i] = part[64 + o * 8 + i] * alpha1; }
-                        if (p.keep[0]) {
-                            box_store8_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, o, x);
-                            box_store8_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, o, y);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = activate<ACT>(x[i]) * y[i];
                     } else {
-                        box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, x);
-                        box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, y);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[i] *= alpha0;
+                    }
+                    if (p.keep[0]) box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = activate<ACT>(x[i]);
+                    if (has_in) {
+#pragma unroll
+                        for (int o = 0; o < 4; ++o) {
+                            float r[8];
+                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, r);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[o * 8 + i] += r[i];
+                        }
+                    }
+                } else if (MODE == MODE_GATED) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) { x[i] *= alpha0; y[i] = part[64 + i] * alpha1; }
+                    if (p.keep[0]) {
+                        box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
+                        box_store32_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, y);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] = activate<ACT>(x[i]) * y[i];
+                } else {
+#pragma unroll
+                    for (int o = 0; o < 4; ++o) {
+                        float g[8], u[8];
+                        box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, g);
+                        box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, u);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             float value, slope;
-                            activate_with_slope<ACT>(x[i], value, slope);
-                            const float dh = part[o * 8 + i] * alpha0;
-                            x[i] = dh * y[i] * slope;
-                            y[i] = dh * value;
+                            activate_with_slope<ACT>(g[i], value, slope);
+                            const float dh = x[o * 8 + i] * alpha0;
+                            x[o * 8 + i] = dh * u[i] * slope;
+                            y[o * 8 + i] = dh * value;
                         }
                     }
-                    if (ragged) {                                      // columns past N count for nothing
+                }
+                if (__builtin_expect(ragged, 0)) {                     // columns past N count for nothing
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (col + o * 8 + i >= p.N) x[i] = y[i] = 0.0f;
-                    }
-                    most = fmax_nan(most, emit8(p, at + tp.s.out[0], lane, o, x, scale_d));
-                    if (MODE == MODE_GATED_BWD) most = fmax_nan(most, emit8(p, at + tp.s.out[NOUT - 1], lane, o, y, scale_d));
+                    for (int i = 0; i < 32; ++i)
+                        if (col + i >= N) { x[i] = 0.0f; if (MODE == MODE_GATED_BWD) y[i] = 0.0f; }
+                }
+                float most = most32(x);
+                emit32<STORE>(p, at + tp.s.out[0], lane, x, most, scale_d);
+                if (MODE == MODE_GATED_BWD) {
+                    const float most_y = most32(y);
+                    emit32<STORE>(p, at + tp.s.out[NOUT - 1], lane, y, most_y, scale_d);
+                    most = fmax_nan(most, most_y);
                 }
                 if (row_ok) top = fmax_nan(top, most);
                 const bool by_hand = ragged && clip_out, keep_by_hand = ragged && clip_keep;
-                if (ragged) {
-                    const int rows = (int)min((int64_t)32, p.M - row0);
-                    const bool inside = col + lane < p.N;
+                if (__builtin_expect(ragged, 0)) {
+                    const int rows = min(32, M - row0);
+                    const bool inside = col + lane < N;
                     if (by_hand) {
                         copy_box_out(p.D[0], out_size, at + tp.s.out[0], row0, rows, col, p.ldd, lane, inside);
                         if (MODE == MODE_GATED_BWD) copy_box_out(p.D[1], out_size, at + tp.s.out[NOUT - 1], row0, rows, col, p.ldd, lane, inside);
@@ -919,11 +981,11 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                 if (lane == 0) {
                     if (!by_hand) {
 #pragma unroll
-                        for (int i = 0; i < NOUT; ++i) tma_store_3d(&maps.out[i], at + tp.s.out[i], (int)(col * out_size), (int)row0, 0, stream);
+                        for (int i = 0; i < NOUT; ++i) tma_store_3d(&maps.out[i], at + tp.s.out[i], col * out_size, row0, 0, stream);
                     }
                     if (MODE != MODE_GATED_BWD && p.keep[0] && !keep_by_hand) {
 #pragma unroll
-                        for (int i = 0; i < (MODE == MODE_GATED ? 2 : 1); ++i) tma_store_3d(&maps.keep[i], at + tp.s.keep[i], (int)(col * keep_size), (int)row0, 0, stream);
+                        for (int i = 0; i < (MODE == MODE_GATED ? 2 : 1); ++i) tma_store_3d(&maps.keep[i], at + tp.s.keep[i], col * keep_size, row0, 0, stream);
                     }
                     bulk_commit();
                 }
@@ -993,28 +1055,28 @@ static fp8_status launch_cluster(const void* kernel, dim3 grid, dim3 cluster, in
 // A kernel's dynamic shared memory limit is raised once per (kernel, device).
 static bool allow_smem(const void* kernel, uint32_t bytes) {
     static std::mutex mu;
-    static const void* done[64][32] = {};
+    static const void* done[64][64] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
     std::lock_guard<std::mutex> lock(mu);
     int i = 0;
-    while (i < 32 && done[dev][i] && done[dev][i] != kernel) ++i;
-    if (i < 32 && done[dev][i] == kernel) return true;
+    while (i < 64 && done[dev][i] && done[dev][i] != kernel) ++i;
+    if (i < 64 && done[dev][i] == kernel) return true;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) { (void)cudaGetLastError(); return false; }
-    if (i < 32) done[dev][i] = kernel;
+    if (i < 64) done[dev][i] = kernel;
     return true;
 }
 
 // CTA pairs of a tiles kernel that can be resident at once on the current device (looked up once per kernel and device).
 static int pair_workers(const void* kernel) {
     static std::mutex mu;
-    static struct { const void* k; int n; } known[64][16] = {};
+    static struct { const void* k; int n; } known[64][48] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / 2;
     std::lock_guard<std::mutex> lock(mu);
     int i = 0;
-    while (i < 16 && known[dev][i].k && known[dev][i].k != kernel) ++i;
-    if (i < 16 && known[dev][i].k == kernel) return known[dev][i].n;
+    while (i < 48 && known[dev][i].k && known[dev][i].k != kernel) ++i;
+    if (i < 48 && known[dev][i].k == kernel) return known[dev][i].n;
     int n = sm_count() / 2, clusters = 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * n), 1, 1);
@@ -1027,7 +1089,7 @@ static int pair_workers(const void* kernel) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0 && clusters < n) n = clusters;
-    if (i < 16) { known[dev][i].k = kernel; known[dev][i].n = n; }
+    if (i < 48) { known[dev][i].k = kernel; known[dev][i].n = n; }
     return n;
 }
 
@@ -1067,7 +1129,7 @@ static bool make_box_map(CUtensorMap* map, const void* base, const Params& p, in
     return make_map(map, base, (uint64_t)(p.N * size), (uint64_t)p.M, (uint64_t)(ld * size), 1, 0, (uint32_t)(32 * size), 32, swizzle);
 }
 
-template <int MODE, int ACT>
+template <int MODE, int ACT, int STORE>
 static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
     const bool a_mn = d->ma == FP8_MAJOR_MN, w_mn = d->mb == FP8_MAJOR_MN;
     TilesMaps m = {};
@@ -1103,9 +1165,17 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
         }
     }
     if (!ok) return FP8_ERR_CUDA;
+    // Five stages, or four where a warp would then have no slot, or only one although it reads boxes and K is short enough
+    // for the epilogue to matter.  Measured (8192 rows, back to back): gated block with both products kept 985 us at five
+    // stages and one slot, 1013 at four and two; its backward pass at K = 4096 626 and 605; six stages gain nothing.
+    const uint32_t columns = MODE == MODE_EPILOGUE && (p.bias || p.sb_inv_vec) ? 1024 : 0;
+    auto slots_at = [&](int stages) { return (int)((tiles_warp_bytes(stages) - columns) / at); };
+    const int wanted = tp.s.in_tx != 0 && d->K <= 8192 ? 2 : 1;
+    const int stages = slots_at(5) >= wanted ? 5 : 4;
+    tp.s.stages = stages;
     tp.s.slot_bytes = at;
-    const uint32_t room = MODE == MODE_EPILOGUE ? TILES_WARP_BYTES - 1024 : TILES_WARP_BYTES;      // 8 KB + column values, 12 KB, 12 KB at most
-    tp.s.slots = (int)(room / at) < MAX_SLOTS ? (int)(room / at) : MAX_SLOTS;
+    tp.s.warp_bytes = tiles_warp_bytes(stages);
+    tp.s.slots = slots_at(stages) < MAX_SLOTS ? slots_at(stages) : MAX_SLOTS;
     p.a_mn = a_mn ? 1 : 0; p.w_mn = w_mn ? 1 : 0;
     p.idesc = (1u << 4) | ((uint32_t)d->fa << 7) | ((uint32_t)d->fb << 10) | ((a_mn ? 1u : 0u) << 15) | ((w_mn ? 1u : 0u) << 16) |
               ((uint32_t)(ACC_COLS >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
@@ -1116,7 +1186,7 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
     tp.p = p;
     tp.tiles_m = (int)tiles_m; tp.tiles_n = (int)tiles_n;
     tp.chunk_blocks = d->acc == FP8_ACC_SPLIT ? TILES_SPLIT_BLOCKS : k_pad;
-    const void* k = reinterpret_cast<const void*>(&k_fused_tiles<MODE, ACT>);
+    const void* k = reinterpret_cast<const void*>(&k_fused_tiles<MODE, ACT, STORE>);
     if (!allow_smem(k, TILES_SMEM)) return FP8_ERR_CUDA;
     const int workers = pair_workers(k);
     const int64_t use = tiles_m * tiles_n < workers ? tiles_m * tiles_n : workers;
@@ -1124,15 +1194,24 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
     return launch_cluster(k, dim3((unsigned)(2 * use), 1, 1), dim3(2, 1, 1), TILES_THREADS, TILES_SMEM, st, args);
 }
 
+template <int MODE, int ACT>
+static fp8_status dispatch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
+    switch (p.store) {
+        case FP8_STORE_E4M3: return launch_tiles<MODE, ACT, FP8_STORE_E4M3>(d, A, B0, B1, p, st);
+        case FP8_STORE_E5M2: return launch_tiles<MODE, ACT, FP8_STORE_E5M2>(d, A, B0, B1, p, st);
+        default: return launch_tiles<MODE, ACT, FP8_STORE_BF16>(d, A, B0, B1, p, st);
+    }
+}
+
 template <int MODE>
 static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
     if (d->K > 0 && (d->M > 64 || d->ma == FP8_MAJOR_MN)) {
         switch (p.act) {
-            case FP8_ACT_RELU: return launch_tiles<MODE, FP8_ACT_RELU>(d, A, B0, B1, p, st);
-            case FP8_ACT_GELU: return launch_tiles<MODE, FP8_ACT_GELU>(d, A, B0, B1, p, st);
-            case FP8_ACT_GELU_TANH: return launch_tiles<MODE, FP8_ACT_GELU_TANH>(d, A, B0, B1, p, st);
-            case FP8_ACT_SILU: return launch_tiles<MODE, FP8_ACT_SILU>(d, A, B0, B1, p, st);
-            default: return launch_tiles<MODE, FP8_ACT_NONE>(d, A, B0, B1, p, st);
+            case FP8_ACT_RELU: return dispatch_tiles<MODE, FP8_ACT_RELU>(d, A, B0, B1, p, st);
+            case FP8_ACT_GELU: return dispatch_tiles<MODE, FP8_ACT_GELU>(d, A, B0, B1, p, st);
+            case FP8_ACT_GELU_TANH: return dispatch_tiles<MODE, FP8_ACT_GELU_TANH>(d, A, B0, B1, p, st);
+            case FP8_ACT_SILU: return dispatch_tiles<MODE, FP8_ACT_SILU>(d, A, B0, B1, p, st);
+            default: return dispatch_tiles<MODE, FP8_ACT_NONE>(d, A, B0, B1, p, st);
         }
     }
     if (d->M <= 16) return launch_rows<MODE, 16>(d, A, B0, B1, p, st);

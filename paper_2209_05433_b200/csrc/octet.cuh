@@ -42,12 +42,17 @@ __device__ __forceinline__ uint2 encode8_special(const float (&v)[8], float scal
     return make_uint2((uint32_t)codes, (uint32_t)(codes >> 32));
 }
 
-// Codes of v * scale_d; `most` is most8(v).  Scaling is monotonic, so the largest magnitude decides for all eight whether
-// the packed hardware convert may be used.
-__device__ __forceinline__ uint2 encode8(const float (&v)[8], float most, float scale_d, bool e4m3, bool nosat) {
+// Whether the packed hardware convert may be used for values of which `most` is the largest magnitude: all finite and,
+// non-saturating, in range.  Scaling is monotonic, so the largest decides for all.
+__device__ __forceinline__ bool converts_packed(float most, float scale_d, bool e4m3, bool nosat) {
     const float far = most * fabsf(scale_d);
     const bool over = e4m3 ? far > Fmt<kE4M3>::nosat_limit : far >= Fmt<kE5M2>::nosat_limit;
-    if (!(far <= 3.402823466e38f) || (nosat && over)) return encode8_special(v, scale_d, e4m3, nosat);
+    return far <= 3.402823466e38f && !(nosat && over);
+}
+
+// Codes of v * scale_d; `most` is most8(v).
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], float most, float scale_d, bool e4m3, bool nosat) {
+    if (!converts_packed(most, scale_d, e4m3, nosat)) return encode8_special(v, scale_d, e4m3, nosat);
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = v[i] * scale_d;
