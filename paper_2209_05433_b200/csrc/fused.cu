@@ -1205,7 +1205,12 @@ static fp8_status dispatch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const
 
 template <int MODE>
 static fp8_status dispatch(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
-    if (d->K > 0 && (d->M > 64 || d->ma == FP8_MAJOR_MN)) {
+    // The kernel for few rows takes up to 64 rows, and up to 256 where its tiles (128 columns x 64 rows) still fit the SMs in
+    // one go.  Measured against the other, 4096 -> 4096: 100 rows 11.7 and 20.5 us, 256 rows 16.7 and 20.7, 333 rows 23.7 and
+    // 21.0; 16384 -> 4096 at 200 rows 35.5 and 56.4; 4096 -> 16384 at 100 rows, two rounds of tiles, 26.9 and 25.3.
+    const int64_t small_tiles = ((d->N + ROWS_BN - 1) / ROWS_BN) * ((d->M + 63) / 64);
+    const bool few_rows = d->M <= 64 || (MODE != MODE_GATED && d->M <= 256 && small_tiles <= sm_count());
+    if (d->K > 0 && (!few_rows || d->ma == FP8_MAJOR_MN)) {
         switch (p.act) {
             case FP8_ACT_RELU: return dispatch_tiles<MODE, FP8_ACT_RELU>(d, A, B0, B1, p, st);
             case FP8_ACT_GELU: return dispatch_tiles<MODE, FP8_ACT_GELU>(d, A, B0, B1, p, st);
