@@ -26,8 +26,38 @@ __device__ __forceinline__ float reciprocal_fast(float x) {
     return y;
 }
 
+// Two binary32 values in one 64-bit register: the arithmetic below runs on pairs, one instruction for both (mul, add and
+// fma on pairs round each half like their scalar forms).
+struct Pair {
+    unsigned long long v;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit Pair(float both) : Pair(both, both) {}
+    __device__ __forceinline__ void split(float& lo, float& hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+};
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+
 // 1 / (1 + 2^y); 2^y overflows to infinity, where the quotient is 0 and so is the limit.
-__device__ __forceinline__ float logistic2(float y) { return reciprocal_fast(1.0f + exp2_fast(y)); }
+__device__ __forceinline__ Pair logistic2(Pair y) {
+    float a, b;
+    y.split(a, b);
+    (Pair(exp2_fast(a), exp2_fast(b)) + Pair(1.0f)).split(a, b);
+    return Pair(reciprocal_fast(a), reciprocal_fast(b));
+}
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGeluTwoC = 1.5957691216057308f;      // 2 sqrt(2/pi)
@@ -38,60 +68,76 @@ constexpr float kInvSqrtTwoPi = 0.39894228040143268f;
 // Stegun, Handbook of Mathematical Functions (absolute error of erf below 1.5e-7, half of that for Phi):
 //   erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) exp(-x^2),  t = 1 / (1 + 0.3275911 x),  x = |z| / sqrt 2.
 // No branches, one exponential that the derivative uses too (the library's erff takes two paths of a dozen terms).
-__device__ __forceinline__ float normal_cdf(float z, float& bell) {
-    const float t = reciprocal_fast(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
-    bell = exp2_fast(-0.5f * kLog2e * z * z);
-    float q = fmaf(0.5f * 1.061405429f, t, -0.5f * 1.453152027f);
-    q = fmaf(q, t, 0.5f * 1.421413741f);
-    q = fmaf(q, t, -0.5f * 0.284496736f);
-    q = fmaf(q, t, 0.5f * 0.254829592f);
-    const float tail = q * t * bell;                              // Phi(-|z|)
-    return z < 0.0f ? tail : 1.0f - tail;                         // NaN: tail is NaN
+__device__ __forceinline__ Pair normal_cdf(float z0, float z1, Pair& bell) {
+    float a, b;
+    const Pair z(z0, z1);
+    fma2(Pair(fabsf(z0), fabsf(z1)), Pair(0.3275911f * 0.70710678118654752f), Pair(1.0f)).split(a, b);
+    const Pair t(reciprocal_fast(a), reciprocal_fast(b));
+    (z * z * Pair(-0.5f * kLog2e)).split(a, b);
+    bell = Pair(exp2_fast(a), exp2_fast(b));
+    Pair q = fma2(Pair(0.5f * 1.061405429f), t, Pair(-0.5f * 1.453152027f));
+    q = fma2(q, t, Pair(0.5f * 1.421413741f));
+    q = fma2(q, t, Pair(-0.5f * 0.284496736f));
+    q = fma2(q, t, Pair(0.5f * 0.254829592f));
+    const Pair tail = q * t * bell;                               // Phi(-|z|)
+    float t0, t1, u0, u1;
+    tail.split(t0, t1);
+    fma2(tail, Pair(-1.0f), Pair(1.0f)).split(u0, u1);
+    return Pair(z0 < 0.0f ? t0 : u0, z1 < 0.0f ? t1 : u1);        // NaN: tail is NaN
 }
 
-// Weight of the smooth activations, act(z) = z * weight(z), at any z.  FAR: where the weight has reached 0 (below -FAR)
-// or 1 (above FAR) in binary32, and its derivative 0.
+// Where the weight of a smooth activation, act(z) = z * weight(z), has reached 0 (below -FAR) or 1 (above FAR) in binary32,
+// and its derivative 0.
 template <int ACT> struct Far { static constexpr float value = ACT == FP8_ACT_SILU ? 100.0f : 16.0f; };
 
 template <int ACT>
-__device__ __forceinline__ float activate(float z) {
-    if (ACT == FP8_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == FP8_ACT_NONE) return z;
-    float w, bell;
-    if (ACT == FP8_ACT_GELU) w = normal_cdf(z, bell);
-    else if (ACT == FP8_ACT_GELU_TANH) w = logistic2(z * fmaf(-kLog2e * kGeluTwoC * kGeluCubic * z, z, -kLog2e * kGeluTwoC));
-    else w = logistic2(-kLog2e * z);
-    return fmaxf(z, -Far<ACT>::value) * w;                        // -inf: finite times 0; NaN: the weight is NaN
+__device__ __forceinline__ Pair weight(float z0, float z1, Pair& bell) {
+    if (ACT == FP8_ACT_GELU) return normal_cdf(z0, z1, bell);
+    const Pair z(z0, z1);
+    if (ACT == FP8_ACT_GELU_TANH) return logistic2(z * fma2(z * z, Pair(-kLog2e * kGeluTwoC * kGeluCubic), Pair(-kLog2e * kGeluTwoC)));
+    return logistic2(z * Pair(-kLog2e));
 }
 
-// act(z) and act'(z) = weight + z * weight'.  The second term is evaluated at z held within +-FAR, where it has vanished,
-// so that it never multiplies an infinity by a zero.
+// act of two values in place
 template <int ACT>
-__device__ __forceinline__ void activate_with_slope(float z, float& value, float& slope) {
+__device__ __forceinline__ void activate(float& z0, float& z1) {
     if (ACT == FP8_ACT_RELU) {
-        value = z < 0.0f ? 0.0f : z;
-        slope = z > 0.0f ? 1.0f : 0.0f;
+        z0 = z0 < 0.0f ? 0.0f : z0;
+        z1 = z1 < 0.0f ? 0.0f : z1;
+    } else if (ACT != FP8_ACT_NONE) {
+        Pair bell;
+        const Pair w = weight<ACT>(z0, z1, bell);
+        // -inf: finite times 0; NaN: the weight is NaN
+        (Pair(fmaxf(z0, -Far<ACT>::value), fmaxf(z1, -Far<ACT>::value)) * w).split(z0, z1);
+    }
+}
+
+// act(z) and act'(z) = weight + z * weight' of two values.  The second term is evaluated at z held within +-FAR, where it
+// has vanished, so that it never multiplies an infinity by a zero.
+template <int ACT>
+__device__ __forceinline__ void activate_with_slope(float z0, float z1, Pair& value, Pair& slope) {
+    if (ACT == FP8_ACT_RELU) {
+        value = Pair(z0 < 0.0f ? 0.0f : z0, z1 < 0.0f ? 0.0f : z1);
+        slope = Pair(z0 > 0.0f ? 1.0f : 0.0f, z1 > 0.0f ? 1.0f : 0.0f);
         return;
     }
     if (ACT == FP8_ACT_NONE) {
-        value = z;
-        slope = 1.0f;
+        value = Pair(z0, z1);
+        slope = Pair(1.0f);
         return;
     }
-    const float above = fmaxf(z, -Far<ACT>::value), c = fminf(above, Far<ACT>::value);
+    constexpr float FAR = Far<ACT>::value;
+    const float a0 = fmaxf(z0, -FAR), a1 = fmaxf(z1, -FAR);
+    const Pair c(fminf(a0, FAR), fminf(a1, FAR));
+    Pair bell;
+    const Pair w = weight<ACT>(z0, z1, bell);
+    value = Pair(a0, a1) * w;
     if (ACT == FP8_ACT_GELU) {
-        float bell;
-        const float w = normal_cdf(z, bell);
-        value = above * w;
-        slope = fmaf(c * kInvSqrtTwoPi, bell, w);
-    } else if (ACT == FP8_ACT_GELU_TANH) {
-        const float w = logistic2(z * fmaf(-kLog2e * kGeluTwoC * kGeluCubic * z, z, -kLog2e * kGeluTwoC));
-        value = above * w;
-        slope = fmaf(c * w * (1.0f - w), fmaf(3.0f * kGeluTwoC * kGeluCubic * c, c, kGeluTwoC), w);
+        slope = fma2(c * Pair(kInvSqrtTwoPi), bell, w);
     } else {
-        const float w = logistic2(-kLog2e * z);
-        value = above * w;
-        slope = fmaf(c * w, 1.0f - w, w);
+        const Pair bend = c * w * fma2(w, Pair(-1.0f), Pair(1.0f));            // c w (1 - w)
+        if (ACT == FP8_ACT_SILU) slope = bend + w;
+        else slope = fma2(bend, fma2(c * c, Pair(3.0f * kGeluTwoC * kGeluCubic), Pair(kGeluTwoC)), w);
     }
 }
 

@@ -443,8 +443,8 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
                 for (int i = 0; i < 4; ++i) z[i] = fmaf(a[0][i], factor[i], bias[i]);
                 if (p.keep[0]) store4_wide(p.keep[0], p.keep_bf16 != 0, t * p.ld_keep + n, count, z);
                 with_activation(p.act, [&](auto tag) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = activate<decltype(tag)::value>(z[i]);
+                    activate<decltype(tag)::value>(z[0], z[1]);
+                    activate<decltype(tag)::value>(z[2], z[3]);
                 });
                 if (has_in) {
 #pragma unroll
@@ -460,20 +460,22 @@ k_fused_rows(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__
                     store4_wide(p.keep[1], p.keep_bf16 != 0, t * p.ld_keep + n, count, u);
                 }
                 with_activation(p.act, [&](auto tag) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) g[i] = activate<decltype(tag)::value>(g[i]) * u[i];
+                    activate<decltype(tag)::value>(g[0], g[1]);
+                    activate<decltype(tag)::value>(g[2], g[3]);
                 });
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g[i] *= u[i];
                 store4(p, p.D[0], t * p.ldd + n, count, g, scale_d, top);
             } else {
                 float dg[4], du[4];
                 with_activation(p.act, [&](auto tag) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float value, slope;
-                        activate_with_slope<decltype(tag)::value>(in[0][i], value, slope);
-                        const float dh = a[0][i] * factor[0];
-                        dg[i] = dh * in[NIN - 1][i] * slope;
-                        du[i] = dh * value;
+                    for (int i = 0; i < 4; i += 2) {
+                        Pair value, slope;
+                        activate_with_slope<decltype(tag)::value>(in[0][i], in[0][i + 1], value, slope);
+                        const Pair dh = Pair(a[0][i], a[0][i + 1]) * Pair(factor[0]);
+                        (dh * Pair(in[NIN - 1][i], in[NIN - 1][i + 1]) * slope).split(dg[i], dg[i + 1]);
+                        (dh * value).split(du[i], du[i + 1]);
                     }
                 });
                 store4(p, p.D[0], t * p.ldd + n, count, dg, scale_d, top);
@@ -598,7 +600,12 @@ __device__ __forceinline__ void emit32(const Params& p, uint32_t box, int row, c
     uint32_t w[8];
     if (__builtin_expect(converts_packed(most, scale_d, FMT == kE4M3, p.nosat != 0), 1)) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) w[u] = cvt_quad<FMT>(v[4 * u] * scale_d, v[4 * u + 1] * scale_d, v[4 * u + 2] * scale_d, v[4 * u + 3] * scale_d);
+        for (int u = 0; u < 8; ++u) {
+            float y[4];
+            (Pair(v[4 * u], v[4 * u + 1]) * Pair(scale_d)).split(y[0], y[1]);
+            (Pair(v[4 * u + 2], v[4 * u + 3]) * Pair(scale_d)).split(y[2], y[3]);
+            w[u] = cvt_quad<FMT>(y[0], y[1], y[2], y[3]);
+        }
     } else {
 #pragma unroll
         for (int o = 0; o < 4; ++o) {
@@ -866,7 +873,10 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) part[(2 * s2 + h) * 32 + i] += __uint_as_float(r[h][i]);
+                            for (int i = 0; i < 32; i += 2) {
+                                float* s = part + (2 * s2 + h) * 32 + i;
+                                (Pair(s[0], s[1]) + Pair(__uint_as_float(r[h][i]), __uint_as_float(r[h][i + 1]))).split(s[0], s[1]);
+                            }
                     }
                 }
                 tc_fence_before();
@@ -915,7 +925,7 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                     }
                     if (p.keep[0]) box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] = activate<ACT>(x[i]);
+                    for (int i = 0; i < 32; i += 2) activate<ACT>(x[i], x[i + 1]);
                     if (has_in) {
 #pragma unroll
                         for (int o = 0; o < 4; ++o) {
@@ -927,13 +937,19 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                     }
                 } else if (MODE == MODE_GATED) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) { x[i] *= alpha0; y[i] = part[64 + i] * alpha1; }
+                    for (int i = 0; i < 32; i += 2) {
+                        (Pair(x[i], x[i + 1]) * Pair(alpha0)).split(x[i], x[i + 1]);
+                        (Pair(part[64 + i], part[65 + i]) * Pair(alpha1)).split(y[i], y[i + 1]);
+                    }
                     if (p.keep[0]) {
                         box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
                         box_store32_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, y);
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] = activate<ACT>(x[i]) * y[i];
+                    for (int i = 0; i < 32; i += 2) {
+                        activate<ACT>(x[i], x[i + 1]);
+                        (Pair(x[i], x[i + 1]) * Pair(y[i], y[i + 1])).split(x[i], x[i + 1]);
+                    }
                 } else {
 #pragma unroll
                     for (int o = 0; o < 4; ++o) {
@@ -941,12 +957,12 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                         box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, g);
                         box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, u);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float value, slope;
-                            activate_with_slope<ACT>(g[i], value, slope);
-                            const float dh = x[o * 8 + i] * alpha0;
-                            x[o * 8 + i] = dh * u[i] * slope;
-                            y[o * 8 + i] = dh * value;
+                        for (int i = 0; i < 8; i += 2) {
+                            Pair value, slope;
+                            activate_with_slope<ACT>(g[i], g[i + 1], value, slope);
+                            const Pair dh = Pair(x[o * 8 + i], x[o * 8 + i + 1]) * Pair(alpha0);
+                            (dh * Pair(u[i], u[i + 1]) * slope).split(x[o * 8 + i], x[o * 8 + i + 1]);
+                            (dh * value).split(y[o * 8 + i], y[o * 8 + i + 1]);
                         }
                     }
                 }

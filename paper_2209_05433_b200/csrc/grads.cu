@@ -127,16 +127,16 @@ k_epilogue_backward(const BackwardParams p) {
                     float z[8];
                     pre[u].values(z);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float value, slope;
-                        activate_with_slope<ACT>(z[i], value, slope);
-                        v[i] *= slope;
+                    for (int i = 0; i < 8; i += 2) {
+                        Pair value, slope;
+                        activate_with_slope<ACT>(z[i], z[i + 1], value, slope);
+                        (Pair(v[i], v[i + 1]) * slope).split(v[i], v[i + 1]);
                     }
                 }
                 const float most = most8(v);
                 top = max_nan(top, most);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] += v[i];
+                for (int i = 0; i < 8; i += 2) (Pair(acc[i], acc[i + 1]) + Pair(v[i], v[i + 1])).split(acc[i], acc[i + 1]);
                 const int64_t at = r * p.ldo + col;
                 if (p.store >= FP8_STORE_E4M3) {
                     const uint2 w = encode8(v, most, scale, p.store == FP8_STORE_E4M3, p.nosat != 0);

@@ -3,6 +3,7 @@
 
 #include <stdint.h>
 
+#include "activation.cuh"
 #include "codec.cuh"
 
 namespace fp8b200 {
@@ -55,7 +56,7 @@ __device__ __forceinline__ uint2 encode8(const float (&v)[8], float most, float 
     if (!converts_packed(most, scale_d, e4m3, nosat)) return encode8_special(v, scale_d, e4m3, nosat);
     float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = v[i] * scale_d;
+    for (int i = 0; i < 8; i += 2) (Pair(v[i], v[i + 1]) * Pair(scale_d)).split(y[i], y[i + 1]);
     return e4m3 ? make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7]))
                 : make_uint2(cvt_quad<kE5M2>(y[0], y[1], y[2], y[3]), cvt_quad<kE5M2>(y[4], y[5], y[6], y[7]));
 }
