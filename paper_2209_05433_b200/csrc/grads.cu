@@ -303,8 +303,9 @@ __device__ __forceinline__ double block_sum(double v, double* smem) {
 __global__ void __launch_bounds__(THREADS) k_grad_norm(const ClipParams p) {
     __shared__ double red[WARPS];
     __shared__ unsigned int last;
-    grid_dependency_wait();
+    // The table is the plan's own: copied to the device before the first call, written by no kernel.
     const Entry e = p.entries[p.chunk_entry[blockIdx.x]];
+    grid_dependency_wait();
     const int64_t lo = ((int64_t)blockIdx.x - e.first_chunk) * CHUNK, n = min(CHUNK, e.n - lo);
     const double mine = e.x_bf16 ? chunk_squares<true>(reinterpret_cast<const uint16_t*>(e.x) + lo, n, e.aligned != 0)
                                  : chunk_squares<false>(reinterpret_cast<const float*>(e.x) + lo, n, e.aligned != 0);
@@ -327,36 +328,45 @@ __global__ void __launch_bounds__(THREADS) k_grad_norm(const ClipParams p) {
     }
 }
 
+// out = x * coef over one chunk.  The first items are loaded before the norm is waited for: this kernel is scheduled when
+// every block of the norm kernel is past its own wait, so whatever wrote x has finished, and the norm kernel itself writes
+// nothing but the norm and its workspace.
 template <bool X_BF16, bool OUT_BF16>
-__device__ __forceinline__ void clip_chunk(const void* x, void* out, int64_t n, bool aligned, float coef) {
-    int64_t done = 0;
-    if (aligned) {
-        constexpr int BATCH = 4;
-        const int64_t octets = n / 8;
-        for (int64_t i0 = threadIdx.x; i0 < octets; i0 += THREADS * BATCH) {
-            Octet<X_BF16> w[BATCH];
+__device__ __forceinline__ void clip_chunk(const ClipParams& p, const Entry& e, int64_t lo, int64_t n) {
+    constexpr int BATCH = 4;
+    const uint8_t* x = reinterpret_cast<const uint8_t*>(e.x) + lo * (X_BF16 ? 2 : 4);
+    uint8_t* out = reinterpret_cast<uint8_t*>(e.out) + lo * (OUT_BF16 ? 2 : 4);
+    const int64_t octets = e.aligned ? n / 8 : 0;
+    Octet<X_BF16> w[BATCH];
+    auto fetch = [&](int64_t i0) {
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b)
-                if (i0 + b * THREADS < octets) w[b].load(x, (i0 + b * THREADS) * 8);
+        for (int b = 0; b < BATCH; ++b)
+            if (i0 + b * THREADS < octets) w[b].load(x, (i0 + b * THREADS) * 8);
+    };
+    fetch(threadIdx.x);
+    grid_dependency_wait();
+    const float norm = __ldcg(p.norm);
+    const float coef = norm <= p.max_norm ? 1.0f : p.max_norm / norm;
+    if (coef == 1.0f && e.x == e.out) return;              // in place: nothing changes
+    for (int64_t i0 = threadIdx.x; i0 < octets; i0 += THREADS * BATCH) {
+        if (i0 != threadIdx.x) fetch(i0);
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                const int64_t i = i0 + b * THREADS;
-                if (i >= octets) continue;
-                float v[8];
-                w[b].values(v);
+        for (int b = 0; b < BATCH; ++b) {
+            const int64_t i = i0 + b * THREADS;
+            if (i >= octets) continue;
+            float v[8];
+            w[b].values(v);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] *= coef;
-                if (OUT_BF16) {
-                    reinterpret_cast<uint4*>(out)[i] = pack8_bf16(v);
-                } else {
-                    reinterpret_cast<float4*>(out)[2 * i] = make_float4(v[0], v[1], v[2], v[3]);
-                    reinterpret_cast<float4*>(out)[2 * i + 1] = make_float4(v[4], v[5], v[6], v[7]);
-                }
+            for (int j = 0; j < 8; ++j) v[j] *= coef;
+            if (OUT_BF16) {
+                reinterpret_cast<uint4*>(out)[i] = pack8_bf16(v);
+            } else {
+                reinterpret_cast<float4*>(out)[2 * i] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4*>(out)[2 * i + 1] = make_float4(v[4], v[5], v[6], v[7]);
             }
         }
-        done = octets * 8;
     }
-    for (int64_t i = done + threadIdx.x; i < n; i += THREADS) {
+    for (int64_t i = octets * 8 + threadIdx.x; i < n; i += THREADS) {
         const float f = (X_BF16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(x)[i] << 16) : reinterpret_cast<const float*>(x)[i]) * coef;
         if (OUT_BF16) reinterpret_cast<uint16_t*>(out)[i] = (uint16_t)pack_bf16(f, 0.0f);
         else reinterpret_cast<float*>(out)[i] = f;
@@ -366,16 +376,14 @@ __device__ __forceinline__ void clip_chunk(const void* x, void* out, int64_t n, 
 // One block per chunk, from the last to the first: the end of what the norm has just read is still in L2.
 __global__ void __launch_bounds__(THREADS) k_grad_clip(const ClipParams p) {
     const int64_t chunk = p.chunks - 1 - blockIdx.x;
-    grid_dependency_wait();
     const Entry e = p.entries[p.chunk_entry[chunk]];
-    const float norm = __ldcg(p.norm);
-    const float coef = norm <= p.max_norm ? 1.0f : p.max_norm / norm;
-    if (!e.out || (coef == 1.0f && e.x == e.out)) return;  // counted in the norm only; in place nothing changes
     const int64_t lo = (chunk - e.first_chunk) * CHUNK, n = min(CHUNK, e.n - lo);
-    const void* x = reinterpret_cast<const uint8_t*>(e.x) + lo * (e.x_bf16 ? 2 : 4);
-    void* out = reinterpret_cast<uint8_t*>(e.out) + lo * (e.out_bf16 ? 2 : 4);
-    if (e.x_bf16) e.out_bf16 ? clip_chunk<true, true>(x, out, n, e.aligned != 0, coef) : clip_chunk<true, false>(x, out, n, e.aligned != 0, coef);
-    else          e.out_bf16 ? clip_chunk<false, true>(x, out, n, e.aligned != 0, coef) : clip_chunk<false, false>(x, out, n, e.aligned != 0, coef);
+    if (!e.out) {                                          // counted in the norm only
+        grid_dependency_wait();
+        return;
+    }
+    if (e.x_bf16) e.out_bf16 ? clip_chunk<true, true>(p, e, lo, n) : clip_chunk<true, false>(p, e, lo, n);
+    else          e.out_bf16 ? clip_chunk<false, true>(p, e, lo, n) : clip_chunk<false, false>(p, e, lo, n);
 }
 
 static bool wide_ok(int t) { return t == FP8_F32 || t == FP8_BF16; }
