@@ -112,6 +112,25 @@ __device__ __forceinline__ void activate(float& z0, float& z1) {
     }
 }
 
+// act'(z) alone, of values that are within +-FAR or NaN (relu and none: any values).
+template <int ACT>
+__device__ __forceinline__ Pair slope_within(float z0, float z1) {
+    if (ACT == FP8_ACT_NONE) return Pair(1.0f);
+    if (ACT == FP8_ACT_RELU) return Pair(z0 > 0.0f ? 1.0f : 0.0f, z1 > 0.0f ? 1.0f : 0.0f);
+    const Pair z(z0, z1);
+    if (ACT == FP8_ACT_GELU) {
+        Pair bell;
+        const Pair w = normal_cdf(z0, z1, bell);
+        return fma2(z * Pair(kInvSqrtTwoPi), bell, w);
+    }
+    const Pair square = z * z;
+    const Pair w = ACT == FP8_ACT_SILU ? logistic2(z * Pair(-kLog2e))
+                                       : logistic2(z * fma2(square, Pair(-kLog2e * kGeluTwoC * kGeluCubic), Pair(-kLog2e * kGeluTwoC)));
+    const Pair bend = z * w * fma2(w, Pair(-1.0f), Pair(1.0f));               // z w (1 - w)
+    if (ACT == FP8_ACT_SILU) return bend + w;
+    return fma2(bend, fma2(square, Pair(3.0f * kGeluTwoC * kGeluCubic), Pair(kGeluTwoC)), w);
+}
+
 // act(z) and act'(z) = weight + z * weight' of two values.  The second term is evaluated at z held within +-FAR, where it
 // has vanished, so that it never multiplies an infinity by a zero.
 template <int ACT>

@@ -33,21 +33,41 @@ __device__ __forceinline__ void unpack_bf16(const uint4& w, float (&v)[8]) {
 // Raw octet of a wide row: one 16-byte word of bf16, two of fp32.
 template <bool BF16> struct Octet {
     uint4 w[BF16 ? 1 : 2];
-    __device__ __forceinline__ void load(const void* base, int64_t at) {
-        const uint8_t* p = reinterpret_cast<const uint8_t*>(base) + at * (BF16 ? 2 : 4);
+    __device__ __forceinline__ void load(const uint8_t* p) {
         w[0] = ld_stream_v4(p);
         if (!BF16) w[BF16 ? 0 : 1] = ld_stream_v4(p + 16);
     }
-    __device__ __forceinline__ void load_some(const void* base, int64_t at, int count) {
+    __device__ __forceinline__ void load_some(const uint8_t* p, int count) {
         uint32_t e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            e[i] = i >= count ? 0u : BF16 ? (uint32_t) reinterpret_cast<const uint16_t*>(base)[at + i] : reinterpret_cast<const uint32_t*>(base)[at + i];
+            e[i] = i >= count ? 0u : BF16 ? (uint32_t) reinterpret_cast<const uint16_t*>(p)[i] : reinterpret_cast<const uint32_t*>(p)[i];
         if (BF16) {
             w[0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
         } else {
             w[0] = make_uint4(e[0], e[1], e[2], e[3]);
             w[BF16 ? 0 : 1] = make_uint4(e[4], e[5], e[6], e[7]);
+        }
+    }
+    // Every value outside [-far, far] moved to the nearer end; NaN stays NaN.  `far` is a bf16 value.
+    __device__ __forceinline__ void hold_within(float far) {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) {
+            uint32_t e[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (BF16) {                                // both halves of the word at once
+                    const uint32_t hi = (__float_as_uint(far) >> 16) * 0x10001u, lo = hi | 0x80008000u;
+                    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(e[j]) : "r"(lo));
+                    asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(e[j]) : "r"(hi));
+                } else {
+                    float f = __uint_as_float(e[j]);
+                    asm("max.NaN.f32 %0, %0, %1;" : "+f"(f) : "f"(-far));
+                    asm("min.NaN.f32 %0, %0, %1;" : "+f"(f) : "f"(far));
+                    e[j] = __float_as_uint(f);
+                }
+            }
+            w[i] = make_uint4(e[0], e[1], e[2], e[3]);
         }
     }
     __device__ __forceinline__ void values(float (&v)[8]) const {
@@ -68,7 +88,7 @@ __device__ __forceinline__ uint4 pack8_bf16(const float (&v)[8]) {
 // ---- backward pass of the epilogue -------------------------------------------------------------------------------
 
 constexpr int STRIP = 32 * 8;                              // columns of a block: one octet per lane
-constexpr int UNROLL = 2;                                  // rows in flight per warp
+constexpr int UNROLL = 2;                                  // rows in flight per warp in the row loop
 
 struct BackwardParams {
     int64_t M, N, ldy, ldp, ldo;
@@ -86,8 +106,12 @@ struct BackwardParams {
 
 // A block takes a strip of 256 columns and a chunk of rows, a warp every eighth row.  Each thread keeps the sums of its
 // eight columns; the block adds its warps' sums in order and the last block of a strip adds the chunks' in order.
-template <int ACT, bool DY_BF16, bool PRE_BF16>
-__global__ void __launch_bounds__(THREADS)
+// What bounds it: 5 bytes per bf16 element against some fourteen instructions, two of them exp2 and reciprocal.  Addresses
+// advance by pointers, bounds are settled outside the row loop and the stored type is fixed at compile time, because
+// branches and address arithmetic were as many instructions as the mathematics (27 per element in all).
+// STORE: FP8_STORE_E4M3, FP8_STORE_E5M2, or a wide type (which one is p.store).
+template <int ACT, bool DY_BF16, bool PRE_BF16, int STORE>
+__global__ void __launch_bounds__(THREADS, 4)
 k_epilogue_backward(const BackwardParams p) {
     __shared__ float sums[WARPS][STRIP];
     __shared__ uint32_t red[32];
@@ -100,73 +124,85 @@ k_epilogue_backward(const BackwardParams p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
     grid_dependency_wait();
-    const float scale = p.store >= FP8_STORE_E4M3 ? __ldg(p.scale) : 1.0f;
-    if (count > 0) {
-        for (int64_t r0 = row_lo + warp; r0 < row_hi; r0 += WARPS * UNROLL) {
-            Octet<DY_BF16> dy[UNROLL];
-            Octet<PRE_BF16> pre[UNROLL];
+    const float scale = STORE >= FP8_STORE_E4M3 ? __ldg(p.scale) : 1.0f;
+    constexpr int YS = DY_BF16 ? 2 : 4, ZS = PRE_BF16 ? 2 : 4;
+    const int os = STORE >= FP8_STORE_E4M3 ? 1 : p.store == FP8_STORE_BF16 ? 2 : 4;
+    const int64_t first = row_lo + warp;
+    const uint8_t* y = reinterpret_cast<const uint8_t*>(p.dy) + (first * p.ldy + col) * YS;
+    const uint8_t* z = reinterpret_cast<const uint8_t*>(p.pre) + (first * p.ldp + col) * ZS;
+    uint8_t* o = reinterpret_cast<uint8_t*>(p.out) + (first * p.ldo + col) * os;
+    const int64_t y_step = WARPS * p.ldy * YS, z_step = WARPS * p.ldp * ZS, o_step = WARPS * p.ldo * os;
+    int rows = count > 0 && first < row_hi ? (int)((row_hi - first + WARPS - 1) / WARPS) : 0;      // of this warp
+    // dz of one octet: magnitudes, column sums, v
+    auto derive = [&](Octet<DY_BF16>& dy, Octet<PRE_BF16>& pre, float (&v)[8]) {
+        dy.values(v);
+        if (ACT != FP8_ACT_NONE) {
+            float x[8];
+            if (ACT != FP8_ACT_RELU) pre.hold_within(Far<ACT>::value);
+            pre.values(x);
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                const int64_t r = r0 + u * WARPS;
-                if (r >= row_hi) continue;
-                if (count == 8) {
-                    dy[u].load(p.dy, r * p.ldy + col);
-                    if (ACT != FP8_ACT_NONE) pre[u].load(p.pre, r * p.ldp + col);
-                } else {
-                    dy[u].load_some(p.dy, r * p.ldy + col, count);
-                    if (ACT != FP8_ACT_NONE) pre[u].load_some(p.pre, r * p.ldp + col, count);
+            for (int i = 0; i < 8; i += 2) (Pair(v[i], v[i + 1]) * slope_within<ACT>(x[i], x[i + 1])).split(v[i], v[i + 1]);
+        }
+        const float most = most8(v);
+        top = max_nan(top, most);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) (Pair(acc[i], acc[i + 1]) + Pair(v[i], v[i + 1])).split(acc[i], acc[i + 1]);
+        return most;
+    };
+    if (count == 8) {
+        auto work = [&](Octet<DY_BF16>& dy, Octet<PRE_BF16>& pre, uint8_t* to) {
+            float v[8];
+            const float most = derive(dy, pre, v);
+            if (STORE >= FP8_STORE_E4M3) {
+                *reinterpret_cast<uint2*>(to) = encode8_as<STORE == FP8_STORE_E5M2 ? kE5M2 : kE4M3>(v, most, scale, p.nosat != 0);
+            } else if (os == 2) {
+                *reinterpret_cast<uint4*>(to) = pack8_bf16(v);
+            } else {
+                reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        };
+        Octet<DY_BF16> dy[2];
+        Octet<PRE_BF16> pre[2];
+#pragma unroll 1
+        for (; rows >= 2; rows -= 2) {                     // two rows in flight
+            dy[0].load(y);
+            dy[1].load(y + y_step);
+            if (ACT != FP8_ACT_NONE) { pre[0].load(z); pre[1].load(z + z_step); }
+            work(dy[0], pre[0], o);
+            work(dy[1], pre[1], o + o_step);
+            y += 2 * y_step; z += 2 * z_step; o += 2 * o_step;
+        }
+        if (rows > 0) {
+            dy[0].load(y);
+            if (ACT != FP8_ACT_NONE) pre[0].load(z);
+            work(dy[0], pre[0], o);
+        }
+    } else {                                               // the last columns of rows whose length is no multiple of 8
+#pragma unroll 1
+        for (; rows > 0; --rows) {
+            Octet<DY_BF16> dy;
+            Octet<PRE_BF16> pre;
+            dy.load_some(y, count);
+            if (ACT != FP8_ACT_NONE) pre.load_some(z, count);
+            float v[8];
+            const float most = derive(dy, pre, v);
+            uint2 w = make_uint2(0u, 0u);
+            if (STORE >= FP8_STORE_E4M3) w = encode8_as<STORE == FP8_STORE_E5M2 ? kE5M2 : kE4M3>(v, most, scale, p.nosat != 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i < count) {
+                    if (STORE >= FP8_STORE_E4M3) o[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+                    else if (os == 2) reinterpret_cast<uint16_t*>(o)[i] = (uint16_t)pack_bf16(v[i], 0.0f);
+                    else reinterpret_cast<float*>(o)[i] = v[i];
                 }
             }
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                const int64_t r = r0 + u * WARPS;
-                if (r >= row_hi) continue;
-                float v[8];
-                dy[u].values(v);
-                if (ACT != FP8_ACT_NONE) {
-                    float z[8];
-                    pre[u].values(z);
-#pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
-                        Pair value, slope;
-                        activate_with_slope<ACT>(z[i], z[i + 1], value, slope);
-                        (Pair(v[i], v[i + 1]) * slope).split(v[i], v[i + 1]);
-                    }
-                }
-                const float most = most8(v);
-                top = max_nan(top, most);
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) (Pair(acc[i], acc[i + 1]) + Pair(v[i], v[i + 1])).split(acc[i], acc[i + 1]);
-                const int64_t at = r * p.ldo + col;
-                if (p.store >= FP8_STORE_E4M3) {
-                    const uint2 w = encode8(v, most, scale, p.store == FP8_STORE_E4M3, p.nosat != 0);
-                    uint8_t* o = reinterpret_cast<uint8_t*>(p.out) + at;
-                    if (count == 8) *reinterpret_cast<uint2*>(o) = w;
-                    else
-                        for (int i = 0; i < count; ++i) o[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
-                } else if (p.store == FP8_STORE_BF16) {
-                    const uint4 w = pack8_bf16(v);
-                    uint16_t* o = reinterpret_cast<uint16_t*>(p.out) + at;
-                    if (count == 8) *reinterpret_cast<uint4*>(o) = w;
-                    else
-                        for (int i = 0; i < count; ++i) o[i] = (uint16_t)((i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w) >> (16 * (i & 1)));
-                } else {
-                    float* o = reinterpret_cast<float*>(p.out) + at;
-                    if (count == 8) {
-                        *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-                        *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (i < count) o[i] = v[i];
-                    }
-                }
-            }
+            y += y_step; z += z_step; o += o_step;
         }
     }
     grid_launch_dependents();
     if (p.amax_bits) {
-        if (p.store == FP8_STORE_BF16) top = __uint_as_float(pack_bf16(top, 0.0f) << 16);
+        if (STORE < FP8_STORE_E4M3 && os == 2) top = __uint_as_float(pack_bf16(top, 0.0f) << 16);
         block_atomic_max_bits(canonical_nan_bits(__float_as_uint(top)), red, p.amax_bits);
     }
     if (!p.dbias) return;
@@ -213,12 +249,19 @@ static int64_t chunk_rows(int64_t M, int64_t N) {
     return rows < unit ? unit : rows;
 }
 
+template <int ACT, bool DY_BF16, bool PRE_BF16>
+static cudaError_t launch_backward_as(dim3 grid, cudaStream_t st, const BackwardParams& p) {
+    switch (p.store) {
+        case FP8_STORE_E4M3: return launch_programmatic(k_epilogue_backward<ACT, DY_BF16, PRE_BF16, FP8_STORE_E4M3>, grid, dim3(THREADS), st, p);
+        case FP8_STORE_E5M2: return launch_programmatic(k_epilogue_backward<ACT, DY_BF16, PRE_BF16, FP8_STORE_E5M2>, grid, dim3(THREADS), st, p);
+        default: return launch_programmatic(k_epilogue_backward<ACT, DY_BF16, PRE_BF16, FP8_STORE_BF16>, grid, dim3(THREADS), st, p);
+    }
+}
 template <int ACT>
 static cudaError_t launch_backward(bool dy_bf16, bool pre_bf16, dim3 grid, cudaStream_t st, const BackwardParams& p) {
-    if (dy_bf16) return pre_bf16 ? launch_programmatic(k_epilogue_backward<ACT, true, true>, grid, dim3(THREADS), st, p)
-                                 : launch_programmatic(k_epilogue_backward<ACT, true, false>, grid, dim3(THREADS), st, p);
-    return pre_bf16 ? launch_programmatic(k_epilogue_backward<ACT, false, true>, grid, dim3(THREADS), st, p)
-                    : launch_programmatic(k_epilogue_backward<ACT, false, false>, grid, dim3(THREADS), st, p);
+    if (ACT == FP8_ACT_NONE) pre_bf16 = true;              // not read
+    if (dy_bf16) return pre_bf16 ? launch_backward_as<ACT, true, true>(grid, st, p) : launch_backward_as<ACT, true, ACT == FP8_ACT_NONE>(grid, st, p);
+    return pre_bf16 ? launch_backward_as<ACT, false, true>(grid, st, p) : launch_backward_as<ACT, false, ACT == FP8_ACT_NONE>(grid, st, p);
 }
 
 // ---- global norm and clipping -------------------------------------------------------------------------------------
@@ -341,7 +384,7 @@ __device__ __forceinline__ void clip_chunk(const ClipParams& p, const Entry& e, 
     auto fetch = [&](int64_t i0) {
 #pragma unroll
         for (int b = 0; b < BATCH; ++b)
-            if (i0 + b * THREADS < octets) w[b].load(x, (i0 + b * THREADS) * 8);
+            if (i0 + b * THREADS < octets) w[b].load(x + (i0 + b * THREADS) * (X_BF16 ? 16 : 32));
     };
     fetch(threadIdx.x);
     grid_dependency_wait();
@@ -481,7 +524,7 @@ fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const
         case FP8_ACT_GELU: e = launch_backward<FP8_ACT_GELU>(yb, pb, grid, st, p); break;
         case FP8_ACT_GELU_TANH: e = launch_backward<FP8_ACT_GELU_TANH>(yb, pb, grid, st, p); break;
         case FP8_ACT_SILU: e = launch_backward<FP8_ACT_SILU>(yb, pb, grid, st, p); break;
-        default: e = launch_backward<FP8_ACT_NONE>(yb, true, grid, st, p); break;
+        default: e = launch_backward<FP8_ACT_NONE>(yb, pb, grid, st, p); break;
     }
     if (e != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
     count_launches(1);

@@ -52,13 +52,13 @@ __device__ __forceinline__ bool converts_packed(float most, float scale_d, bool 
 }
 
 // Codes of v * scale_d; `most` is most8(v).
-__device__ __forceinline__ uint2 encode8(const float (&v)[8], float most, float scale_d, bool e4m3, bool nosat) {
-    if (!converts_packed(most, scale_d, e4m3, nosat)) return encode8_special(v, scale_d, e4m3, nosat);
+template <int FMT>
+__device__ __forceinline__ uint2 encode8_as(const float (&v)[8], float most, float scale_d, bool nosat) {
+    if (__builtin_expect(!converts_packed(most, scale_d, FMT == kE4M3, nosat), 0)) return encode8_special(v, scale_d, FMT == kE4M3, nosat);
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; i += 2) (Pair(v[i], v[i + 1]) * Pair(scale_d)).split(y[i], y[i + 1]);
-    return e4m3 ? make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7]))
-                : make_uint2(cvt_quad<kE5M2>(y[0], y[1], y[2], y[3]), cvt_quad<kE5M2>(y[4], y[5], y[6], y[7]));
+    return make_uint2(cvt_quad<FMT>(y[0], y[1], y[2], y[3]), cvt_quad<FMT>(y[4], y[5], y[6], y[7]));
 }
 
 }  // namespace fp8b200
