@@ -823,9 +823,25 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
             }
             issued |= 1u << slot;
         };
+        // factors and biases of this warp's columns of a tile, four columns per lane
+        float factor[4], bias[4];
+        auto fetch_columns = [&](int tn) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = tn * OUT_COLS + part_no * WARP_COLS + i * 32 + lane;
+                factor[i] = alpha0;
+                bias[i] = 0.0f;
+                if (c < N) {
+                    if (p.sb_inv_vec) factor[i] = sa_inv * __ldg(p.sb_inv_vec + c);
+                    if (p.bias) bias[i] = p.bias_bf16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p.bias) + c) << 16)
+                                                      : __ldg(reinterpret_cast<const float*>(p.bias) + c);
+                }
+            }
+        };
+        int tm = 0, tn = 0;
+        fused_tile_coords(worker, tp.tiles_m, tp.tiles_n, tm, tn);     // (every worker has a tile)
+        if (MODE == MODE_EPILOGUE && has_columns) fetch_columns(tn);
         for (int t = worker; t < num_tiles && ok; t += num_workers) {
-            int tm, tn;
-            fused_tile_coords(t, tp.tiles_m, tp.tiles_n, tm, tn);
             const int row0 = tm * TILE_M + (int)cta_rank * BM + q * 32;
             const int col0 = tn * OUT_COLS + part_no * WARP_COLS;
             const bool row_ok = row0 + lane < M;
@@ -834,17 +850,14 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
             if (MODE == MODE_EPILOGUE && has_columns) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int c = col0 + i * 32 + lane;
-                    float factor = alpha0, bias = 0.0f;
-                    if (c < N) {
-                        if (p.sb_inv_vec) factor = sa_inv * __ldg(p.sb_inv_vec + c);
-                        if (p.bias) bias = p.bias_bf16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p.bias) + c) << 16)
-                                                       : __ldg(reinterpret_cast<const float*>(p.bias) + c);
-                    }
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(columns + (uint32_t)(i * 32 + lane) * 4), "f"(factor) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(columns + 512 + (uint32_t)(i * 32 + lane) * 4), "f"(bias) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(columns + (uint32_t)(i * 32 + lane) * 4), "f"(factor[i]) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(columns + 512 + (uint32_t)(i * 32 + lane) * 4), "f"(bias[i]) : "memory");
                 }
                 __syncwarp();
+            }
+            if (t + num_workers < num_tiles) {                         // the next tile's are on their way during this one
+                fused_tile_coords(t + num_workers, tp.tiles_m, tp.tiles_n, tm, tn);
+                if (MODE == MODE_EPILOGUE && has_columns) fetch_columns(tn);
             }
             if (has_in && steps > 0) {
                 if (lane == 0) bulk_wait_read<0>();                    // the previous tile's boxes have left the slots
@@ -884,139 +897,141 @@ k_fused_tiles(const __grid_constant__ TilesMaps maps, const __grid_constant__ Ti
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bars.acc_empty[acc]), 0));
             }
             if (!ok) break;
-            // The loop over steps is rolled: its body is hundreds of instructions, and the warps come through it at different
-            // times, so unrolled they wait for instruction fetches more than for anything else.  Each round works on the
-            // first 32 sums and then moves the others down.  What is rarely needed (special values, ragged edges) is kept
-            // out of the loop's straight line.
+            // The loop takes two steps a round: its body is hundreds of instructions, and the warps come through it at different
+            // times, so fully unrolled they wait for instruction fetches more than for anything else.  A round works on the
+            // first 64 sums, then moves the others down.  What is rarely needed (special values, ragged edges) is kept out of
+            // the straight line.  (One step a round: gated backward at K = 1024 346 us instead of 329.)
 #pragma unroll 1
-            for (int st = 0; st < steps; ++st) {
-                const uint32_t at = staging + (uint32_t)slot * tp.s.slot_bytes;
-                const int col = col0 + st * 32;
-                const bool ragged = col + 32 > N;
-                if (has_in) {
-                    ok = mbar_wait(smem_u32(&bars.in[ew][slot]), (in_phase >> slot) & 1u, abort_flag, F_WAIT_IN);
-                    if (!ok) break;
-                    in_phase ^= 1u << slot;
-                    issued &= ~(1u << slot);
-                } else {
-                    if (lane == 0) {                                   // the boxes last stored from this slot have left it
-                        if (slots >= 4) bulk_wait_read<3>();
-                        else if (slots == 3) bulk_wait_read<2>();
-                        else if (slots == 2) bulk_wait_read<1>();
-                        else bulk_wait_read<0>();
-                    }
-                    __syncwarp();
-                }
-                float* x = part;                                       // this step's sums become its results in place
-                float y[32];
-                if (MODE == MODE_EPILOGUE) {
-                    if (has_columns) {
+            for (int round = 0; round < steps; round += 2) {
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const float4 f = ld_shared_f4(columns + (uint32_t)(st * 32 + u * 4) * 4), b = ld_shared_f4(columns + 512 + (uint32_t)(st * 32 + u * 4) * 4);
-                            x[u * 4 + 0] = fmaf(x[u * 4 + 0], f.x, b.x);
-                            x[u * 4 + 1] = fmaf(x[u * 4 + 1], f.y, b.y);
-                            x[u * 4 + 2] = fmaf(x[u * 4 + 2], f.z, b.z);
-                            x[u * 4 + 3] = fmaf(x[u * 4 + 3], f.w, b.w);
+                for (int half = 0; half < 2; ++half) {
+                    const int st = round + half;
+                    if (st >= steps || !ok) break;
+                    const uint32_t at = staging + (uint32_t)slot * tp.s.slot_bytes;
+                    const int col = col0 + st * 32;
+                    const bool ragged = col + 32 > N;
+                    if (has_in) {
+                        ok = mbar_wait(smem_u32(&bars.in[ew][slot]), (in_phase >> slot) & 1u, abort_flag, F_WAIT_IN);
+                        if (!ok) break;
+                        in_phase ^= 1u << slot;
+                        issued &= ~(1u << slot);
+                    } else {
+                        if (lane == 0) {                                   // the boxes last stored from this slot have left it
+                            if (slots >= 4) bulk_wait_read<3>();
+                            else if (slots == 3) bulk_wait_read<2>();
+                            else if (slots == 2) bulk_wait_read<1>();
+                            else bulk_wait_read<0>();
+                        }
+                        __syncwarp();
+                    }
+                    float* x = part + half * 32;                                       // this step's sums become its results in place
+                    float y[32];
+                    if (MODE == MODE_EPILOGUE) {
+                        if (has_columns) {
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const float4 f = ld_shared_f4(columns + (uint32_t)(st * 32 + u * 4) * 4), b = ld_shared_f4(columns + 512 + (uint32_t)(st * 32 + u * 4) * 4);
+                                x[u * 4 + 0] = fmaf(x[u * 4 + 0], f.x, b.x);
+                                x[u * 4 + 1] = fmaf(x[u * 4 + 1], f.y, b.y);
+                                x[u * 4 + 2] = fmaf(x[u * 4 + 2], f.z, b.z);
+                                x[u * 4 + 3] = fmaf(x[u * 4 + 3], f.w, b.w);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] *= alpha0;
+                        }
+                        if (p.keep[0]) box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) activate<ACT>(x[i], x[i + 1]);
+                        if (has_in) {
+#pragma unroll
+                            for (int o = 0; o < 4; ++o) {
+                                float r[8];
+                                box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, r);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x[o * 8 + i] += r[i];
+                            }
+                        }
+                    } else if (MODE == MODE_GATED) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            (Pair(x[i], x[i + 1]) * Pair(alpha0)).split(x[i], x[i + 1]);
+                            (Pair(part[(64 + half * 32 + i) & 127], part[(65 + half * 32 + i) & 127]) * Pair(alpha1)).split(y[i], y[i + 1]);
+                        }
+                        if (p.keep[0]) {
+                            box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
+                            box_store32_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, y);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            activate<ACT>(x[i], x[i + 1]);
+                            (Pair(x[i], x[i + 1]) * Pair(y[i], y[i + 1])).split(x[i], x[i + 1]);
                         }
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] *= alpha0;
-                    }
-                    if (p.keep[0]) box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) activate<ACT>(x[i], x[i + 1]);
-                    if (has_in) {
-#pragma unroll
                         for (int o = 0; o < 4; ++o) {
-                            float r[8];
-                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, r);
+                            float g[8], u[8];
+                            box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, g);
+                            box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, u);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) x[o * 8 + i] += r[i];
+                            for (int i = 0; i < 8; i += 2) {
+                                Pair value, slope;
+                                activate_with_slope<ACT>(g[i], g[i + 1], value, slope);
+                                const Pair dh = Pair(x[o * 8 + i], x[o * 8 + i + 1]) * Pair(alpha0);
+                                (dh * Pair(u[i], u[i + 1]) * slope).split(x[o * 8 + i], x[o * 8 + i + 1]);
+                                (dh * value).split(y[o * 8 + i], y[o * 8 + i + 1]);
+                            }
                         }
                     }
-                } else if (MODE == MODE_GATED) {
+                    if (__builtin_expect(ragged, 0)) {                     // columns past N count for nothing
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        (Pair(x[i], x[i + 1]) * Pair(alpha0)).split(x[i], x[i + 1]);
-                        (Pair(part[64 + i], part[65 + i]) * Pair(alpha1)).split(y[i], y[i + 1]);
+                        for (int i = 0; i < 32; ++i)
+                            if (col + i >= N) { x[i] = 0.0f; if (MODE == MODE_GATED_BWD) y[i] = 0.0f; }
                     }
-                    if (p.keep[0]) {
-                        box_store32_wide(at + tp.s.keep[0], p.keep_bf16 != 0, lane, x);
-                        box_store32_wide(at + tp.s.keep[1], p.keep_bf16 != 0, lane, y);
+                    float most = most32(x);
+                    emit32<STORE>(p, at + tp.s.out[0], lane, x, most, scale_d);
+                    if (MODE == MODE_GATED_BWD) {
+                        const float most_y = most32(y);
+                        emit32<STORE>(p, at + tp.s.out[NOUT - 1], lane, y, most_y, scale_d);
+                        most = fmax_nan(most, most_y);
                     }
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        activate<ACT>(x[i], x[i + 1]);
-                        (Pair(x[i], x[i + 1]) * Pair(y[i], y[i + 1])).split(x[i], x[i + 1]);
-                    }
-                } else {
-#pragma unroll
-                    for (int o = 0; o < 4; ++o) {
-                        float g[8], u[8];
-                        box_load8(at + tp.s.in[0], p.in_bf16 != 0, lane, o, g);
-                        box_load8(at + tp.s.in[NIN - 1], p.in_bf16 != 0, lane, o, u);
-#pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            Pair value, slope;
-                            activate_with_slope<ACT>(g[i], g[i + 1], value, slope);
-                            const Pair dh = Pair(x[o * 8 + i], x[o * 8 + i + 1]) * Pair(alpha0);
-                            (dh * Pair(u[i], u[i + 1]) * slope).split(x[o * 8 + i], x[o * 8 + i + 1]);
-                            (dh * value).split(y[o * 8 + i], y[o * 8 + i + 1]);
+                    if (row_ok) top = fmax_nan(top, most);
+                    const bool by_hand = ragged && clip_out, keep_by_hand = ragged && clip_keep;
+                    if (__builtin_expect(ragged, 0)) {
+                        const int rows = min(32, M - row0);
+                        const bool inside = col + lane < N;
+                        if (by_hand) {
+                            copy_box_out(p.D[0], out_size, at + tp.s.out[0], row0, rows, col, p.ldd, lane, inside);
+                            if (MODE == MODE_GATED_BWD) copy_box_out(p.D[1], out_size, at + tp.s.out[NOUT - 1], row0, rows, col, p.ldd, lane, inside);
+                        }
+                        if (MODE != MODE_GATED_BWD && keep_by_hand && p.keep[0]) {
+                            copy_box_out(p.keep[0], keep_size, at + tp.s.keep[0], row0, rows, col, p.ld_keep, lane, inside);
+                            if (MODE == MODE_GATED) copy_box_out(p.keep[1], keep_size, at + tp.s.keep[1], row0, rows, col, p.ld_keep, lane, inside);
                         }
                     }
-                }
-                if (__builtin_expect(ragged, 0)) {                     // columns past N count for nothing
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (col + i >= N) { x[i] = 0.0f; if (MODE == MODE_GATED_BWD) y[i] = 0.0f; }
-                }
-                float most = most32(x);
-                emit32<STORE>(p, at + tp.s.out[0], lane, x, most, scale_d);
-                if (MODE == MODE_GATED_BWD) {
-                    const float most_y = most32(y);
-                    emit32<STORE>(p, at + tp.s.out[NOUT - 1], lane, y, most_y, scale_d);
-                    most = fmax_nan(most, most_y);
-                }
-                if (row_ok) top = fmax_nan(top, most);
-                const bool by_hand = ragged && clip_out, keep_by_hand = ragged && clip_keep;
-                if (__builtin_expect(ragged, 0)) {
-                    const int rows = min(32, M - row0);
-                    const bool inside = col + lane < N;
-                    if (by_hand) {
-                        copy_box_out(p.D[0], out_size, at + tp.s.out[0], row0, rows, col, p.ldd, lane, inside);
-                        if (MODE == MODE_GATED_BWD) copy_box_out(p.D[1], out_size, at + tp.s.out[NOUT - 1], row0, rows, col, p.ldd, lane, inside);
-                    }
-                    if (MODE != MODE_GATED_BWD && keep_by_hand && p.keep[0]) {
-                        copy_box_out(p.keep[0], keep_size, at + tp.s.keep[0], row0, rows, col, p.ld_keep, lane, inside);
-                        if (MODE == MODE_GATED) copy_box_out(p.keep[1], keep_size, at + tp.s.keep[1], row0, rows, col, p.ld_keep, lane, inside);
-                    }
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    if (!by_hand) {
-#pragma unroll
-                        for (int i = 0; i < NOUT; ++i) tma_store_3d(&maps.out[i], at + tp.s.out[i], col * out_size, row0, 0, stream);
-                    }
-                    if (MODE != MODE_GATED_BWD && p.keep[0] && !keep_by_hand) {
-#pragma unroll
-                        for (int i = 0; i < (MODE == MODE_GATED ? 2 : 1); ++i) tma_store_3d(&maps.keep[i], at + tp.s.keep[i], col * keep_size, row0, 0, stream);
-                    }
-                    bulk_commit();
-                }
-                if (has_in && st + slots < steps) {                    // the slot's next read, once these boxes have left it
-                    if (lane == 0) bulk_wait_read<0>();
+                    fence_async_smem();
                     __syncwarp();
-                    issue(slot, st + slots, row0, col0);
+                    if (lane == 0) {
+                        if (!by_hand) {
+#pragma unroll
+                            for (int i = 0; i < NOUT; ++i) tma_store_3d(&maps.out[i], at + tp.s.out[i], col * out_size, row0, 0, stream);
+                        }
+                        if (MODE != MODE_GATED_BWD && p.keep[0] && !keep_by_hand) {
+#pragma unroll
+                            for (int i = 0; i < (MODE == MODE_GATED ? 2 : 1); ++i) tma_store_3d(&maps.keep[i], at + tp.s.keep[i], col * keep_size, row0, 0, stream);
+                        }
+                        bulk_commit();
+                    }
+                    if (has_in && st + slots < steps) {                    // the slot's next read, once these boxes have left it
+                        if (lane == 0) bulk_wait_read<0>();
+                        __syncwarp();
+                        issue(slot, st + slots, row0, col0);
+                    }
+                    if (++slot == slots) slot = 0;
                 }
-                if (++slot == slots) slot = 0;
-                if (MODE == MODE_GATED) {
+                if (MODE != MODE_GATED) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) { part[i] = part[32 + i]; part[64 + i] = part[96 + i]; }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 96; ++i) part[i] = part[32 + i];
+                    for (int i = 0; i < 64; ++i) part[i] = part[64 + i];
                 }
             }
         }
