@@ -344,6 +344,10 @@ fp8_status fp8_gemm_splitk(const fp8_gemm_desc* d, const uint8_t* A, const uint8
  * the chip, and the result is stored in a wider type or converted to FP8 on the way out.
  *
  * What a result is stored as: a wide type, or FP8 codes  encode(v * scale_d)  by the rules of fp8_quantize.
+ *
+ * The three products below take an optional workspace (NULL, or 16 bytes of device memory on 16 bytes): with it the amax
+ * needs no launch of its own for its start value.  It must hold zeros before its first use and is left zeroed by every
+ * call, so one serves all calls of a stream; calls that may overlap on the GPU need different ones.
  */
 typedef enum { FP8_STORE_F32 = 0, FP8_STORE_BF16 = 1, FP8_STORE_E4M3 = 2, FP8_STORE_E5M2 = 3 } fp8_store;
 /*
@@ -383,7 +387,7 @@ typedef struct {
 
 fp8_status fp8_gemm_epilogue(const fp8_gemm_desc* d, const fp8_epilogue* e, const uint8_t* A, const uint8_t* B, void* D,
                              const float* scale_inv_a_dev, const float* scale_inv_b_dev, const float* scale_d_dev,
-                             float* amax_d_dev, void* stream);
+                             float* amax_d_dev, void* workspace_dev, void* stream);
 
 /*
  * fp8_gemm_gated — the two up projections of a gated feed-forward block, the activation and the product, in one kernel:
@@ -406,7 +410,7 @@ typedef struct {
 
 fp8_status fp8_gemm_gated(const fp8_gemm_desc* d, const fp8_gated* w, const uint8_t* A, const uint8_t* Bg, const uint8_t* Bu, void* H,
                           const float* scale_inv_a_dev, const float* scale_inv_bg_dev, const float* scale_inv_bu_dev,
-                          const float* scale_h_dev, float* amax_h_dev, void* stream);
+                          const float* scale_h_dev, float* amax_h_dev, void* workspace_dev, void* stream);
 
 /*
  * fp8_gemm_gated_backward — the data gradient of the down projection and the derivative of the gate in one kernel; the
@@ -419,7 +423,7 @@ fp8_status fp8_gemm_gated(const fp8_gemm_desc* d, const fp8_gated* w, const uint
  */
 fp8_status fp8_gemm_gated_backward(const fp8_gemm_desc* d, const fp8_gated* w, const uint8_t* A, const uint8_t* B, void* dG, void* dU,
                                    const float* scale_inv_a_dev, const float* scale_inv_b_dev, const float* scale_d_dev,
-                                   float* amax_dev, void* stream);
+                                   float* amax_dev, void* workspace_dev, void* stream);
 
 /*
  * fp8_epilogue_backward — the backward pass of fp8_gemm_epilogue up to its product, in one pass over the output gradient:
@@ -432,9 +436,10 @@ fp8_status fp8_gemm_gated_backward(const fp8_gemm_desc* d, const fp8_gated* w, c
  * that depends on the shape alone: repeated calls give the same bits.
  * Alignment: dy, pre and out 16-byte aligned with pitches that are multiples of 16 bytes (FP8_ERR_ALIGN).  out may be dy
  * itself (same address, pitch and type).
- *   workspace  needed when dbias_dev is given: fp8_epilogue_backward_workspace_bytes(M, N) bytes, 16-byte aligned.  It must
- *              hold zeros before its first use; every call leaves the part that matters zeroed again, so one buffer of the
- *              largest size serves any number of calls on one stream.  Calls that may overlap need different workspaces.
+ *   workspace  fp8_epilogue_backward_workspace_bytes(M, N) bytes, 16-byte aligned; required when dbias_dev is given, else it
+ *              may be NULL (then the amax takes a launch of its own for its start value).  It must hold zeros before its
+ *              first use; every call leaves the part that matters zeroed again, so one buffer of the largest size serves any
+ *              number of calls on one stream.  Calls that may overlap need different workspaces.
  */
 size_t fp8_epilogue_backward_workspace_bytes(int64_t M, int64_t N);
 fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const void* dy, fp8_wide dy_t, int64_t ldy,

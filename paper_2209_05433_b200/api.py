@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -41,6 +42,13 @@ class GemmDesc(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
                 ("fa", ctypes.c_int), ("fb", ctypes.c_int), ("ma", ctypes.c_int), ("mb", ctypes.c_int),
                 ("lda", ctypes.c_int64), ("ldb", ctypes.c_int64), ("ldd", ctypes.c_int64), ("out", ctypes.c_int), ("acc", ctypes.c_int)]
+
+
+# The structures of the fused products as bytes, in the header's native layout: packing one and passing it costs a third of
+# making the ctypes structure below, and single-token calls are short enough for that to show.
+_pack_desc = struct.Struct("qqqiiiiqqqii").pack
+_pack_epilogue = struct.Struct("iiiiiiPPPPqq").pack
+_pack_gated = struct.Struct("iiiiPPq").pack
 
 
 class Epilogue(ctypes.Structure):
@@ -126,11 +134,11 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.fp8_gemm_splitk.restype = i32
     lib.fp8_gemm_splitk.argtypes = [ctypes.POINTER(GemmDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.fp8_gemm_epilogue.restype = i32
-    lib.fp8_gemm_epilogue.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Epilogue), vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fp8_gemm_epilogue.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.fp8_gemm_gated.restype = i32
-    lib.fp8_gemm_gated.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Gated), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fp8_gemm_gated.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.fp8_gemm_gated_backward.restype = i32
-    lib.fp8_gemm_gated_backward.argtypes = [ctypes.POINTER(GemmDesc), ctypes.POINTER(Gated), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fp8_gemm_gated_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.fp8_epilogue_backward_workspace_bytes.restype = sz
     lib.fp8_epilogue_backward_workspace_bytes.argtypes = [i64, i64]
     lib.fp8_epilogue_backward.restype = i32
@@ -288,6 +296,11 @@ def fp8_gemm(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int, mb: in
 
 def _gemm_desc_2d(A, ma, B, mb, D, fa, fb, acc, codes_out=False):
     """descriptor of a 2-D product from the tensors' shapes and strides; D is a wide tensor, or uint8 codes"""
+    return GemmDesc(*_gemm_fields(A, ma, B, mb, D, fa, fb, acc, codes_out))
+
+
+def _gemm_fields(A, ma, B, mb, D, fa, fb, acc, codes_out=False):
+    """the fields of that descriptor, checked"""
     if A.dtype is not torch.uint8 or B.dtype is not torch.uint8 or A.dim() != 2 or B.dim() != 2 or D.dim() != 2 or (codes_out and D.dtype is not torch.uint8):
         raise TypeError("A and B must be 2-D uint8 tensors and D a 2-D %s tensor" % ("uint8" if codes_out else "float32 or bfloat16"))
     lda, ia = A.stride()
@@ -308,7 +321,7 @@ def _gemm_desc_2d(A, ma, B, mb, D, fa, fb, acc, codes_out=False):
     rows, cols = D.shape
     if K != Kb or rows != M or cols != N:
         raise ValueError("shape mismatch: A gives M=%d K=%d, B gives K=%d N=%d, D is %s" % (M, K, Kb, N, tuple(D.shape)))
-    return GemmDesc(M, N, K, fa, fb, ma, mb, lda, ldb, ldd, BF16 if codes_out else _wide_of(D), acc)
+    return M, N, K, fa, fb, ma, mb, lda, ldb, ldd, BF16 if codes_out else _wide_of(D), acc
 
 
 def fp8_gemm_splitk_workspace(M: int, N: int, K: int) -> tuple[int, int]:
@@ -438,9 +451,26 @@ def _wide2d(t: torch.Tensor, shape, name: str) -> int:
     return _wide_of(t)
 
 
+_amax_workspaces: dict = {}
+
+
+def _amax_args(amax_out: torch.Tensor | None) -> tuple:
+    """(amax address, workspace address, stream) of a fused product: the workspace takes the place of a launch that would
+    zero the amax, and is kept per (device, stream)"""
+    stream = _stream()
+    if amax_out is None:
+        return None, None, stream
+    ptr, key = _scalar(amax_out, "amax_out"), (amax_out.device.index, stream)
+    ws = _amax_workspaces.get(key)
+    if ws is None:
+        ws = torch.zeros(16, dtype=torch.uint8, device=amax_out.device)
+        _amax_workspaces[key] = ws
+    return ptr, ws.data_ptr(), stream
+
+
 def _store_of(D: torch.Tensor, fd: int | None, scale_d: torch.Tensor | None) -> tuple[int, int | None]:
     """(fp8_store, address of the output scale) of an output tensor: wide, or uint8 codes of format fd"""
-    if D.dtype == torch.uint8:
+    if D.dtype is torch.uint8:
         if fd is None or scale_d is None:
             raise TypeError("a uint8 output needs its format fd and its scale_d")
         if fd not in (E4M3, E5M2):
@@ -459,36 +489,38 @@ def fp8_gemm_epilogue(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: in
     """D = act((A . B) * scale_inv_a * scale_inv_b + bias) + residual, one kernel.  Operands as fp8_gemm; ``scale_inv_b``
     has one element or one per column of B.  D is float32, bfloat16, or uint8 codes of format ``fd`` made with ``scale_d``.
     ``pre`` (wide) receives the value before the activation, which fp8_epilogue_backward reads."""
-    codes = D.dtype == torch.uint8
-    d = _gemm_desc_2d(A, ma, B, mb, D, fa, fb, acc, codes_out=codes)
+    fields = _gemm_fields(A, ma, B, mb, D, fa, fb, acc, D.dtype is torch.uint8)
+    N = fields[1]
     store, scale_d_ptr = _store_of(D, fd, scale_d)
-    e = Epilogue(act, store, overflow)
+    bias_t = residual_t = pre_t = BF16
+    bias_ptr = residual_ptr = pre_ptr = sb_vec = 0
+    ldr = ldp = 0
     if scale_inv_b.numel() == 1:
         sb = _scalar(scale_inv_b, "scale_inv_b")
     else:
-        sb, e.scale_inv_b_vec = None, _vec(scale_inv_b, d.N, "scale_inv_b")
+        sb, sb_vec = None, _vec(scale_inv_b, N, "scale_inv_b")
     if bias is not None:
-        if bias.numel() != d.N:
-            raise ValueError("bias must have %d elements" % d.N)
-        e.bias_t, e.bias = _wide_of(bias), _dev(bias, "bias")
+        if bias.numel() != N:
+            raise ValueError("bias must have %d elements" % N)
+        bias_t, bias_ptr = _wide_of(bias), _dev(bias, "bias")
     if residual is not None:
-        e.residual_t, e.residual, e.ldr = _wide2d(residual, D.shape, "residual"), residual.data_ptr(), residual.stride(0)
+        residual_t, residual_ptr, ldr = _wide2d(residual, D.shape, "residual"), residual.data_ptr(), residual.stride(0)
     if pre is not None:
-        e.pre_t, e.pre, e.ldp = _wide2d(pre, D.shape, "pre"), pre.data_ptr(), pre.stride(0)
-    _check(load().fp8_gemm_epilogue(ctypes.byref(d), ctypes.byref(e), A.data_ptr(), B.data_ptr(), D.data_ptr(),
-                                    _scalar(scale_inv_a, "scale_inv_a"), sb, scale_d_ptr,
-                                    None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()), "fp8_gemm_epilogue")
+        pre_t, pre_ptr, ldp = _wide2d(pre, D.shape, "pre"), pre.data_ptr(), pre.stride(0)
+    e = _pack_epilogue(act, store, overflow, bias_t, residual_t, pre_t, sb_vec, bias_ptr, residual_ptr, pre_ptr, ldr, ldp)
+    _check((_lib or load()).fp8_gemm_epilogue(_pack_desc(*fields), e, A.data_ptr(), B.data_ptr(), D.data_ptr(),
+                                              _scalar(scale_inv_a, "scale_inv_a"), sb, scale_d_ptr, *_amax_args(amax_out)), "fp8_gemm_epilogue")
 
 
-def _gate_of(gate, up, shape, act, store, overflow) -> Gated:
-    w = Gated(act, store, overflow)
+def _gate_of(gate, up, shape, act, store, overflow) -> bytes:
     if (gate is None) != (up is None):
         raise ValueError("gate and up go together")
-    if gate is not None:
-        w.gate_t, w.gate, w.up, w.ldg = _wide2d(gate, shape, "gate"), gate.data_ptr(), up.data_ptr(), gate.stride(0)
-        if _wide2d(up, shape, "up") != w.gate_t or up.stride(0) != gate.stride(0):
-            raise ValueError("gate and up must have one dtype and one row pitch")
-    return w
+    if gate is None:
+        return _pack_gated(act, store, overflow, BF16, 0, 0, 0)
+    gate_t, ldg = _wide2d(gate, shape, "gate"), gate.stride(0)
+    if _wide2d(up, shape, "up") != gate_t or up.stride(0) != ldg:
+        raise ValueError("gate and up must have one dtype and one row pitch")
+    return _pack_gated(act, store, overflow, gate_t, gate.data_ptr(), up.data_ptr(), ldg)
 
 
 def fp8_gemm_gated(A: torch.Tensor, fa: int, ma: int, Bg: torch.Tensor, Bu: torch.Tensor, fb: int, mb: int, H: torch.Tensor,
@@ -501,13 +533,12 @@ def fp8_gemm_gated(A: torch.Tensor, fa: int, ma: int, Bg: torch.Tensor, Bu: torc
     two products for the backward pass."""
     if Bg.shape != Bu.shape or Bg.stride() != Bu.stride() or Bu.dtype != Bg.dtype or not Bu.is_cuda:
         raise ValueError("Bg and Bu must be CUDA tensors of one dtype, one shape and one row pitch")
-    d = _gemm_desc_2d(A, ma, Bg, mb, H, fa, fb, acc, codes_out=H.dtype == torch.uint8)
+    fields = _gemm_fields(A, ma, Bg, mb, H, fa, fb, acc, H.dtype is torch.uint8)
     store, scale_d_ptr = _store_of(H, fd, scale_d)
     w = _gate_of(gate, up, H.shape, act, store, overflow)
-    _check(load().fp8_gemm_gated(ctypes.byref(d), ctypes.byref(w), A.data_ptr(), Bg.data_ptr(), Bu.data_ptr(), H.data_ptr(),
+    _check((_lib or load()).fp8_gemm_gated(_pack_desc(*fields), w, A.data_ptr(), Bg.data_ptr(), Bu.data_ptr(), H.data_ptr(),
                                  _scalar(scale_inv_a, "scale_inv_a"), _scalar(scale_inv_bg, "scale_inv_bg"),
-                                 _scalar(scale_inv_bu, "scale_inv_bu"), scale_d_ptr,
-                                 None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()), "fp8_gemm_gated")
+                                 _scalar(scale_inv_bu, "scale_inv_bu"), scale_d_ptr, *_amax_args(amax_out)), "fp8_gemm_gated")
 
 
 def fp8_gemm_gated_backward(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, fb: int, mb: int, gate: torch.Tensor, up: torch.Tensor,
@@ -519,15 +550,14 @@ def fp8_gemm_gated_backward(A: torch.Tensor, fa: int, ma: int, B: torch.Tensor, 
     converted with one ``scale_d`` and covered by one ``amax_out``."""
     if dG.shape != dU.shape or dG.stride() != dU.stride() or dG.dtype != dU.dtype or not dU.is_cuda:
         raise ValueError("dG and dU must be CUDA tensors of one dtype, one shape and one row pitch")
-    d = _gemm_desc_2d(A, ma, B, mb, dG, fa, fb, acc, codes_out=dG.dtype == torch.uint8)
+    fields = _gemm_fields(A, ma, B, mb, dG, fa, fb, acc, dG.dtype is torch.uint8)
     store, scale_d_ptr = _store_of(dG, fd, scale_d)
     if gate is None or up is None:
         raise ValueError("gate and up are required")
     w = _gate_of(gate, up, dG.shape, act, store, overflow)
-    _check(load().fp8_gemm_gated_backward(ctypes.byref(d), ctypes.byref(w), A.data_ptr(), B.data_ptr(), dG.data_ptr(), dU.data_ptr(),
+    _check((_lib or load()).fp8_gemm_gated_backward(_pack_desc(*fields), w, A.data_ptr(), B.data_ptr(), dG.data_ptr(), dU.data_ptr(),
                                           _scalar(scale_inv_a, "scale_inv_a"), _scalar(scale_inv_b, "scale_inv_b"), scale_d_ptr,
-                                          None if amax_out is None else _scalar(amax_out, "amax_out"), _stream()),
-           "fp8_gemm_gated_backward")
+                                          *_amax_args(amax_out)), "fp8_gemm_gated_backward")
 
 
 _backward_workspaces: dict = {}
@@ -536,8 +566,8 @@ _backward_workspaces: dict = {}
 def epilogue_backward_workspace(device: torch.device, M: int, N: int) -> torch.Tensor:
     """A workspace for fp8_epilogue_backward on `device`, kept per (device, stream) and grown as needed."""
     key = (device.index if device.index is not None else torch.cuda.current_device(), _stream())
-    need = int(load().fp8_epilogue_backward_workspace_bytes(M, N))
     ws = _backward_workspaces.get(key)
+    need = int(load().fp8_epilogue_backward_workspace_bytes(M, N))
     if ws is None or ws.numel() < need:
         ws = torch.zeros(need, dtype=torch.uint8, device=device)
         _backward_workspaces[key] = ws
@@ -560,6 +590,7 @@ def fp8_epilogue_backward(dy: torch.Tensor, pre: torch.Tensor | None, out: torch
     ws_ptr, ws_bytes, dbias_ptr = None, 0, None
     if dbias is not None:
         dbias_ptr = _vec(dbias, N, "dbias")
+    if dbias is not None or amax_out is not None:
         ws = epilogue_backward_workspace(dy.device, M, N) if workspace is None else workspace
         ws_ptr, ws_bytes = _dev(ws, "workspace"), ws.numel() * ws.element_size()
     _check(load().fp8_epilogue_backward(M, N, act, dy.data_ptr(), dy_t, dy.stride(0), pre_ptr, pre_t, ldp, store, overflow, scale_ptr,
@@ -609,12 +640,12 @@ WAIT_MBARRIER, WAIT_GRID_BARRIER = 0, 1       # fp8_wait_kind
 
 def fp8_async_status() -> tuple[int, int]:
     """(status, detail) of the device-side error latch; synchronises the device.  After a time-out the cached
-    current-scaling workspaces are cleared again (the kernel leaves them zeroed; this costs nothing and does not
+    workspaces are cleared again (the kernel leaves them zeroed; this costs nothing and does not
     rely on it)."""
     detail = ctypes.c_uint32(0)
     s = load().fp8_async_status(ctypes.byref(detail))
     if int(s) == TIMEOUT:
-        for ws in _workspaces.values():
+        for ws in (*_workspaces.values(), *_amax_workspaces.values(), *_backward_workspaces.values()):
             ws.zero_()
         torch.cuda.synchronize()
     return int(s), int(detail.value)

@@ -97,4 +97,35 @@ __device__ __forceinline__ void block_atomic_max_bits(uint32_t v, uint32_t* smem
     }
 }
 
+// The amax of a whole grid without a start value in memory: every contributor (a warp or a block; one thread of it calls
+// this) folds its maximum into words[0] and counts itself in words[1]; the last one moves the result to `out` and leaves
+// both words zero for the next call.
+__device__ __forceinline__ void fold_amax(uint32_t bits, unsigned int contributors, unsigned int* words, uint32_t* out) {
+    if (bits != 0u) atomicMax(&words[0], bits);
+    __threadfence();
+    if (atomicAdd(&words[1], 1u) == contributors - 1u) {
+        __threadfence();
+        *out = atomicExch(&words[0], 0u);
+        words[1] = 0u;
+    }
+}
+
+// Block-wide maximum, then one fold_amax (words) or one atomicMax on an accumulator that an earlier kernel has zeroed.
+// Every thread of the block must call it; smem holds >= 32 words.
+__device__ __forceinline__ void block_fold_amax(uint32_t v, uint32_t* smem, unsigned int* words, uint32_t* out) {
+    if (!words) {
+        block_atomic_max_bits(v, smem, out);
+        return;
+    }
+    v = warp_max_u32(v);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lane == 0) smem[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+        const int nwarps = (blockDim.x + 31) >> 5;
+        const uint32_t w = warp_max_u32(lane < nwarps ? smem[lane] : 0u);
+        if (lane == 0) fold_amax(w, gridDim.x * gridDim.y * gridDim.z, words, out);
+    }
+}
+
 }  // namespace fp8b200

@@ -99,6 +99,7 @@ struct BackwardParams {
     float* dbias;
     uint32_t* amax_bits;
     unsigned int* counters;                                // one per strip, zero between calls
+    unsigned int* amax_words;                              // two more, or null: *amax_bits is zero when the kernel starts
     float* partial;                                        // [row chunks][N]
     int64_t rows;                                          // of a chunk
     int store, nosat;
@@ -203,7 +204,7 @@ k_epilogue_backward(const BackwardParams p) {
     grid_launch_dependents();
     if (p.amax_bits) {
         if (STORE < FP8_STORE_E4M3 && os == 2) top = __uint_as_float(pack_bf16(top, 0.0f) << 16);
-        block_atomic_max_bits(canonical_nan_bits(__float_as_uint(top)), red, p.amax_bits);
+        block_fold_amax(canonical_nan_bits(__float_as_uint(top)), red, p.amax_words, p.amax_bits);
     }
     if (!p.dbias) return;
 #pragma unroll
@@ -234,8 +235,8 @@ k_epilogue_backward(const BackwardParams p) {
 
 // The counters lie at the start of the workspace in a region of fixed size, so that the partial sums of one shape never
 // lie where another shape's counters are.  Tensors of more strips fill the GPU without cutting rows.
-constexpr int64_t MAX_COUNTERS = 4096;
-constexpr size_t COUNTER_BYTES = MAX_COUNTERS * 4;
+constexpr int64_t MAX_COUNTERS = 4092;                     // and four words, two of them for the amax
+constexpr size_t COUNTER_BYTES = (MAX_COUNTERS + 4) * 4;
 
 // Rows of a chunk: about sixteen blocks per SM over all strips, at least 16 rows (two per warp).
 static int64_t chunk_rows(int64_t M, int64_t N) {
@@ -490,14 +491,14 @@ fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const
             ((ldy * ys) & 15) || ((ldo * os) & 15) || (pre && ((ldp * ps) & 15)))
             return FP8_ERR_ALIGN;
         if (N > ((int64_t)1 << 31) - 512 || M > (int64_t)1 << 40) return FP8_ERR_UNSUPPORTED;
-        if (dbias_dev) {
-            if (!workspace_dev) return FP8_ERR_NULL;
+        if (dbias_dev && !workspace_dev) return FP8_ERR_NULL;
+        if (workspace_dev) {
             if (workspace_bytes < fp8_epilogue_backward_workspace_bytes(M, N)) return FP8_ERR_SHAPE;
             if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) return FP8_ERR_ALIGN;
         }
     }
     cudaStream_t st = (cudaStream_t)stream;
-    if (amax_dev) {
+    if (amax_dev && (!workspace_dev || !some)) {
         const fp8_status rc = launch_zero_word(reinterpret_cast<uint32_t*>(amax_dev), st);
         if (rc != FP8_OK) return rc;
     }
@@ -513,6 +514,7 @@ fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const
     p.dy = dy; p.pre = pre; p.out = out; p.scale = scale_dz_dev; p.dbias = dbias_dev;
     p.amax_bits = reinterpret_cast<uint32_t*>(amax_dev);
     p.counters = reinterpret_cast<unsigned int*>(workspace_dev);
+    p.amax_words = workspace_dev && amax_dev ? p.counters + MAX_COUNTERS : nullptr;
     p.partial = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace_dev) + COUNTER_BYTES);
     p.rows = chunk_rows(M, N);
     p.store = store; p.nosat = overflow == FP8_NOSAT ? 1 : 0;

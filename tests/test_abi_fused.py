@@ -18,11 +18,12 @@ def test_epilogue_refusals():
     one, odd = _addresses()
     d = api.GemmDesc(64, 64, 64, 0, 0, 0, 0, 64, 64, 64, 1)
     e = api.Epilogue(api.ACT_SILU, api.STORE_BF16, api.SATURATE, api.BF16, api.BF16, api.BF16)
-    call = lambda A=one, B=one, D=one, sa=one, sb=one, sd=one: lib.fp8_gemm_epilogue(  # noqa: E731
-        ctypes.byref(d), ctypes.byref(e), A, B, D, sa, sb, sd, None, None)
-    assert lib.fp8_gemm_epilogue(None, ctypes.byref(e), one, one, one, one, one, one, None, None) == NULL
-    assert lib.fp8_gemm_epilogue(ctypes.byref(d), None, one, one, one, one, one, one, None, None) == NULL
+    call = lambda A=one, B=one, D=one, sa=one, sb=one, sd=one, ws=None: lib.fp8_gemm_epilogue(  # noqa: E731
+        ctypes.byref(d), ctypes.byref(e), A, B, D, sa, sb, sd, None, ws, None)
+    assert lib.fp8_gemm_epilogue(None, ctypes.byref(e), one, one, one, one, one, one, None, None, None) == NULL
+    assert lib.fp8_gemm_epilogue(ctypes.byref(d), None, one, one, one, one, one, one, None, None, None) == NULL
     assert call(sa=None) == NULL and call(sb=None) == NULL and call(A=None) == NULL and call(D=None) == NULL
+    assert call(ws=odd) == ALIGN
     assert call(A=odd) == ALIGN and call(B=odd) == ALIGN and call(D=odd) == ALIGN
     for name, bad, good in (("act", 5, 0), ("act", -1, 0), ("store", 4, 1), ("overflow", 2, 0), ("bias_t", 2, 1), ("residual_t", 7, 1), ("pre_t", -1, 1)):
         setattr(e, name, bad)
@@ -61,8 +62,8 @@ def test_gated_refusals():
     one, odd = _addresses()
     d = api.GemmDesc(64, 64, 64, 0, 0, 0, 0, 64, 64, 64, 1)
     w = api.Gated(api.ACT_SILU, api.STORE_BF16, api.SATURATE, api.BF16)
-    fwd = lambda Bu=one, H=one, sh=one: lib.fp8_gemm_gated(ctypes.byref(d), ctypes.byref(w), one, one, Bu, H, one, one, one, sh, None, None)  # noqa: E731
-    bwd = lambda dU=one: lib.fp8_gemm_gated_backward(ctypes.byref(d), ctypes.byref(w), one, one, one, dU, one, one, one, None, None)  # noqa: E731
+    fwd = lambda Bu=one, H=one, sh=one: lib.fp8_gemm_gated(ctypes.byref(d), ctypes.byref(w), one, one, Bu, H, one, one, one, sh, None, None, None)  # noqa: E731
+    bwd = lambda dU=one: lib.fp8_gemm_gated_backward(ctypes.byref(d), ctypes.byref(w), one, one, one, dU, one, one, one, None, None, None)  # noqa: E731
     assert fwd(Bu=None) == NULL and fwd(H=None) == NULL and fwd(Bu=odd) == ALIGN
     assert bwd() == NULL                                 # gate and up are read
     w.gate, w.ldg = one, 64
