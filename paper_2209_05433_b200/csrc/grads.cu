@@ -23,6 +23,16 @@ __device__ __forceinline__ uint4 ld_stream_v4(const void* p) {
     return v;
 }
 
+// Stores whose lines L2 may give up first: written once, read by no kernel here.
+__device__ __forceinline__ uint64_t policy_once() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void st_once_v4(void* p, const uint4& v, uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy) : "memory");
+}
+
 __device__ __forceinline__ void unpack_bf16(const uint4& w, float (&v)[8]) {
     v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
     v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
@@ -381,6 +391,7 @@ __device__ __forceinline__ void clip_chunk(const ClipParams& p, const Entry& e, 
     const uint8_t* x = reinterpret_cast<const uint8_t*>(e.x) + lo * (X_BF16 ? 2 : 4);
     uint8_t* out = reinterpret_cast<uint8_t*>(e.out) + lo * (OUT_BF16 ? 2 : 4);
     const int64_t octets = e.aligned ? n / 8 : 0;
+    const uint64_t once = policy_once();
     Octet<X_BF16> w[BATCH];
     auto fetch = [&](int64_t i0) {
 #pragma unroll
@@ -403,10 +414,10 @@ __device__ __forceinline__ void clip_chunk(const ClipParams& p, const Entry& e, 
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= coef;
             if (OUT_BF16) {
-                reinterpret_cast<uint4*>(out)[i] = pack8_bf16(v);
+                st_once_v4(out + i * 16, pack8_bf16(v), once);
             } else {
-                reinterpret_cast<float4*>(out)[2 * i] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4*>(out)[2 * i + 1] = make_float4(v[4], v[5], v[6], v[7]);
+                st_once_v4(out + i * 32, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])), once);
+                st_once_v4(out + i * 32 + 16, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])), once);
             }
         }
     }
