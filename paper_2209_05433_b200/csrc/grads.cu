@@ -117,7 +117,9 @@ struct BackwardParams {
 
 // A block takes a strip of 256 columns and a chunk of rows, a warp every eighth row.  Each thread keeps the sums of its
 // eight columns; the block adds its warps' sums in order and the last block of a strip adds the chunks' in order.
-// What bounds it: 5 bytes per bf16 element against some fourteen instructions, two of them exp2 and reciprocal.  Addresses
+// What bounds it: 5 bytes per bf16 element against some fourteen instructions, two of them exp2 and reciprocal: 8192 x 16384
+// bf16 -> E5M2 with gelu_tanh and bias gradient 117 us (5.7 TB/s), without activation 82 us; the column sums are 9 of them.
+// Wider strips (up to 2048 columns) or more rows in flight measured the same.  Addresses
 // advance by pointers, bounds are settled outside the row loop and the stored type is fixed at compile time, because
 // branches and address arithmetic were as many instructions as the mathematics (27 per element in all).
 // STORE: FP8_STORE_E4M3, FP8_STORE_E5M2, or a wide type (which one is p.store).
@@ -276,6 +278,10 @@ static cudaError_t launch_backward(bool dy_bf16, bool pre_bf16, dim3 grid, cudaS
 }
 
 // ---- global norm and clipping -------------------------------------------------------------------------------------
+//
+// Bound by HBM: two reads and one write, because the factor needs the whole norm first; 805M bf16 elements 712 us, 6.8 TB/s.
+// What fits L2 is found there the second time (24M elements 26 us), the more since the outputs are written evict-first
+// (30 us without).  Small lists are bound by two launches: 288 tensors, 3M elements, 7.3 us.
 
 constexpr int64_t CHUNK = 32768;                           // elements of a tensor handled by one block
 
