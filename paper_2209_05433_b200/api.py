@@ -463,6 +463,8 @@ def _amax_args(amax_out: torch.Tensor | None) -> tuple:
     ptr, key = _scalar(amax_out, "amax_out"), (amax_out.device.index, stream)
     ws = _amax_workspaces.get(key)
     if ws is None:
+        if torch.cuda.is_current_stream_capturing():     # a buffer made here would be zeroed by replays only
+            return ptr, None, stream
         ws = torch.zeros(16, dtype=torch.uint8, device=amax_out.device)
         _amax_workspaces[key] = ws
     return ptr, ws.data_ptr(), stream
@@ -570,7 +572,8 @@ def epilogue_backward_workspace(device: torch.device, M: int, N: int) -> torch.T
     need = int(load().fp8_epilogue_backward_workspace_bytes(M, N))
     if ws is None or ws.numel() < need:
         ws = torch.zeros(need, dtype=torch.uint8, device=device)
-        _backward_workspaces[key] = ws
+        if not torch.cuda.is_current_stream_capturing():     # else its zeros are part of the graph, and so is the buffer
+            _backward_workspaces[key] = ws
     return ws
 
 

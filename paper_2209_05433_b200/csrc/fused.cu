@@ -1296,7 +1296,8 @@ static fp8_status check_product(const fp8_gemm_desc* d, const uint8_t* A, const 
     }
     if (misaligned(D0, d->ldd * store_bytes(store)) || (two_out && misaligned(D1, d->ldd * store_bytes(store)))) return FP8_ERR_ALIGN;
     const int64_t most = ((int64_t)1 << 31) - 512;
-    if (d->M > most || d->N > most || d->K > most || ((d->M + 127) / 128) * ((d->N + 127) / 128) > (int64_t)1 << 30) return FP8_ERR_UNSUPPORTED;
+    // (byte coordinates along a row of four-byte elements are 32-bit)
+    if (d->M > most || d->N > most / 4 || d->K > most || ((d->M + 127) / 128) * ((d->N + 127) / 128) > (int64_t)1 << 30) return FP8_ERR_UNSUPPORTED;
     return FP8_OK;
 }
 

@@ -504,3 +504,24 @@ def test_refusals():
     with pytest.raises(ValueError):
         api.fp8_gemm_gated_backward(A, E4, K_, B, E4, K_, None, None, D, z(32, 48, dtype=BF), one, one)
     _ok()
+
+
+@pytest.mark.parametrize("M", [3, 300])
+def test_amax_with_and_without_a_workspace(M):
+    """the C entry with a workspace, left zeroed by every call, and without one"""
+    import ctypes
+    N, K = 384, 256
+    g = _gen(M)
+    A, a = _codes(g, M, K, E4, False)
+    B, bt = _codes(g, N, K, E4, False)
+    D = torch.empty(M, N, dtype=F32, device=DEV)
+    d = api.GemmDesc(M, N, K, E4, E4, K_, K_, A.stride(0), B.stride(0), N, api.F32, api.ACC_SPLIT)
+    e = api.Epilogue(api.ACT_NONE, api.STORE_F32, api.SATURATE, 0, 0, 0)
+    one = _scalar(1.0)
+    ws = torch.zeros(16, dtype=torch.uint8, device=DEV)
+    for use in (None, ws, ws, None, ws):
+        amax = _scalar(-3.0)
+        st = api.load().fp8_gemm_epilogue(ctypes.byref(d), ctypes.byref(e), A.data_ptr(), B.data_ptr(), D.data_ptr(), one.data_ptr(), one.data_ptr(), None,
+                                          amax.data_ptr(), None if use is None else use.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        _ok()
+        assert st == 0 and float(amax) == float(D.abs().max()) and int(ws.sum()) == 0

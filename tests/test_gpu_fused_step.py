@@ -96,3 +96,45 @@ def test_the_step_in_a_cuda_graph():
     assert all(torch.equal(scales[n], getattr(net, n).scale) for n in scales)
     assert torch.equal(net.y, wy) and torch.equal(net.norm, wn) and all(torch.equal(net.grads[n], want[n]) for n in want)
     assert api.fp8_async_status()[0] == 0
+
+
+def test_first_calls_of_a_stream_inside_a_capture():
+    """workspaces first needed while a graph is captured: the replays and later plain calls on that stream are both right"""
+    M, N, K = 64, 256, 128
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    A, B = ((torch.randn(r, K, generator=g, device="cuda")).to(torch.float8_e4m3fn).view(torch.uint8) for r in (M, N))
+    dy = torch.randn(300, N, generator=g, device="cuda").to(torch.bfloat16)
+    one = torch.ones(1, device="cuda")
+    D, dz = torch.empty(M, N, dtype=torch.uint8, device="cuda"), torch.empty(300, N, dtype=torch.uint8, device="cuda")
+    amax, amax2, db = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(N, device="cuda")
+
+    def calls():
+        api.fp8_gemm_epilogue(A, api.E4M3, api.MAJOR_K, B, api.E4M3, api.MAJOR_K, D, one, one, fd=api.E4M3, scale_d=one, amax_out=amax)
+        api.fp8_epilogue_backward(dy, None, dz, fd=api.E5M2, scale_d=one, dbias=db, amax_out=amax2)
+
+    calls()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (D, dz, amax, amax2, db)]
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+
+    def check():
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (D, dz, amax, amax2, db)))
+        for t in (D, dz, amax, amax2, db):
+            t.zero_()
+
+    for t in (D, dz, amax, amax2, db):
+        t.zero_()
+    with torch.cuda.stream(side):
+        calls()                                              # before any replay
+    check()
+    for _ in range(2):
+        graph.replay()
+        check()
+    with torch.cuda.stream(side):
+        calls()
+    check()
