@@ -67,7 +67,7 @@ constexpr float kInvSqrtTwoPi = 0.39894228040143268f;
 // Phi(z), the normal distribution function, and bell = exp(-z^2/2).  Rational approximation 7.1.26 of Abramowitz and
 // Stegun, Handbook of Mathematical Functions (absolute error of erf below 1.5e-7, half of that for Phi):
 //   erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) exp(-x^2),  t = 1 / (1 + 0.3275911 x),  x = |z| / sqrt 2.
-// No branches, one exponential that the derivative uses too (the library's erff takes two paths of a dozen terms).
+// No branches, one exponential that the derivative uses too.
 __device__ __forceinline__ Pair normal_cdf(float z0, float z1, Pair& bell) {
     float a, b;
     const Pair z(z0, z1);
