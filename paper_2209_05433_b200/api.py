@@ -456,15 +456,16 @@ _amax_workspaces: dict = {}
 
 def _amax_args(amax_out: torch.Tensor | None) -> tuple:
     """(amax address, workspace address, stream) of a fused product: the workspace takes the place of a launch that would
-    zero the amax, and is kept per (device, stream)"""
+    zero the amax, and is kept per (device, stream).  A captured call takes none: a graph may be replayed on any stream,
+    beside plain calls on the stream it was captured on, and the two words must not be shared by calls that overlap."""
     stream = _stream()
     if amax_out is None:
         return None, None, stream
     ptr, key = _scalar(amax_out, "amax_out"), (amax_out.device.index, stream)
+    if torch.cuda.is_current_stream_capturing():
+        return ptr, None, stream
     ws = _amax_workspaces.get(key)
     if ws is None:
-        if torch.cuda.is_current_stream_capturing():     # a buffer made here would be zeroed by replays only
-            return ptr, None, stream
         ws = torch.zeros(16, dtype=torch.uint8, device=amax_out.device)
         _amax_workspaces[key] = ws
     return ptr, ws.data_ptr(), stream
@@ -566,14 +567,18 @@ _backward_workspaces: dict = {}
 
 
 def epilogue_backward_workspace(device: torch.device, M: int, N: int) -> torch.Tensor:
-    """A workspace for fp8_epilogue_backward on `device`, kept per (device, stream) and grown as needed."""
+    """A workspace for fp8_epilogue_backward on `device`, kept per (device, stream) and grown as needed.  While a graph is
+    captured it is a buffer of the graph's own, cleared by every replay: the kept one may be replaced by a larger one while
+    the graph lives, and the graph may be replayed beside calls that use the kept one."""
+    need = int(load().fp8_epilogue_backward_workspace_bytes(M, N))
+    if torch.cuda.is_current_stream_capturing():
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws[:int(load().fp8_epilogue_backward_workspace_bytes(0, 0))].zero_()     # the counters; partial sums are written before they are read
+        return ws
     key = (device.index if device.index is not None else torch.cuda.current_device(), _stream())
     ws = _backward_workspaces.get(key)
-    need = int(load().fp8_epilogue_backward_workspace_bytes(M, N))
     if ws is None or ws.numel() < need:
-        ws = torch.zeros(need, dtype=torch.uint8, device=device)
-        if not torch.cuda.is_current_stream_capturing():     # else its zeros are part of the graph, and so is the buffer
-            _backward_workspaces[key] = ws
+        ws = _backward_workspaces[key] = torch.zeros(need, dtype=torch.uint8, device=device)
     return ws
 
 
@@ -593,7 +598,7 @@ def fp8_epilogue_backward(dy: torch.Tensor, pre: torch.Tensor | None, out: torch
     ws_ptr, ws_bytes, dbias_ptr = None, 0, None
     if dbias is not None:
         dbias_ptr = _vec(dbias, N, "dbias")
-    if dbias is not None or amax_out is not None:
+    if dbias is not None or (amax_out is not None and (workspace is not None or not torch.cuda.is_current_stream_capturing())):
         ws = epilogue_backward_workspace(dy.device, M, N) if workspace is None else workspace
         ws_ptr, ws_bytes = _dev(ws, "workspace"), ws.numel() * ws.element_size()
     _check(load().fp8_epilogue_backward(M, N, act, dy.data_ptr(), dy_t, dy.stride(0), pre_ptr, pre_t, ldp, store, overflow, scale_ptr,
