@@ -222,13 +222,16 @@ _workspaces: dict = {}
 
 
 def current_scaling_workspace(device: torch.device) -> torch.Tensor:
-    """A zeroed workspace for fp8_quantize_current on `device`, made once per (device, stream)."""
+    """A zeroed workspace for fp8_quantize_current on `device`, made once per (device, stream).  A graph keeps the workspace
+    of the stream it is captured on: where its replays may overlap plain calls of that stream, or another such graph's, pass
+    each a workspace of its own.  One that is first needed inside a capture belongs to the graph, whose replays clear it."""
     key = (device.index if device.index is not None else torch.cuda.current_device(), _stream())
     ws = _workspaces.get(key)
     if ws is None:
         nbytes = int(load().fp8_quantize_current_workspace_bytes())
         ws = torch.zeros(max(nbytes, 16), dtype=torch.uint8, device=device)
-        _workspaces[key] = ws
+        if not torch.cuda.is_current_stream_capturing():
+            _workspaces[key] = ws
     return ws
 
 

@@ -14,13 +14,14 @@ HEAD = 16384
 @pytest.fixture
 def state(monkeypatch):
     s = types.SimpleNamespace(capturing=False, stream=7)
-    lib = types.SimpleNamespace(fp8_epilogue_backward_workspace_bytes=lambda M, N: HEAD + 4 * M * N)
+    lib = types.SimpleNamespace(fp8_epilogue_backward_workspace_bytes=lambda M, N: HEAD + 4 * M * N,
+                                fp8_quantize_current_workspace_bytes=lambda: 64)
     monkeypatch.setattr(api, "load", lambda: lib)
     monkeypatch.setattr(api, "_stream", lambda: s.stream)
     monkeypatch.setattr(api, "_scalar", lambda t, name: t.data_ptr())
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: s.capturing)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    for name in ("_amax_workspaces", "_backward_workspaces"):
+    for name in ("_workspaces", "_amax_workspaces", "_backward_workspaces"):
         monkeypatch.setattr(api, name, {})
     return s
 
@@ -60,3 +61,14 @@ def test_a_capture_never_gets_a_kept_amax_workspace(state):
     assert api._amax_args(amax) == (ptr, None, 7) and api._amax_args(None) == (None, None, 7)
     state.capturing, state.stream = False, 9
     assert api._amax_args(amax)[1] not in (None, kept)
+
+
+def test_a_current_scaling_workspace_made_inside_a_capture_is_not_kept(state):
+    """its zeros are written by replays only, so a plain call could find it uncleared"""
+    state.capturing = True
+    mine = api.current_scaling_workspace(CPU)
+    state.capturing = False
+    kept = api.current_scaling_workspace(CPU)
+    assert kept is not mine and api.current_scaling_workspace(CPU) is kept
+    state.capturing = True
+    assert api.current_scaling_workspace(CPU) is kept
