@@ -630,8 +630,9 @@ class ClipPlan:
         device = self.grads[0].device if self.grads else torch.device("cuda", torch.cuda.current_device())
         host = torch.zeros(max(16, self.sizes.table_bytes), dtype=torch.uint8)
         _check(load().fp8_clip_plan_fill(items, ctypes.byref(self.sizes), host.data_ptr()), "fp8_clip_plan_fill")
-        self.table = host.to(device)
+        # the copy from pageable memory returns when the stream has done it, and with it the zeros: any stream may use the plan
         self.workspace = torch.zeros(self.sizes.workspace_bytes, dtype=torch.uint8, device=device)
+        self.table = host.to(device)
         self._call = (ctypes.byref(self.sizes), self.table.data_ptr(), self.workspace.data_ptr())
 
 

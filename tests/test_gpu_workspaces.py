@@ -93,3 +93,24 @@ def test_graphs_of_one_stream_replayed_beside_its_plain_calls():
         for c in calls:
             c.check()
     _ok()
+
+
+def test_a_clip_plan_is_ready_for_any_stream():
+    """a plan made behind other work of its stream, used at once on another one"""
+    xs = [torch.randint(-3, 4, (100000 + i,), generator=_gen(i), device=DEV).float() for i in range(3)]
+    want = torch.stack([x.double().square().sum() for x in xs]).sum().sqrt().float().reshape(1)      # sums of whole numbers: exact
+    junk = [torch.full((n,), 0xAB, dtype=torch.uint8, device=DEV) for n in (16, 128, 512, 1024, 4096) for _ in range(8)]
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    del junk                                                 # what the allocator hands out next is not zero
+    for _ in range(5):
+        with torch.cuda.stream(first):
+            torch.cuda._sleep(20_000_000)                    # some 10 ms
+            plan = api.ClipPlan(xs, [torch.empty_like(x) for x in xs])
+        norm = _scalar(0.0)
+        torch.cuda.current_stream().synchronize()
+        with torch.cuda.stream(second):
+            api.fp8_grad_clip(plan, 1.0, norm)
+        second.synchronize()
+        assert torch.equal(norm, want)
+    _ok()
