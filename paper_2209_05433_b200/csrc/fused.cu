@@ -1141,6 +1141,23 @@ static int pair_workers(const void* kernel) {
     return n;
 }
 
+// The start value of the amax where no workspace takes its place: enqueued when nothing but the kernel itself is left to do,
+// so that a refused call leaves nothing behind.
+static fp8_status start_amax(const Params& p, cudaStream_t st) {
+    return p.amax_bits && !p.amax_words ? launch_zero_word(p.amax_bits, st) : FP8_OK;
+}
+
+constexpr int64_t MAX_GRID_Y = 65535;
+
+static void skip_rows(Params& p, int64_t rows) {
+    p.M -= rows;
+    for (int i = 0; i < 2; ++i) {
+        if (p.in[i]) p.in[i] = reinterpret_cast<const uint8_t*>(p.in[i]) + rows * p.ld_in * (p.in_bf16 ? 2 : 4);
+        if (p.keep[i]) p.keep[i] = reinterpret_cast<uint8_t*>(p.keep[i]) + rows * p.ld_keep * (p.keep_bf16 ? 2 : 4);
+        if (p.D[i]) p.D[i] = reinterpret_cast<uint8_t*>(p.D[i]) + rows * p.ldd * store_bytes(p.store);
+    }
+}
+
 template <int MODE, int T>
 static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const uint8_t* B0, const uint8_t* B1, Params& p, cudaStream_t st) {
     using G = RowsGeo<MODE, T>;
@@ -1158,7 +1175,6 @@ static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const ui
     p.idesc = (1u << 4) | ((uint32_t)d->fb << 7) | ((uint32_t)d->fa << 10) | ((w_mn ? 1u : 0u) << 15) |
               ((uint32_t)(T >> 3) << 17) | ((uint32_t)(ROWS_BN >> 4) << 24);
     const int64_t tiles_n = (d->N + ROWS_BN - 1) / ROWS_BN, tiles_t = (d->M + T - 1) / T;
-    if (tiles_t > 65535) return FP8_ERR_UNSUPPORTED;
     const int64_t k_blocks = (d->K + BK - 1) / BK;
     unsigned slices = 1;
     while (slices < 8 && tiles_n * tiles_t * slices * 2 <= 2 * (int64_t)sm_count() && k_blocks >= 8 * (int64_t)slices) slices *= 2;
@@ -1167,8 +1183,16 @@ static fp8_status launch_rows(const fp8_gemm_desc* d, const uint8_t* A, const ui
     int stages = G::stages(rows);
     const uint32_t smem = (uint32_t)stages * G::STAGE_BYTES + G::exchange_bytes(rows) + 1024;
     if (!allow_smem(k, ROWS_SMEM)) return FP8_ERR_CUDA;
+    fp8_status rc = start_amax(p, st);
     void* args[] = {&w0, &w1, &x, &p, &stages};
-    return launch_cluster(k, dim3((unsigned)tiles_n, (unsigned)tiles_t, slices), dim3(1, 1, slices), ROWS_THREADS, smem, st, args);
+    // The tiles of a launch lie on grid y, which ends at 65535.  Only an empty sum (K == 0) can have more: it takes several
+    // launches, which fold into one amax (no workspace is used for it).
+    for (int64_t done = 0; rc == FP8_OK && done < tiles_t; done += MAX_GRID_Y) {
+        const int64_t here = tiles_t - done < MAX_GRID_Y ? tiles_t - done : MAX_GRID_Y;
+        rc = launch_cluster(k, dim3((unsigned)tiles_n, (unsigned)here, slices), dim3(1, 1, slices), ROWS_THREADS, smem, st, args);
+        skip_rows(p, here * T);
+    }
+    return rc;
 }
 
 // Tensor map of a wide or FP8 matrix in boxes of 32 rows x 32 columns (`size` bytes per element).
@@ -1229,7 +1253,6 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
               ((uint32_t)(ACC_COLS >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
     const int out_cols = MODE == MODE_GATED ? 128 : 256;
     const int64_t tiles_m = (d->M + TILE_M - 1) / TILE_M, tiles_n = (d->N + out_cols - 1) / out_cols;
-    if (tiles_m * tiles_n > (int64_t)1 << 30) return FP8_ERR_UNSUPPORTED;
     const int k_pad = (int)((d->K + BK - 1) / BK + TILES_FG - 1) / TILES_FG * TILES_FG;
     tp.p = p;
     tp.tiles_m = (int)tiles_m; tp.tiles_n = (int)tiles_n;
@@ -1238,6 +1261,8 @@ static fp8_status launch_tiles(const fp8_gemm_desc* d, const uint8_t* A, const u
     if (!allow_smem(k, TILES_SMEM)) return FP8_ERR_CUDA;
     const int workers = pair_workers(k);
     const int64_t use = tiles_m * tiles_n < workers ? tiles_m * tiles_n : workers;
+    const fp8_status rc = start_amax(p, st);
+    if (rc != FP8_OK) return rc;
     void* args[] = {&m, &tp};
     return launch_cluster(k, dim3((unsigned)(2 * use), 1, 1), dim3(2, 1, 1), TILES_THREADS, TILES_SMEM, st, args);
 }
@@ -1301,17 +1326,17 @@ static fp8_status check_product(const fp8_gemm_desc* d, const uint8_t* A, const 
     return FP8_OK;
 }
 
-// Before the product: the start value of the amax, where no workspace takes its place or nothing will be computed.  With
-// the workspace the call is one launch (2.0 us less host time: one token 4096 -> 128 with codes out 12.6 us, then 10.6), but
-// the kernel ends with three more round trips to L2; without it the launch of the one-thread kernel hides behind the
-// kernel before it.  So the workspace serves the short kernels, bound by launches, and calls that move more than 32 MB (5 us
-// of HBM time) leave it alone: gated block of one token, 134 MB, 22.1 us without and 23.1 us with it.
-// `done`: there is nothing to compute; `words`: the workspace, where it is to be used.
+// How the amax gets its start value.  With the workspace the call is one launch (2.0 us less host time: one token 4096 -> 128
+// with codes out 12.6 us, then 10.6), but the kernel ends with three more round trips to L2; without it the launch of the
+// one-thread kernel hides behind the kernel before it.  So the workspace serves the short kernels, bound by launches, and calls
+// that move more than 32 MB (5 us of HBM time) leave it alone: gated block of one token, 134 MB, 22.1 us without and 23.1 us
+// with it.  Nor is it used where several launches may share the rows (see launch_rows).
+// `done`: there is nothing to compute, and the amax is 0; `words`: the workspace, where it is to be used.
 static fp8_status prepare_amax(const fp8_gemm_desc* d, int operands, float* amax, void* workspace, bool& done, void*& words, cudaStream_t st) {
     done = d->M == 0 || d->N == 0;
     const double bytes = (double)d->K * ((double)d->N * operands + (double)d->M) + 4.0 * (double)d->M * (double)d->N;
-    words = workspace && !done && bytes <= 32.0 * (1 << 20) ? workspace : nullptr;
-    return amax && !words ? launch_zero_word(reinterpret_cast<uint32_t*>(amax), st) : FP8_OK;
+    words = workspace && d->K > 0 && bytes <= 32.0 * (1 << 20) ? workspace : nullptr;
+    return amax && done ? launch_zero_word(reinterpret_cast<uint32_t*>(amax), st) : FP8_OK;
 }
 
 static Params common_params(const fp8_gemm_desc* d, int act, int store, int overflow, const float* scale_d, float* amax, void* workspace) {
