@@ -51,12 +51,17 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
     return d;
 }
 
-// 1 / (1 + 2^y); 2^y overflows to infinity, where the quotient is 0 and so is the limit.
-__device__ __forceinline__ Pair logistic2(Pair y) {
-    float a, b;
+// 1 / (1 + 2^y) and, as `rest`, one minus that: 2^y / (1 + 2^y), not a difference, which would lose the slope's second term
+// where the weight is near 1.  2^y overflows to infinity, where the quotient is 0 and so is the limit; `rest` is then the
+// largest number times 0, not infinity times 0.
+__device__ __forceinline__ Pair logistic2(Pair y, Pair& rest) {
+    float a, b, u, v;
     y.split(a, b);
-    (Pair(exp2_fast(a), exp2_fast(b)) + Pair(1.0f)).split(a, b);
-    return Pair(reciprocal_fast(a), reciprocal_fast(b));
+    const float ea = exp2_fast(a), eb = exp2_fast(b);
+    (Pair(ea, eb) + Pair(1.0f)).split(u, v);
+    const Pair w(reciprocal_fast(u), reciprocal_fast(v));
+    rest = Pair(fminf(ea, 3.402823466e38f), fminf(eb, 3.402823466e38f)) * w;      // NaN: w is NaN
+    return w;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -99,12 +104,22 @@ __device__ __forceinline__ Pair normal_cdf(float z0, float z1, Pair& bell) {
 // and its derivative 0.
 template <int ACT> struct Far { static constexpr float value = ACT == FP8_ACT_SILU ? 100.0f : 16.0f; };
 
+// The weight, and what its derivative takes beside it: gelu the bell, the others one minus the weight.
 template <int ACT>
-__device__ __forceinline__ Pair weight(float z0, float z1, Pair& bell) {
-    if (ACT == FP8_ACT_GELU) return normal_cdf(z0, z1, bell);
+__device__ __forceinline__ Pair weight(float z0, float z1, Pair& other) {
+    if (ACT == FP8_ACT_GELU) return normal_cdf(z0, z1, other);
     const Pair z(z0, z1);
-    if (ACT == FP8_ACT_GELU_TANH) return logistic2(z * fma2(z * z, Pair(-kLog2e * kGeluTwoC * kGeluCubic), Pair(-kLog2e * kGeluTwoC)));
-    return logistic2(z * Pair(-kLog2e));
+    if (ACT == FP8_ACT_GELU_TANH) return logistic2(z * fma2(z * z, Pair(-kLog2e * kGeluTwoC * kGeluCubic), Pair(-kLog2e * kGeluTwoC)), other);
+    return logistic2(z * Pair(-kLog2e), other);
+}
+
+// weight + z * weight', of a weight and its `other`
+template <int ACT>
+__device__ __forceinline__ Pair slope_of(Pair z, Pair w, Pair other) {
+    if (ACT == FP8_ACT_GELU) return fma2(z * Pair(kInvSqrtTwoPi), other, w);
+    const Pair bend = z * w * other;
+    if (ACT == FP8_ACT_SILU) return bend + w;
+    return fma2(bend, fma2(z * z, Pair(3.0f * kGeluTwoC * kGeluCubic), Pair(kGeluTwoC)), w);
 }
 
 // act of two values in place
@@ -114,8 +129,8 @@ __device__ __forceinline__ void activate(float& z0, float& z1) {
         z0 = z0 < 0.0f ? 0.0f : z0;
         z1 = z1 < 0.0f ? 0.0f : z1;
     } else if (ACT != FP8_ACT_NONE) {
-        Pair bell;
-        const Pair w = weight<ACT>(z0, z1, bell);
+        Pair other;
+        const Pair w = weight<ACT>(z0, z1, other);
         // -inf: finite times 0; NaN: the weight is NaN
         (Pair(fmaxf(z0, -Far<ACT>::value), fmaxf(z1, -Far<ACT>::value)) * w).split(z0, z1);
     }
@@ -126,18 +141,9 @@ template <int ACT>
 __device__ __forceinline__ Pair slope_within(float z0, float z1) {
     if (ACT == FP8_ACT_NONE) return Pair(1.0f);
     if (ACT == FP8_ACT_RELU) return Pair(z0 > 0.0f ? 1.0f : 0.0f, z1 > 0.0f ? 1.0f : 0.0f);
-    const Pair z(z0, z1);
-    if (ACT == FP8_ACT_GELU) {
-        Pair bell;
-        const Pair w = normal_cdf(z0, z1, bell);
-        return fma2(z * Pair(kInvSqrtTwoPi), bell, w);
-    }
-    const Pair square = z * z;
-    const Pair w = ACT == FP8_ACT_SILU ? logistic2(z * Pair(-kLog2e))
-                                       : logistic2(z * fma2(square, Pair(-kLog2e * kGeluTwoC * kGeluCubic), Pair(-kLog2e * kGeluTwoC)));
-    const Pair bend = z * w * fma2(w, Pair(-1.0f), Pair(1.0f));               // z w (1 - w)
-    if (ACT == FP8_ACT_SILU) return bend + w;
-    return fma2(bend, fma2(square, Pair(3.0f * kGeluTwoC * kGeluCubic), Pair(kGeluTwoC)), w);
+    Pair other;
+    const Pair w = weight<ACT>(z0, z1, other);
+    return slope_of<ACT>(Pair(z0, z1), w, other);
 }
 
 // act(z) and act'(z) = weight + z * weight' of two values.  The second term is evaluated at z held within +-FAR, where it
@@ -157,16 +163,10 @@ __device__ __forceinline__ void activate_with_slope(float z0, float z1, Pair& va
     constexpr float FAR = Far<ACT>::value;
     const float a0 = fmaxf(z0, -FAR), a1 = fmaxf(z1, -FAR);
     const Pair c(fminf(a0, FAR), fminf(a1, FAR));
-    Pair bell;
-    const Pair w = weight<ACT>(z0, z1, bell);
+    Pair other;
+    const Pair w = weight<ACT>(z0, z1, other);
     value = Pair(a0, a1) * w;
-    if (ACT == FP8_ACT_GELU) {
-        slope = fma2(c * Pair(kInvSqrtTwoPi), bell, w);
-    } else {
-        const Pair bend = c * w * fma2(w, Pair(-1.0f), Pair(1.0f));            // c w (1 - w)
-        if (ACT == FP8_ACT_SILU) slope = bend + w;
-        else slope = fma2(bend, fma2(c * c, Pair(3.0f * kGeluTwoC * kGeluCubic), Pair(kGeluTwoC)), w);
-    }
+    slope = slope_of<ACT>(c, w, other);
 }
 
 // Calls f with the activation as a compile-time constant: f(std::integral_constant-like tag).  `act` is uniform over
