@@ -155,7 +155,10 @@ __device__ __forceinline__ void store4(const Params& p, void* base, int64_t at, 
 
 constexpr int ROWS_THREADS = 192;                  // loader warp, MMA warp, four accumulator warps
 constexpr int ROWS_BN = 128;                       // columns of D per tile = the tensor core's M
-constexpr int ROWS_SPLIT_BLOCKS = 8;               // the tensor core's accumulator is drained every 1024 of K
+// The tensor core's accumulator, whose additions truncate, is drained every 512 of K into sums that round: it costs nothing
+// beside the stream of weights (1 to 64 tokens, three shapes: within 0.1 us of draining every 1024; every 256 costs up to 1 %).
+// With the sizes of a layer the error is the plain form's, 6e-8 of the result in the 2-norm at K = 16384 (1.1e-7 at 1024).
+constexpr int ROWS_SPLIT_BLOCKS = 4;
 constexpr uint32_t ROWS_TMEM_COLS = 256;           // half of an SM's TMEM: two CTAs share an SM
 constexpr uint32_t ROWS_SMEM = 112 * 1024;         // dynamic shared memory of a CTA: two fit an SM
 constexpr int ROWS_MAX_STAGES = 8;

@@ -68,3 +68,21 @@ def test_a_refused_call_leaves_nothing_behind(M):
         api.fp8_gemm_epilogue(A, E4, K_, B, E4, K_, D, one, one, amax_out=amax)
     _ok()
     assert api.fp8_launch_count() == before and float(amax) == 7.0
+
+
+@pytest.mark.parametrize("M", [1, 20, 40, 64])
+def test_few_rows_add_partial_sums_every_512_of_k(M):
+    """The tensor core's additions truncate at 24 bits.  Behind one product of 448 * 448 come 15/1024 in every step of 32 of K:
+    beside the large number (units of 2^-6) each may be lost, but only in the 16 steps of one partial sum.  Then two terms of
+    the bound: 16 units, and one rounding by half a unit for each of at most 3 + 7 additions of partial sums that hold the
+    large number (4 partial sums in a slice of 2048, 8 slices)."""
+    K, N = 16384, 128
+    a, b = torch.zeros(M, K, device=DEV), torch.zeros(N, K, device=DEV)
+    a[:, ::32], b[:, ::32] = 0.5, 15.0 / 512
+    a[:, 0], b[:, 0] = 448.0, 448.0
+    A, B = (t.to(torch.float8_e4m3fn).view(torch.uint8) for t in (a, b))
+    D = torch.empty(M, N, device=DEV)
+    api.fp8_gemm_epilogue(A, E4, K_, B, E4, K_, D, _scalar(1.0), _scalar(1.0))
+    _ok()
+    want = 448.0 * 448 + (K // 32 - 1) * 15.0 / 1024
+    assert bool(((D.double() - want).abs() <= (16 + 10 * 0.5) * 2.0 ** -6).all()), (float(D.min()) - want, float(D.max()) - want)
