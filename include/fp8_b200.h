@@ -352,8 +352,10 @@ fp8_status fp8_gemm_splitk(const fp8_gemm_desc* d, const uint8_t* A, const uint8
 typedef enum { FP8_STORE_F32 = 0, FP8_STORE_BF16 = 1, FP8_STORE_E4M3 = 2, FP8_STORE_E5M2 = 3 } fp8_store;
 /*
  * Activations: relu max(z,0); gelu z*Phi(z) with the normal distribution function Phi; gelu_tanh
- * z*(1 + tanh(sqrt(2/pi)*(z + 0.044715 z^3)))/2; silu z/(1 + exp(-z)).  Computed in binary32; at -inf they are 0 (their
- * limit), NaN stays NaN.  The derivative of relu at 0 is 0.
+ * z*(1 + tanh(sqrt(2/pi)*(z + 0.044715 z^3)))/2; silu z/(1 + exp(-z)).  Computed in binary32 with the hardware's exponential
+ * (2 ulp) and reciprocal (1 ulp), Phi by a fitted polynomial: values are within 3e-7 times max(1, |z|), slopes within 3e-7.
+ * Relative to the value the error grows where the functions vanish (z = -6: gelu 6e-6, gelu_tanh 1e-5, silu 1e-6), and what is
+ * below the normal range becomes 0.  At -inf they are 0 (their limit), NaN stays NaN.  The derivative of relu at 0 and at NaN is 0.
  */
 typedef enum { FP8_ACT_NONE = 0, FP8_ACT_RELU = 1, FP8_ACT_GELU = 2, FP8_ACT_GELU_TANH = 3, FP8_ACT_SILU = 4 } fp8_activation;
 
@@ -451,11 +453,14 @@ fp8_status fp8_epilogue_backward(int64_t M, int64_t N, fp8_activation act, const
  * Global gradient norm and clipping over many tensors — Section 4.1 trains with the recipes of the higher-precision
  * baselines, of which norm clipping is a part; weight gradients are wide tensors.
  *   norm = sqrt(sum over all tensors of x^2);   coef = norm <= max_norm ? 1 : max_norm / norm;   out = round(x * coef)
- * The squares are binary32 (a magnitude above 1.8e19 overflows to an infinite norm, one below 1e-23 counts as 0); sums of
- * 64 and more of them are carried on in binary64.  The order of the additions depends on the plan alone.  A NaN anywhere
+ * The squares and the sums of up to 64 of them are binary32, the rest of the sum binary64.  So a magnitude above 1.8e19, or 64 of
+ * more than 2.3e18 together, overflows to an infinite norm; below 1e-19 squares lose precision, below 2.6e-23 they count as 0.
+ * The order of the additions depends on the plan alone.  The norm is that of the plan's tensors: where gradients are sharded
+ * over ranks, their norms have to be combined by the caller, and the factor of fp8_grad_clip is each rank's own.  A NaN anywhere
  * gives a NaN norm and NaN everywhere in out; an infinite norm gives coef = 0 (0 for finite x, NaN for infinite x).
  *
- * A plan is made once for a list of tensors (their addresses, sizes and types):
+ * A plan is made once for a list of tensors and holds their addresses, sizes and types: it is good as long as they stay where
+ * they are, and a list whose tensors are freed or replaced (gradients dropped after a step) needs a new plan.
  *   fp8_clip_plan_size   fills *plan with the sizes of the table and of the workspace for these items.
  *   fp8_clip_plan_fill   writes the table (plan->table_bytes) to HOST memory; the caller copies it to the device.
  * fp8_grad_norm writes *norm_dev.  fp8_grad_clip writes *norm_dev and every out (out == x clips in place; then nothing is

@@ -612,8 +612,11 @@ def fp8_epilogue_backward(dy: torch.Tensor, pre: torch.Tensor | None, out: torch
 
 class ClipPlan:
     """The tensors that fp8_grad_norm and fp8_grad_clip go over, laid out once: their table and workspace on the device.
-    ``outs`` (same sizes, float32 or bfloat16 each) receive the clipped gradients; None clips in place.  The plan keeps its
-    tensors alive; calls that may overlap on the GPU need plans of their own."""
+    ``outs`` (same sizes, float32 or bfloat16 each) receive the clipped gradients; None clips in place.  The plan goes by the
+    tensors' addresses and keeps them alive: gradients that live in other tensors after a step (``zero_grad`` drops them by
+    default; ``set_to_none=False`` keeps them) need a new plan, whose making copies its table and waits for the stream (288
+    tensors: 430 us, 12 of 67M elements: 80 us).  It must outlive the graphs that captured calls with it.  The norm is that of
+    these tensors alone, not of other ranks'.  Calls that may overlap on the GPU need plans of their own."""
 
     def __init__(self, grads: list[torch.Tensor], outs: list[torch.Tensor] | None = None):
         self.grads, self.outs = list(grads), list(grads if outs is None else outs)

@@ -148,10 +148,11 @@ __device__ __forceinline__ void store4(const Params& p, void* base, int64_t at, 
 // ---- products with few rows ---------------------------------------------------
 //
 // Bound by the stream of weights.  Two CTAs of 112 KB share an SM, so that some 200 KB per SM are in flight (one CTA alone
-// draws 45 GB/s however deep its ring: the issue of its matrix instructions is its limit).  Measured in a graph of such calls:
-// one token 16384 -> 4096 (67 MB) 13.0 us, gated 4096 -> 2 x 16384 (134 MB) 22.1 us, 37 tokens 4096 -> 16384 17.5 us; of the
-// first, 7.4 us are the stream, 1.1 the latency of the first loads, 2.3 partial sums and epilogue, the rest the hand-over
-// between kernels.
+// draws 45 GB/s however deep its ring: the issue of its matrix instructions is its limit).  Measured in a graph that goes round
+// enough different weights (530 to 800 MB) that none is still in L2: one token 16384 -> 4096 (67 MB) 13.6 us (10.3 at the
+// measured copy rate), gated 4096 -> 2 x 16384 (134 MB) 22.7 us (20.5), 37 tokens 4096 -> 16384 18.0 us (10.4).  With one weight
+// again and again, partly found in L2: 11.5, 20.7 and 16.4 us.  Of the first, 1.1 us are the latency of the first loads, 2.3
+// partial sums and epilogue; the rest is the stream and the hand-over between kernels.
 
 constexpr int ROWS_THREADS = 192;                  // loader warp, MMA warp, four accumulator warps
 constexpr int ROWS_BN = 128;                       // columns of D per tile = the tensor core's M
