@@ -486,6 +486,48 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
                          float* norm_dev, void* stream);
 
 /*
+ * Softmax cross entropy of a vocabulary projection — Sections 3.1 and 4.1: the loss that the language models are trained and
+ * evaluated with (perplexity is its exponential), and the first gradient of their backward pass.  The logits never reach
+ * memory: the vocabulary is gone through in pieces, forward and backward.
+ *   z[t,v] = (sum_k x[t,k] * w[v,k]) * (sx_inv * sw_inv)          binary32
+ *   lse[t] = log sum_v exp(z[t,v]),   loss[t] = lse[t] - z[t, target[t]]
+ *   dz[t,v] = (exp(z[t,v] - lse[t]) - [v == target[t]]) * dloss[t]
+ *   dx = dz . w,   dw = dz^T . x       rounded to dx_t, dw_t
+ * Operands: x (tokens x width, pitch ldx) and w (vocab x width, pitch ldw), rows contiguous, both FP8 codes (any pair of
+ * formats, inverse scales required) or both bf16 (the inverse scales may be NULL, which counts as 1).
+ * Targets: 64-bit indices.  A token whose target is not in 0 .. vocab-1 does not count: its loss is 0, its row of dz is 0 and
+ * dloss is not looked at; its lse is written all the same.  (Its row of x still meets these zeros in dw: NaN or infinities
+ * there give NaN.)
+ * The gradient of the logits: FP8 operands take E5M2 codes encode(dz * s) with s = 57344 / max |dloss[t]| over the tokens that
+ * count (1 where that is 0 or not finite): |dz| never exceeds it, so no amax of dz is needed, and what is below 1.2e-10 of it
+ * becomes 0.  bf16 operands take bf16.  dz never leaves the workspace.
+ * Precision: products are exact, their sums as FP8_ACC_SPLIT; exponentials by the hardware (2 ulp).  A row with a NaN or a
+ * plus-infinite logit gives NaN; a row of minus infinities has lse = -inf.
+ * fp8_cross_entropy_backward reads the lse that the forward pass wrote and the per-token factors dloss (1/tokens for a mean).
+ * dx and dw are OVERWRITTEN; either may be NULL.  tokens == 0: dw = 0, nothing else is touched.  width and vocab are at least 1.
+ * x, w, dx, dw are 16-byte aligned with pitches that are multiples of 16 bytes (FP8_ERR_ALIGN) and at least width
+ * (FP8_ERR_SHAPE); the written matrices overlap nothing.
+ * Workspace: device, 16-byte aligned, of the size that fp8_cross_entropy_workspace_bytes gives for the descriptor on the
+ * current device; its contents before and after do not matter.  Calls that may overlap need different ones.
+ * Results depend on the shape and the device alone, not on timing: repeated calls give the same bits.
+ */
+typedef enum { FP8_OPERAND_E4M3 = 0, FP8_OPERAND_E5M2 = 1, FP8_OPERAND_BF16 = 2 } fp8_operand;
+typedef struct {
+    int64_t tokens, width, vocab;
+    fp8_operand x_t, w_t;
+    int64_t ldx, ldw;                  /* elements */
+} fp8_cross_entropy_desc;
+
+fp8_status fp8_cross_entropy_workspace_bytes(const fp8_cross_entropy_desc* d, size_t* forward_bytes_out, size_t* backward_bytes_out);
+fp8_status fp8_cross_entropy(const fp8_cross_entropy_desc* d, const void* x, const void* w, const float* scale_inv_x_dev,
+                             const float* scale_inv_w_dev, const int64_t* target_dev, float* loss_dev, float* lse_dev,
+                             void* workspace_dev, size_t workspace_bytes, void* stream);
+fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const void* x, const void* w, const float* scale_inv_x_dev,
+                                      const float* scale_inv_w_dev, const int64_t* target_dev, const float* lse_dev,
+                                      const float* dloss_dev, void* dx, fp8_wide dx_t, int64_t lddx, void* dw, fp8_wide dw_t,
+                                      int64_t lddw, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
  * fp8_async_status — reads and clears the device-side error latch of the
  * current device (synchronises the device).  FP8_OK, or FP8_ERR_TIMEOUT if a
  * kernel gave up on a bounded wait since the last call; *detail (optional, host

@@ -20,6 +20,7 @@ F32, BF16 = 0, 1             # fp8_wide
 SATURATE, NOSAT = 0, 1       # fp8_overflow
 MAJOR_K, MAJOR_MN = 0, 1     # fp8_major
 ACC_SPLIT, ACC_FAST = 0, 1    # fp8_accumulate: bounded error for any data (default) / one accumulator
+OPERAND_BF16 = 2             # fp8_operand: E4M3, E5M2, or this
 STORE_F32, STORE_BF16, STORE_E4M3, STORE_E5M2 = 0, 1, 2, 3                       # fp8_store
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4            # fp8_activation
 
@@ -31,6 +32,7 @@ EXPORTS = ["fp8_amax", "fp8_scale_from_amax", "fp8_quantize", "fp8_quantize_curr
            "fp8_gemm_epilogue", "fp8_gemm_gated", "fp8_gemm_gated_backward",
            "fp8_epilogue_backward", "fp8_epilogue_backward_workspace_bytes",
            "fp8_clip_plan_size", "fp8_clip_plan_fill", "fp8_grad_norm", "fp8_grad_clip",
+           "fp8_cross_entropy_workspace_bytes", "fp8_cross_entropy", "fp8_cross_entropy_backward",
            "fp8_async_status", "fp8_self_test_expire_wait", "fp8_sm_clock_probe", "fp8_status_string", "fp8_launch_count"]
 
 
@@ -60,6 +62,15 @@ class Epilogue(ctypes.Structure):
 class Gated(ctypes.Structure):
     _fields_ = [("act", ctypes.c_int), ("store", ctypes.c_int), ("overflow", ctypes.c_int), ("gate_t", ctypes.c_int),
                 ("gate", ctypes.c_void_p), ("up", ctypes.c_void_p), ("ldg", ctypes.c_int64)]
+
+
+_pack_cross_entropy = struct.Struct("qqqiiqq").pack
+
+
+class CrossEntropyDesc(ctypes.Structure):
+    """fp8_cross_entropy_desc of the header"""
+    _fields_ = [("tokens", ctypes.c_int64), ("width", ctypes.c_int64), ("vocab", ctypes.c_int64), ("x_t", ctypes.c_int), ("w_t", ctypes.c_int),
+                ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64)]
 
 
 class ClipItem(ctypes.Structure):
@@ -151,6 +162,12 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.fp8_grad_norm.argtypes = [ctypes.POINTER(ClipSizes), vp, vp, vp, vp]
     lib.fp8_grad_clip.restype = i32
     lib.fp8_grad_clip.argtypes = [ctypes.POINTER(ClipSizes), vp, vp, ctypes.c_float, vp, vp]
+    lib.fp8_cross_entropy_workspace_bytes.restype = i32
+    lib.fp8_cross_entropy_workspace_bytes.argtypes = [vp, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.fp8_cross_entropy.restype = i32
+    lib.fp8_cross_entropy.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.fp8_cross_entropy_backward.restype = i32
+    lib.fp8_cross_entropy_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i64, vp, i32, i64, vp, sz, vp]
     lib.fp8_async_status.restype = i32
     lib.fp8_async_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     lib.fp8_self_test_expire_wait.restype = i32
@@ -647,6 +664,100 @@ def fp8_grad_norm(plan: ClipPlan, norm_out: torch.Tensor) -> None:
 def fp8_grad_clip(plan: ClipPlan, max_norm: float, norm_out: torch.Tensor) -> None:
     """Global 2-norm of the plan's gradients, and outs = grads * min(1, max_norm / norm)."""
     _check(load().fp8_grad_clip(*plan._call, max_norm, _scalar(norm_out, "norm_out"), _stream()), "fp8_grad_clip")
+
+
+def _here(t: torch.Tensor, name: str) -> torch.Tensor:
+    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+        raise ValueError("%s must be a tensor of the current CUDA device" % name)
+    return t
+
+
+def _pitch_of(t: torch.Tensor) -> int:
+    """Row pitch in elements; of a single row, whose stride means nothing, one that suits any alignment."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+
+
+def _vocabulary_operand(t: torch.Tensor, fmt: int | None, name: str) -> int:
+    """fp8_operand of a 2-D operand with contiguous rows: uint8 codes of format fmt, or bfloat16 with fmt None"""
+    _here(t, name)
+    if t.dim() != 2 or t.stride(1) != 1:
+        raise ValueError("%s must be a 2-D tensor with unit inner stride" % name)
+    if t.dtype is torch.uint8:
+        if fmt not in (E4M3, E5M2):
+            raise TypeError("the codes of %s need their format, E4M3 or E5M2" % name)
+        return fmt
+    if t.dtype is not torch.bfloat16 or fmt is not None:
+        raise TypeError("%s must be uint8 codes with their format, or bfloat16 with format None" % name)
+    return OPERAND_BF16
+
+
+def _per_token(t: torch.Tensor, dtype: torch.dtype, tokens: int, name: str) -> int:
+    _here(t, name)
+    if t.dtype is not dtype or t.shape != (tokens,) or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous %s tensor with %d elements" % (name, dtype, tokens))
+    return t.data_ptr()
+
+
+def _cross_entropy_args(x, fx, w, fw, scale_inv_x, scale_inv_w):
+    x_t, w_t = _vocabulary_operand(x, fx, "x"), _vocabulary_operand(w, fw, "w")
+    tokens, width = x.shape
+    vocab, width_w = w.shape
+    if width != width_w:
+        raise ValueError("x has rows of %d, w of %d" % (width, width_w))
+    d = _pack_cross_entropy(tokens, width, vocab, x_t, w_t, _pitch_of(x), _pitch_of(w))
+    sx = None if scale_inv_x is None else _scalar(_here(scale_inv_x, "scale_inv_x"), "scale_inv_x")
+    sw = None if scale_inv_w is None else _scalar(_here(scale_inv_w, "scale_inv_w"), "scale_inv_w")
+    return tokens, width, vocab, d, (x.data_ptr(), w.data_ptr(), sx, sw)
+
+
+def cross_entropy_workspace_bytes(tokens: int, width: int, vocab: int, bf16: bool = False) -> tuple[int, int]:
+    """Workspace bytes of (fp8_cross_entropy, fp8_cross_entropy_backward) on the current device."""
+    t = OPERAND_BF16 if bf16 else E4M3
+    forward, backward = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check((_lib or load()).fp8_cross_entropy_workspace_bytes(_pack_cross_entropy(tokens, width, vocab, t, t, 0, 0), ctypes.byref(forward), ctypes.byref(backward)),
+           "fp8_cross_entropy_workspace_bytes")
+    return forward.value, backward.value
+
+
+def _loss_workspace(d: bytes, which: int, device: torch.device, workspace: torch.Tensor | None) -> tuple:
+    """(address, bytes, what keeps it alive).  Its contents mean nothing, so it comes from torch's allocator for this call:
+    memory that goes back to it is handed out on this stream alone, or belongs to the graph that is being captured."""
+    if workspace is not None:
+        return _dev(_here(workspace, "workspace"), "workspace"), workspace.numel() * workspace.element_size(), workspace
+    sizes = (ctypes.c_size_t(0), ctypes.c_size_t(0))
+    _check((_lib or load()).fp8_cross_entropy_workspace_bytes(d, ctypes.byref(sizes[0]), ctypes.byref(sizes[1])), "fp8_cross_entropy_workspace_bytes")
+    ws = torch.empty(max(16, sizes[which].value), dtype=torch.uint8, device=device)
+    return ws.data_ptr(), ws.numel(), ws
+
+
+def fp8_cross_entropy(x: torch.Tensor, fx: int | None, w: torch.Tensor, fw: int | None, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                      scale_inv_x: torch.Tensor | None = None, scale_inv_w: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> None:
+    """loss[t] = log sum_v exp z[t, v] - z[t, target[t]] with z = (x . w^T) * scale_inv_x * scale_inv_w, which is never stored.
+
+    x [tokens, width] and w [vocab, width] are uint8 codes of the formats ``fx`` and ``fw``, or both bfloat16 (formats None).
+    target is int64; a token whose target is outside 0 .. vocab - 1 does not count (loss 0).  loss and lse are float32, one
+    element per token; the backward pass reads lse.  ``workspace`` of cross_entropy_workspace_bytes(...)[0] bytes is taken from
+    torch's allocator where none is given."""
+    tokens, _, _, d, operands = _cross_entropy_args(x, fx, w, fw, scale_inv_x, scale_inv_w)
+    target_ptr = _per_token(target, torch.int64, tokens, "target")
+    loss_ptr, lse_ptr = _per_token(loss, torch.float32, tokens, "loss"), _per_token(lse, torch.float32, tokens, "lse")
+    ws, nbytes, _keep = _loss_workspace(d, 0, x.device, workspace)
+    _check(_lib.fp8_cross_entropy(d, *operands, target_ptr, loss_ptr, lse_ptr, ws, nbytes, _stream()), "fp8_cross_entropy")
+
+
+def fp8_cross_entropy_backward(x: torch.Tensor, fx: int | None, w: torch.Tensor, fw: int | None, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                               dx: torch.Tensor | None, dw: torch.Tensor | None, scale_inv_x: torch.Tensor | None = None,
+                               scale_inv_w: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> None:
+    """Gradients of sum(dloss * loss): dx [tokens, width] and dw [vocab, width], float32 or bfloat16 each, overwritten; None
+    leaves one out.  ``lse`` is what fp8_cross_entropy wrote, ``dloss`` one float32 factor per token (1 / tokens for a mean).  The
+    gradient of the logits passes through E5M2 codes (FP8 operands) or bfloat16, a piece of the vocabulary at a time."""
+    tokens, width, vocab, d, operands = _cross_entropy_args(x, fx, w, fw, scale_inv_x, scale_inv_w)
+    target_ptr = _per_token(target, torch.int64, tokens, "target")
+    lse_ptr, dloss_ptr = _per_token(lse, torch.float32, tokens, "lse"), _per_token(dloss, torch.float32, tokens, "dloss")
+    dx_args = (None, BF16, width) if dx is None else (_here(dx, "dx").data_ptr(), _wide2d(dx, (tokens, width), "dx"), _pitch_of(dx))
+    dw_args = (None, BF16, width) if dw is None else (_here(dw, "dw").data_ptr(), _wide2d(dw, (vocab, width), "dw"), _pitch_of(dw))
+    ws, nbytes, _keep = _loss_workspace(d, 1, x.device, workspace)
+    _check(_lib.fp8_cross_entropy_backward(d, *operands, target_ptr, lse_ptr, dloss_ptr, *dx_args, *dw_args, ws, nbytes, _stream()), "fp8_cross_entropy_backward")
 
 
 TIMEOUT = 7                                   # FP8_ERR_TIMEOUT

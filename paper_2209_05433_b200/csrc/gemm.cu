@@ -852,7 +852,10 @@ fp8_status fp8_self_test_expire_wait(int which, uint64_t limit_cycles, void* str
 
 void fp8_cast_read_clear_latch(unsigned int out2[2]);      // defined with the cast kernels
 }
-namespace fp8b200 { void fused_read_clear_latch(unsigned int out2[2]); }      // defined with the fused products
+namespace fp8b200 {
+void fused_read_clear_latch(unsigned int out2[2]);         // defined with the fused products
+void loss_read_clear_latch(unsigned int out2[2]);          // defined with the loss
+}
 extern "C" {
 
 fp8_status fp8_async_status(uint32_t* detail) {
@@ -861,6 +864,7 @@ fp8_status fp8_async_status(uint32_t* detail) {
     unsigned int cast_latch[2];
     fp8_cast_read_clear_latch(cast_latch);
     if (cast_latch[0] == 0u) fused_read_clear_latch(cast_latch);
+    if (cast_latch[0] == 0u) loss_read_clear_latch(cast_latch);
     if (cudaMemcpyFromSymbol(latch, g_async_latch, sizeof(latch)) != cudaSuccess) return FP8_ERR_CUDA;
     if (latch[0] == 0u && cast_latch[0] != 0u) {
         if (detail) *detail = cast_latch[0];

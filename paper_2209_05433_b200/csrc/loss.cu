@@ -1,0 +1,848 @@
+// Softmax cross entropy of a vocabulary projection, and its gradients (sm_100a): the logits never reach memory.
+//
+//   z = (x . w^T) * (sx * sw)          T x V, in tiles of 256 x 256 in tensor memory
+//   lse_t = log sum_v exp z[t,v],      loss_t = lse_t - z[t, target_t]
+//   dz[t,v] = (exp(z[t,v] - lse_t) - [v = target_t]) * dloss_t,     dx = dz . w,     dw = dz^T . x
+//
+// Forward: the epilogue of a tile reduces its columns to one (maximum, sum of exponentials) pair per row; a second kernel
+// joins the pairs of a row, in a fixed order.  Backward: the vocabulary in pieces; for each the tile is multiplied again,
+// its epilogue turns it into dz (E5M2 codes for FP8 operands, bf16 for bf16), and two products read dz.  dx is added up
+// over the pieces in binary32.
+//
+// Exponentials are taken to base 2 of logits that were scaled by log2(e) with the operands' inverse scales.
+//
+// All products here are one kernel on persistent CTAs or CTA pairs: TMA-fed ring, tcgen05 into two TMEM accumulators, and
+// eight epilogue warps that take the accumulator into registers every 2048 of K (partial sums are added there with
+// round-to-nearest: the tensor core's own additions truncate) and hand it back before they work on it.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <mutex>
+
+#include "activation.cuh"
+#include "codec.cuh"
+#include "common.cuh"
+#include "umma.cuh"
+
+namespace fp8b200 {
+namespace loss {
+
+using namespace gemm;
+
+constexpr int MODE_STATS = 0;           // (maximum, sum of exponentials) of a row's columns, and the target's logit
+constexpr int MODE_DZ = 1;              // gradient of the logits
+constexpr int MODE_BF16 = 2;            // the scaled product, rounded
+constexpr int MODE_F32 = 3;             // the scaled product
+constexpr int MODE_ADD = 4;             // added to what is there, in binary32
+
+constexpr int ROWS = 128;               // rows of a CTA's tile (one TMEM lane each)
+constexpr int K_BYTES = 128;            // K-block: one 128-byte swizzle row, 128 elements of 8 bits or 64 of 16
+constexpr int K_STEP_BYTES = 32;        // K of one tcgen05.mma
+constexpr int SPLIT_BYTES = 2048;       // of K, in elements of either size: what one use of the accumulator covers
+constexpr int FG = 2;                   // K-blocks consumed per barrier wait
+constexpr int MAX_STAGES = 6;
+constexpr uint32_t A_BYTES = ROWS * K_BYTES;
+constexpr uint32_t RING_BYTES = 196608;
+constexpr uint32_t BOX_BYTES = 4096;    // 32 rows x 128 B: staging of one epilogue warp
+constexpr int EPI_BASE = 4, EPI_WARPS = 8, THREADS = 32 * (EPI_BASE + EPI_WARPS);
+constexpr int REGS_FRONT = 56, REGS_EPILOGUE = 224;      // 128 x 56 + 256 x 224 = 64512, the launch's 384 x 168
+constexpr uint32_t SMEM_BYTES = RING_BYTES + EPI_WARPS * BOX_BYTES + 256 + 1024;
+constexpr uint32_t TMEM_COLS = 512;
+constexpr int GROUP_M = 16;             // row tiles that advance together over the columns
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
+// codes written to the error latch
+enum : uint32_t { L_WAIT_EMPTY = 49, L_WAIT_FULL = 50, L_WAIT_ACC_EMPTY = 51, L_WAIT_ACC_FULL = 52 };
+
+struct Params {
+    int64_t M, N, K;
+    const float* s[2];                  // factors of the product; null counts as 1
+    uint32_t idesc;
+    int tiles_m, tiles_n;
+    int slices, slice_blocks;           // K in slices of slice_blocks K-blocks, each with an output plane of its own
+    int a_mn, b_mn;                     // operand stored with its M (N) index contiguous
+    void* D;
+    int64_t ldd;                        // elements
+    int ragged;                         // rows of D do not end on 16 bytes
+    const int64_t* target;
+    int64_t first, vocab;               // vocabulary column of the first column here; all columns of the vocabulary
+    float2* part;                       // [2 tiles_n][M]
+    float* logit;                       // [M]: the target's, times log2(e)
+    const float* lse;
+    const float* dloss;
+    const float* dz_scale;              // scale of dz's codes; null: dz is bf16
+};
+
+struct alignas(8) Barriers {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem_base, abort_flag;
+};
+static_assert(sizeof(Barriers) <= 256, "barrier block too large");
+
+__device__ __forceinline__ void mma_bf16(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_bf16_pair(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+// tile index -> (row tile, column tile): GROUP_M row tiles share each sweep over the columns
+__device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int per_group = GROUP_M * tiles_n;
+    const int g = t / per_group, first = g * GROUP_M;
+    const int rows = min(GROUP_M, tiles_m - first);
+    const int r = t - g * per_group;
+    tm = first + r % rows;
+    tn = r / rows;
+}
+
+// ESZ: bytes of an operand's element (1: FP8, 2: bf16).  CG: CTAs of a tile.  BN: its columns.
+template <int ESZ, int CG, int BN, int MODE>
+__global__ void __launch_bounds__(THREADS, 1)
+k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_d,
+             const Params p) {
+    constexpr int KE = K_BYTES / ESZ;                             // elements of a K-block
+    constexpr int MNE = 128 / ESZ;                                // M or N elements of a 128-byte row of an MN-major box
+    constexpr uint32_t MN_BOX = (uint32_t)KE * 128;               // such a box: MNE elements x one K-block
+    constexpr int B_ROWS = BN / CG;                               // columns of the tile that this CTA loads
+    constexpr uint32_t STAGE_BYTES = A_BYTES + B_ROWS * K_BYTES;
+    constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+    static_assert(STAGES % FG == 0 && STAGES <= MAX_STAGES, "ring depth");
+    constexpr int SPLIT = SPLIT_BYTES / KE;                       // K-blocks per use of an accumulator
+    constexpr int NC = BN / 2;                                    // columns of an epilogue thread
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;
+    Barriers* bars = reinterpret_cast<Barriers*>(smem_raw + (ring - raw) + RING_BYTES + EPI_WARPS * BOX_BYTES);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_ctarank() : 0u;       // 0 = leader of the pair
+    const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+    const int plane_tiles = p.tiles_m * p.tiles_n, tiles = plane_tiles * p.slices;
+    const int k_blocks = (int)((p.K + KE - 1) / KE);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), FG * CG); mbar_init(smem_u32(&bars->empty[s]), 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars->acc_full[a]), 1); mbar_init(smem_u32(&bars->acc_empty[a]), EPI_WARPS * CG); }
+        bars->abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = bars->tmem_base;
+    // Nothing that an earlier kernel may still be writing is touched above this line.
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    if (warp < EPI_BASE) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FRONT));
+    if (warp == 0) {
+        // ---- loads: this CTA's rows of A and columns of B, one destination each
+        uint32_t stage = 0, phase = 0;
+        bool ok = true;
+        const uint64_t keep = policy_evict_last();
+        int nth = 0;
+        for (int t = worker; t < tiles && ok; t += workers) {
+            int tm, tn;
+            const int slice = t / plane_tiles;
+            tile_at(t - slice * plane_tiles, p.tiles_m, p.tiles_n, tm, tn);
+            const int m0 = (tm * CG + (int)rank) * ROWS, n0 = tn * BN + (int)rank * B_ROWS;
+            const int kb0 = slice * p.slice_blocks, kn = min(p.slice_blocks, k_blocks - kb0);
+            const int kn_pad = (kn + FG - 1) / FG * FG;
+            const bool backwards = (nth++ & 1) != 0;              // every second tile starts where the last one ended: L2 still has it
+            for (int kb = 0; kb < kn_pad; ++kb) {
+                ok = mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, L_WAIT_EMPTY);
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + A_BYTES;
+                    const uint32_t bar = smem_u32(&bars->full[stage / FG]);
+                    const uint32_t full = CG == 2 ? map_to_cta(bar, 0) : bar;          // the leader's
+                    if (kb < kn) {
+                        const int k = kb0 + (backwards ? kn - 1 - kb : kb);
+                        auto load = [&](uint32_t dst, const CUtensorMap* map, int c0, int c1) {
+                            if (CG == 2) tma_load_3d_pair(dst, map, c0, c1, 0, full, keep);
+                            else         tma_load_3d(dst, map, c0, c1, 0, full, keep);
+                        };
+                        if (CG == 2) mbar_arrive_expect_tx_cluster(full, STAGE_BYTES);
+                        else         mbar_arrive_expect_tx(full, STAGE_BYTES);
+                        if (p.a_mn) {
+#pragma unroll
+                            for (int j = 0; j < ROWS / MNE; ++j) load(sa + j * MN_BOX, &map_a, m0 * ESZ + j * 128, k * KE);
+                        } else {
+                            load(sa, &map_a, k * K_BYTES, m0);
+                        }
+                        if (p.b_mn) {
+#pragma unroll
+                            for (int j = 0; j < B_ROWS / MNE; ++j) load(sb + j * MN_BOX, &map_b, n0 * ESZ + j * 128, k * KE);
+                        } else {
+                            load(sb, &map_b, k * K_BYTES, n0);
+                        }
+                    } else if (CG == 2) {
+                        mbar_arrive_cluster(full);                // padding block: nothing to load
+                    } else {
+                        mbar_arrive(full);
+                    }
+                }
+                __syncwarp();
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        // ---- tensor core (leader only)
+        uint32_t stage = 0, phase = 0;
+        bool ok = rank == 0;
+        int it = 0;
+        // K-major: groups of 8 rows 1024 B apart, 32 B per step.  MN-major: groups of 8 k 1024 B apart, boxes MN_BOX apart.
+        const uint32_t a_step = p.a_mn ? K_STEP_BYTES / ESZ * 128 : K_STEP_BYTES, a_lbo = p.a_mn ? MN_BOX : 16;
+        const uint32_t b_step = p.b_mn ? K_STEP_BYTES / ESZ * 128 : K_STEP_BYTES, b_lbo = p.b_mn ? MN_BOX : 16;
+        for (int t = worker; t < tiles && ok; t += workers) {
+            const int kb0 = t / plane_tiles * p.slice_blocks, kn = min(p.slice_blocks, k_blocks - kb0);
+            const int kn_pad = (kn + FG - 1) / FG * FG;
+            for (int kc = 0; kc < kn_pad && ok; kc += SPLIT, ++it) {
+                const uint32_t acc = (uint32_t)it & 1u;
+                ok = mbar_wait(smem_u32(&bars->acc_empty[acc]), (((uint32_t)it >> 1) & 1u) ^ 1u, abort_flag, L_WAIT_ACC_EMPTY);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t tmem_d = tmem_base + acc * BN;
+                const int kend = min(kn_pad, kc + SPLIT), last = min(kn, kend) - 1;
+                for (int kb = kc; kb < kend; kb += FG) {
+                    ok = mbar_wait(smem_u32(&bars->full[stage / FG]), phase, abort_flag, L_WAIT_FULL);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int h = 0; h < FG; ++h) {
+                            const uint32_t st = stage + h;
+                            if (kb + h < kn) {
+                                const uint32_t sa = ring + st * STAGE_BYTES, sb = sa + A_BYTES;
+#pragma unroll
+                                for (int k = 0; k < K_BYTES / K_STEP_BYTES; ++k) {
+                                    const uint64_t da = smem_desc(sa + k * a_step, a_lbo, 1024), db = smem_desc(sb + k * b_step, b_lbo, 1024);
+                                    const uint32_t more = ((kb - kc) | h | k) != 0 ? 1u : 0u;
+                                    if (ESZ == 1) {
+                                        if (CG == 2) tc_mma_f8_pair(tmem_d, da, db, p.idesc, more);
+                                        else         tc_mma_f8(tmem_d, da, db, p.idesc, more);
+                                    } else {
+                                        if (CG == 2) mma_bf16_pair(tmem_d, da, db, p.idesc, more);
+                                        else         mma_bf16(tmem_d, da, db, p.idesc, more);
+                                    }
+                                }
+                            }
+                            if (CG == 2) {
+                                tc_commit_pair(smem_u32(&bars->empty[st]));
+                                if (kb + h == last) tc_commit_pair(smem_u32(&bars->acc_full[acc]));
+                            } else {
+                                tc_commit(smem_u32(&bars->empty[st]));
+                                if (kb + h == last) tc_commit(smem_u32(&bars->acc_full[acc]));
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    stage += FG;
+                    if (stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+        }
+    }
+    } else {
+        // ---- epilogue: a warp has 32 rows and half of the tile's columns, a thread one row of them
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPILOGUE));
+        const int q = warp & 3, half = (warp - EPI_BASE) >> 2;
+        float alpha = (p.s[0] ? __ldg(p.s[0]) : 1.0f) * (p.s[1] ? __ldg(p.s[1]) : 1.0f);
+        if (MODE == MODE_STATS || MODE == MODE_DZ) alpha *= LOG2E;
+        const float dz_scale = MODE == MODE_DZ && p.dz_scale ? __ldg(p.dz_scale) : 1.0f;
+        const uint32_t box = ring + RING_BYTES + (uint32_t)(warp - EPI_BASE) * BOX_BYTES;
+        const uint32_t box_row = box + lane * 128;
+        const uint64_t out_policy = MODE == MODE_DZ ? policy_evict_last() : policy_evict_first();      // dz is read next
+        bool ok = true;
+        int it = 0;
+        float v[NC];
+        for (int t = worker; t < tiles && ok; t += workers) {
+            int tm, tn;
+            const int slice = t / plane_tiles;
+            tile_at(t - slice * plane_tiles, p.tiles_m, p.tiles_n, tm, tn);
+            const int kb0 = slice * p.slice_blocks, kn = min(p.slice_blocks, k_blocks - kb0);
+            const int kn_pad = (kn + FG - 1) / FG * FG;
+            const int64_t row0 = ((int64_t)tm * CG + rank) * ROWS + q * 32, row = row0 + lane;
+            const int64_t col0 = (int64_t)tn * BN + half * NC;                 // first column of this warp
+            const bool row_ok = row < p.M;
+            const int cols = (int)max((int64_t)0, min((int64_t)NC, p.N - col0));
+            int rel = -1;                                         // the target's column among this thread's, if it is there
+            bool counted = false;
+            float g = 0.0f, lse2 = 0.0f;
+            if ((MODE == MODE_STATS || MODE == MODE_DZ) && row_ok) {
+                const int64_t target = __ldg(p.target + row), at = target - p.first - col0;
+                counted = target >= 0 && target < p.vocab;
+                if (at >= 0 && at < cols) rel = (int)at;
+                if (MODE == MODE_DZ) {
+                    g = __ldg(p.dloss + row) * dz_scale;
+                    lse2 = __ldg(p.lse + row) * LOG2E;
+                }
+            }
+            for (int kc = 0; kc < kn_pad && ok; kc += SPLIT, ++it) {
+                const uint32_t acc = (uint32_t)it & 1u;
+                ok = mbar_wait(smem_u32(&bars->acc_full[acc]), ((uint32_t)it >> 1) & 1u, abort_flag, L_WAIT_ACC_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q * 32) << 16) + half * NC;
+                const bool more = kc != 0;
+#pragma unroll
+                for (int c = 0; c < NC; c += 64) {                // two loads in flight, one wait for both
+                    uint32_t r[2][32];
+                    tc_ld32(taddr + c, r[0]);
+                    tc_ld32(taddr + c + 32, r[1]);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) v[c + i] = (more ? v[c + i] : 0.0f) + __uint_as_float(r[i >> 5][i & 31]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 2) mbar_arrive_cluster(map_to_cta(smem_u32(&bars->acc_empty[acc]), 0));
+                    else         mbar_arrive(smem_u32(&bars->acc_empty[acc]));
+                }
+            }
+            if (!ok) break;
+            if (MODE == MODE_STATS) {
+                if (row0 >= p.M) continue;                        // the whole warp
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    v[i] *= alpha;
+                    if (i >= cols) v[i] = -INFINITY;
+                    top = fmaxf(top, v[i]);
+                }
+                if (__any_sync(0xFFFFFFFFu, rel >= 0)) {
+                    float z = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) z = i == rel ? v[i] : z;
+                    if (rel >= 0) p.logit[row] = z;
+                }
+                // a row of minus infinities keeps a sum of zero; a NaN or plus infinity makes the sum NaN
+                const float shift = top == -INFINITY ? 0.0f : top;
+                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < NC; ++i) s[i & 3] += exp2_fast(v[i] - shift);
+                if (row_ok) p.part[(int64_t)(2 * tn + half) * p.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+                continue;
+            }
+            constexpr int OSZ = MODE == MODE_DZ ? ESZ : MODE == MODE_BF16 ? 2 : 4;
+            constexpr int BOX_COLS = 128 / OSZ, SUBS = BOX_COLS / 32, WORDS = 8 * OSZ;
+#pragma unroll
+            for (int c = 0; c < NC; c += BOX_COLS) {
+                const int64_t col = col0 + c;
+                // A box over the right edge is clipped by the TMA unit in units of 16 bytes: where rows end elsewhere, plain
+                // stores write it.  dz and the planes of dx have rows of whole boxes.
+                const bool by_hand = (MODE == MODE_BF16 || MODE == MODE_F32) && p.ragged && col + BOX_COLS > p.N;
+                if (!by_hand) {
+                    if (lane == 0) bulk_wait_read<0>();
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int sub = 0; sub < SUBS; ++sub) {
+                    float y[32];
+                    uint32_t w[WORDS];
+                    const int base = c + sub * 32;
+                    if (MODE == MODE_DZ) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] = exp2_fast(fmaf(v[base + i], alpha, -lse2));
+                        if (__any_sync(0xFFFFFFFFu, rel >= base && rel < base + 32)) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[i] -= base + i == rel ? 1.0f : 0.0f;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] *= g;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] = v[base + i] * alpha;
+                    }
+                    if (OSZ == 4) {
+#pragma unroll
+                        for (int i = 0; i < WORDS; ++i) w[i] = __float_as_uint(y[i % 32]);
+                    } else if (OSZ == 2) {
+#pragma unroll
+                        for (int i = 0; i < WORDS; ++i) w[i] = pack_bf16(y[2 * i % 32], y[(2 * i + 1) % 32]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < WORDS; ++i) w[i] = cvt_quad<kE5M2>(y[4 * i % 32], y[(4 * i + 1) % 32], y[(4 * i + 2) % 32], y[(4 * i + 3) % 32]);
+                    }
+                    if (MODE == MODE_DZ && !counted) {            // whatever its logits are
+#pragma unroll
+                        for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+                    }
+                    if (by_hand) {
+                        if (row_ok) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                if (col + sub * 32 + i >= p.N) continue;
+                                const int64_t at = row * p.ldd + col + sub * 32 + i;
+                                if (OSZ == 4) reinterpret_cast<uint32_t*>(p.D)[at] = w[i % WORDS];
+                                else          reinterpret_cast<uint16_t*>(p.D)[at] = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < WORDS / 4; ++j) {
+                            const int pos = sub * (WORDS / 4) + j;
+                            st_shared_v4(box_row + ((pos ^ (lane & 7)) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                        }
+                    }
+                }
+                if (by_hand) continue;
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (row0 < p.M && col < p.N) {
+                        if (MODE == MODE_ADD) tma_add_3d(&map_d, box, (int)col, (int)row0, slice);
+                        else                  tma_store_3d(&map_d, box, (int)(col * OSZ), (int)row0, slice, out_policy);
+                    }
+                    bulk_commit();
+                }
+            }
+        }
+        if (MODE != MODE_STATS && lane == 0) bulk_wait_all();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync_all();        // neither CTA leaves while the other may still touch its memory, barriers or TMEM
+    if (warp == 1) {
+        tc_fence_after();
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+        else         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+// Joins the pairs of 32 rows: lane = row, the warps take every 32nd pair, then a warp joins what the warps have of a row.
+__global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const float* logit, int64_t parts, int64_t M,
+                                                    const int64_t* target, int64_t vocab, float* loss, float* lse) {
+    __shared__ float2 got[32][33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    auto join = [](float2 a, float2 b) {
+        const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
+        return make_float2(top, a.y * exp2_fast(a.x - shift) + b.y * exp2_fast(b.x - shift));
+    };
+    const int64_t mine = (int64_t)blockIdx.x * 32 + lane;
+    float2 sum = make_float2(-INFINITY, 0.0f);
+    if (mine < M) {
+        for (int64_t i0 = warp; i0 < parts; i0 += 32 * 8) {
+            float2 w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = i0 + 32 * j < parts ? part[(i0 + 32 * j) * M + mine] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = join(sum, w[j]);
+        }
+    }
+    got[warp][lane] = sum;
+    __syncthreads();
+    sum = got[lane][warp];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const float2 other = make_float2(__shfl_xor_sync(0xFFFFFFFFu, sum.x, d), __shfl_xor_sync(0xFFFFFFFFu, sum.y, d));
+        sum = join(sum, other);
+    }
+    const int64_t row = (int64_t)blockIdx.x * 32 + warp;
+    if (lane == 0 && row < M) {
+        const float l2 = sum.x + log2f(sum.y);
+        const int64_t t = target[row];
+        lse[row] = l2 * LN2;
+        loss[row] = t >= 0 && t < vocab ? (l2 - logit[row]) * LN2 : 0.0f;
+    }
+}
+
+// The scale of dz's codes: |dz| is at most |dloss| of a counted token.  out[0] = scale, out[1] = 1 / scale.
+__global__ void __launch_bounds__(1024) k_dz_scale(const float* dloss, const int64_t* target, int64_t M, int64_t vocab, float* out) {
+    __shared__ uint32_t most[32];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    uint32_t bits = 0u;
+    for (int64_t i = threadIdx.x; i < M; i += 1024) {
+        const int64_t t = target[i];
+        if (t >= 0 && t < vocab) bits = max(bits, canonical_nan_bits(__float_as_uint(dloss[i]) & 0x7FFFFFFFu));
+    }
+    bits = warp_max_u32(bits);
+    if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = bits;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const float a = __uint_as_float(warp_max_u32(most[threadIdx.x]));
+        if (threadIdx.x == 0) {
+            float s = 1.0f;
+            if (a > 0.0f && a <= 3.402823466e38f) s = fminf(57344.0f / a, 3.402823466e38f);
+            out[0] = s;
+            out[1] = 1.0f / s;
+        }
+    }
+}
+
+// dx from its binary32 planes, added in order.
+template <bool BF16>
+__global__ void __launch_bounds__(256) k_sum_planes(const float* planes, int count, int64_t M, int64_t N, int64_t pitch, void* out, int64_t ldo) {
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int64_t octets = (N + 7) / 8, total = M * octets;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / octets, col = (i - row * octets) * 8;
+        const float* at = planes + row * pitch + col;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        for (int s = 0; s < count; ++s, at += M * pitch) {
+            const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 4);
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        }
+        if (col + 8 <= N) {
+            if (BF16) {
+                *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(out) + row * ldo + col) =
+                    make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            } else {
+                float* o = reinterpret_cast<float*>(out) + row * ldo + col;
+                *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (col + j >= N) continue;
+                if (BF16) reinterpret_cast<uint16_t*>(out)[row * ldo + col + j] = (uint16_t)pack_bf16(v[j], 0.0f);
+                else      reinterpret_cast<float*>(out)[row * ldo + col + j] = v[j];
+            }
+        }
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+static int64_t round_up(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
+
+struct Operand {
+    const void* p;
+    int64_t ld;                         // elements
+    bool mn;
+};
+
+template <int ESZ, int CG, int BN, int MODE>
+static fp8_status launch(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& md, const Params& p, int64_t tiles, cudaStream_t st) {
+    auto k = k_vocabulary<ESZ, CG, BN, MODE>;
+    constexpr int MAX_DEVICES = 64;
+    static std::mutex mu;
+    static int cached_workers[MAX_DEVICES] = {0};                 // 0 = not looked up yet
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    int dev = 0, workers = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return FP8_ERR_CUDA;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (dev >= 0 && dev < MAX_DEVICES) workers = cached_workers[dev];
+        if (workers == 0) {
+            if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES) != cudaSuccess) return FP8_ERR_CUDA;
+            workers = sm_count() / CG;
+            if (CG == 2) {
+                cfg.gridDim = dim3(2 * workers);
+                int clusters = 0;
+                if (cudaOccupancyMaxActiveClusters(&clusters, k, &cfg) == cudaSuccess && clusters > 0 && clusters < workers) workers = clusters;
+            }
+            if (dev >= 0 && dev < MAX_DEVICES) cached_workers[dev] = workers;
+        }
+    }
+    if ((int64_t)workers > tiles) workers = (int)tiles;
+    cfg.gridDim = dim3(workers * CG);
+    if (cudaLaunchKernelEx(&cfg, k, ma, mb, md, p) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
+    count_launches(1);
+    return launch_status();
+}
+
+// Output planes of a product: bytes for stores, binary32 elements for additions (the unit adds what the map's type says).
+static bool make_plane_map(CUtensorMap* map, void* base, int64_t cols, int64_t rows, int64_t ld, int planes, int osz, bool add) {
+    if (!add) return make_map(map, base, (uint64_t)(cols * osz), (uint64_t)rows, (uint64_t)(ld * osz), (uint64_t)planes, (uint64_t)(ld * osz * rows), 128, 32);
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)ld * 4, (cuuint64_t)(ld * 4 * rows)};
+    const cuuint32_t box[3] = {32, 32, 1}, step[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Columns of a tile for products with at most 128 rows (one CTA per tile): 256, or 128 where fewer rounds of the SMs are
+// needed for the same columns.
+static int few_rows_width(int64_t N) {
+    const int64_t sms = sm_count();
+    const int64_t wide = ((N + 255) / 256 + sms - 1) / sms * 256, narrow = ((N + 127) / 128 + sms - 1) / sms * 128;
+    return narrow < wide ? 128 : 256;
+}
+
+// One product of the kernel above: p holds M, N, K, the factors, the output and what its mode reads.
+template <int MODE>
+static fp8_status product(int esz, int fa, int fb, const Operand& A, const Operand& B, int64_t out_cols, int out_size, Params p, cudaStream_t st) {
+    const int cg = p.M > ROWS ? 2 : 1;
+    const int bn = MODE == MODE_STATS && cg == 1 ? few_rows_width(p.N) : 256;
+    const int ke = K_BYTES / esz;
+    CUtensorMap ma, mb, md;
+    auto map = [&](CUtensorMap* m, const Operand& o, int64_t mn, uint32_t rows) {
+        return o.mn ? make_map(m, o.p, (uint64_t)(mn * esz), (uint64_t)p.K, (uint64_t)(o.ld * esz), 1, 0, 128, (uint32_t)ke)
+                    : make_map(m, o.p, (uint64_t)(p.K * esz), (uint64_t)mn, (uint64_t)(o.ld * esz), 1, 0, K_BYTES, rows);
+    };
+    if (!map(&ma, A, p.M, ROWS) || !map(&mb, B, p.N, (uint32_t)(bn / cg))) return FP8_ERR_CUDA;
+    if (MODE == MODE_STATS) md = ma;                              // not used
+    else if (!make_plane_map(&md, p.D, out_cols, p.M, p.ldd, p.slices, out_size, MODE == MODE_ADD)) return FP8_ERR_CUDA;
+    p.ragged = (out_cols * out_size & 15) != 0 ? 1 : 0;
+    p.a_mn = A.mn ? 1 : 0;
+    p.b_mn = B.mn ? 1 : 0;
+    p.tiles_m = (int)((p.M + ROWS * cg - 1) / (ROWS * cg));
+    p.tiles_n = (int)((p.N + bn - 1) / bn);
+    const int64_t blocks = (p.K + ke - 1) / ke;
+    p.slice_blocks = (int)((blocks + p.slices - 1) / p.slices);
+    p.slices = (int)((blocks + p.slice_blocks - 1) / p.slice_blocks);
+    // binary32 accumulator; formats (bf16 is 1), layouts, N / 8, M / 16
+    p.idesc = (1u << 4) | ((uint32_t)(esz == 2 ? 1 : fa) << 7) | ((uint32_t)(esz == 2 ? 1 : fb) << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
+              ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(ROWS * cg >> 4) << 24);
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.slices;
+    if (cg == 2) return esz == 1 ? launch<1, 2, 256, MODE>(ma, mb, md, p, tiles, st) : launch<2, 2, 256, MODE>(ma, mb, md, p, tiles, st);
+    if constexpr (MODE == MODE_STATS) {
+        if (bn == 128) return esz == 1 ? launch<1, 1, 128, MODE>(ma, mb, md, p, tiles, st) : launch<2, 1, 128, MODE>(ma, mb, md, p, tiles, st);
+    }
+    return esz == 1 ? launch<1, 1, 256, MODE>(ma, mb, md, p, tiles, st) : launch<2, 1, 256, MODE>(ma, mb, md, p, tiles, st);
+}
+
+template <typename... KArgs, typename... Args>
+static fp8_status launch_small(void (*k)(KArgs...), unsigned grid, unsigned block, cudaStream_t st, Args... args) {
+    if (launch_programmatic(k, dim3(grid), dim3(block), st, args...) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
+    count_launches(1);
+    return launch_status();
+}
+
+// How the backward pass cuts its work.
+struct Cut {
+    int64_t cols;                       // vocabulary columns of a piece (the last may have fewer)
+    int pieces;
+    int slices;                         // K-slices of dx's product
+    bool planes;                        // dx goes through binary32 planes
+    int64_t pitch_z, pitch_x;           // of dz and of the planes, elements
+    size_t z_bytes, x_bytes;
+};
+
+constexpr int64_t Z_BYTES = 64 << 20;   // dz of a piece: half of L2, so that the two products that read it find it there
+constexpr int64_t LEAST_COLS = 8192;    // but no fewer columns: dx's planes are read and written once per piece
+
+static Cut cut_of(int64_t T, int64_t K, int64_t V, int esz) {
+    Cut c;
+    int64_t most = Z_BYTES / (T * esz);
+    if (most < LEAST_COLS) most = LEAST_COLS;
+    c.pieces = (int)((V + most - 1) / most);
+    c.cols = round_up((V + c.pieces - 1) / c.pieces, 256);
+    c.pieces = (int)((V + c.cols - 1) / c.cols);
+    // few rows: dx has few tiles and a long contraction, cut so that the SMs have a tile each
+    const int cg = T > ROWS ? 2 : 1;
+    const int64_t tiles = (T + ROWS * cg - 1) / (ROWS * cg) * ((K + 255) / 256), workers = sm_count() / cg;
+    int64_t slices = workers / (tiles > 0 ? tiles : 1);
+    const int64_t longest = c.cols / 1024;                        // a slice has at least 1024 of K
+    if (slices > longest) slices = longest;
+    if (slices > 16) slices = 16;
+    const int64_t ke = K_BYTES / esz, blocks = ((V < c.cols ? V : c.cols) + ke - 1) / ke;
+    const int64_t each = (blocks + (slices < 1 ? 1 : slices) - 1) / (slices < 1 ? 1 : slices);
+    c.slices = (int)((blocks + each - 1) / each);                 // as `product` counts them for the first piece, which writes every plane
+    c.planes = c.slices > 1 || c.pieces > 1;
+    c.pitch_z = c.cols;
+    c.pitch_x = round_up(K, 32);
+    c.z_bytes = (size_t)round_up(T * c.pitch_z * esz, 256);
+    c.x_bytes = c.planes ? (size_t)c.slices * (size_t)T * (size_t)c.pitch_x * 4 : 0;
+    return c;
+}
+
+static int64_t parts_of(int64_t T, int64_t V) { return 2 * ((V + 127) / 128); }      // of either tile width
+static size_t forward_bytes(int64_t T, int64_t V) { return T > 0 ? (size_t)parts_of(T, V) * (size_t)T * 8 + (size_t)T * 4 : 0; }
+static size_t backward_bytes(int64_t T, int64_t K, int64_t V, int esz) {
+    if (T <= 0) return 0;
+    const Cut c = cut_of(T, K, V, esz);
+    return 256 + c.z_bytes + c.x_bytes;
+}
+
+static fp8_status check(const fp8_cross_entropy_desc* d) {
+    if (!d) return FP8_ERR_NULL;
+    if (d->x_t < FP8_OPERAND_E4M3 || d->x_t > FP8_OPERAND_BF16 || d->w_t < FP8_OPERAND_E4M3 || d->w_t > FP8_OPERAND_BF16 ||
+        (d->x_t == FP8_OPERAND_BF16) != (d->w_t == FP8_OPERAND_BF16))
+        return FP8_ERR_ENUM;
+    if (d->tokens < 0 || d->width < 1 || d->vocab < 1) return FP8_ERR_SHAPE;
+    const int64_t far = ((int64_t)1 << 30) - 512;                 // 32-bit coordinates in bytes
+    if (d->tokens > far || d->width > far / 2 || d->vocab > far) return FP8_ERR_UNSUPPORTED;
+    const int64_t tiles = ((d->tokens + 127) / 128) * ((d->vocab + 127) / 128), across = ((d->width + 255) / 256);
+    if (tiles > (int64_t)1 << 29 || ((d->vocab + 127) / 128) * across > (int64_t)1 << 29 || ((d->tokens + 127) / 128) * across > (int64_t)1 << 25)
+        return FP8_ERR_UNSUPPORTED;
+    return FP8_OK;
+}
+
+static fp8_status check_operands(const fp8_cross_entropy_desc* d, const void* x, const void* w, const float* sx, const float* sw) {
+    const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
+    if (!x || !w || (esz == 1 && (!sx || !sw))) return FP8_ERR_NULL;
+    if (d->ldx < d->width || d->ldw < d->width) return FP8_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(x) & 15u) || (reinterpret_cast<uintptr_t>(w) & 15u) || ((d->ldx * esz) & 15) || ((d->ldw * esz) & 15)) return FP8_ERR_ALIGN;
+    return FP8_OK;
+}
+
+}  // namespace loss
+
+void loss_read_clear_latch(unsigned int out2[2]) {
+    out2[0] = out2[1] = 0u;
+    if (cudaMemcpyFromSymbol(out2, g_async_latch, 2 * sizeof(unsigned int)) != cudaSuccess || out2[0] == 0u) return;
+    const unsigned int zero[2] = {0u, 0u};
+    (void)cudaMemcpyToSymbol(g_async_latch, zero, sizeof(zero));
+}
+
+}  // namespace fp8b200
+
+using namespace fp8b200;
+
+extern "C" {
+
+fp8_status fp8_cross_entropy_workspace_bytes(const fp8_cross_entropy_desc* d, size_t* forward_bytes_out, size_t* backward_bytes_out) {
+    using namespace fp8b200::loss;
+    const fp8_status rc = check(d);
+    if (rc != FP8_OK) return rc;
+    if (forward_bytes_out) *forward_bytes_out = forward_bytes(d->tokens, d->vocab);
+    if (backward_bytes_out) *backward_bytes_out = backward_bytes(d->tokens, d->width, d->vocab, d->x_t == FP8_OPERAND_BF16 ? 2 : 1);
+    return FP8_OK;
+}
+
+fp8_status fp8_cross_entropy(const fp8_cross_entropy_desc* d, const void* x, const void* w, const float* scale_inv_x_dev, const float* scale_inv_w_dev,
+                             const int64_t* target_dev, float* loss_dev, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    using namespace fp8b200::loss;
+    fp8_status rc = check(d);
+    if (rc != FP8_OK) return rc;
+    const int64_t T = d->tokens, V = d->vocab;
+    if (T == 0) return FP8_OK;
+    if (!target_dev || !loss_dev || !lse_dev || !workspace_dev) return FP8_ERR_NULL;
+    if ((rc = check_operands(d, x, w, scale_inv_x_dev, scale_inv_w_dev)) != FP8_OK) return rc;
+    if (workspace_bytes < forward_bytes(T, V)) return FP8_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) return FP8_ERR_ALIGN;
+    cudaStream_t st = (cudaStream_t)stream;
+    const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
+    Params p = {};
+    p.M = T; p.N = V; p.K = d->width;
+    p.s[0] = scale_inv_x_dev; p.s[1] = scale_inv_w_dev;
+    p.slices = 1;
+    p.target = target_dev; p.vocab = V;
+    p.part = reinterpret_cast<float2*>(workspace_dev);
+    p.logit = reinterpret_cast<float*>(p.part + parts_of(T, V) * T);
+    const int bn = T > ROWS ? 256 : few_rows_width(V);
+    if ((rc = product<MODE_STATS>(esz, d->x_t, d->w_t, Operand{x, d->ldx, false}, Operand{w, d->ldw, false}, 0, 0, p, st)) != FP8_OK) return rc;
+    return launch_small(k_loss_join, (unsigned)((T + 31) / 32), 1024u, st, (const float2*)p.part, (const float*)p.logit, 2 * ((V + bn - 1) / bn), T, target_dev, V,
+                        loss_dev, lse_dev);
+}
+
+fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const void* x, const void* w, const float* scale_inv_x_dev, const float* scale_inv_w_dev,
+                                      const int64_t* target_dev, const float* lse_dev, const float* dloss_dev, void* dx, fp8_wide dx_t, int64_t lddx,
+                                      void* dw, fp8_wide dw_t, int64_t lddw, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    using namespace fp8b200::loss;
+    fp8_status rc = check(d);
+    if (rc != FP8_OK) return rc;
+    if ((dx_t != FP8_F32 && dx_t != FP8_BF16) || (dw_t != FP8_F32 && dw_t != FP8_BF16)) return FP8_ERR_ENUM;
+    const int64_t T = d->tokens, K = d->width, V = d->vocab;
+    const int xo = dx_t == FP8_BF16 ? 2 : 4, wo = dw_t == FP8_BF16 ? 2 : 4;
+    if (dw) {
+        if (lddw < K) return FP8_ERR_SHAPE;
+        if ((reinterpret_cast<uintptr_t>(dw) & 15u) || ((lddw * wo) & 15)) return FP8_ERR_ALIGN;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    if (T == 0) {                                                 // an empty sum
+        if (!dw) return FP8_OK;
+        if (cudaMemset2DAsync(dw, (size_t)(lddw * wo), 0, (size_t)(K * wo), (size_t)V, st) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
+        count_launches(1);
+        return FP8_OK;
+    }
+    if (dx) {
+        if (lddx < K) return FP8_ERR_SHAPE;
+        if ((reinterpret_cast<uintptr_t>(dx) & 15u) || ((lddx * xo) & 15)) return FP8_ERR_ALIGN;
+    }
+    if (!target_dev || !lse_dev || !dloss_dev || !workspace_dev) return FP8_ERR_NULL;
+    if ((rc = check_operands(d, x, w, scale_inv_x_dev, scale_inv_w_dev)) != FP8_OK) return rc;
+    const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
+    if (workspace_bytes < backward_bytes(T, K, V, esz)) return FP8_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) return FP8_ERR_ALIGN;
+    if (!dx && !dw) return FP8_OK;
+    const Cut c = cut_of(T, K, V, esz);
+    uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
+    float* scale = reinterpret_cast<float*>(ws);
+    void* dz = ws + 256;
+    float* planes = reinterpret_cast<float*>(ws + 256 + c.z_bytes);
+    if (esz == 1 && (rc = launch_small(k_dz_scale, 1u, 1024u, st, dloss_dev, target_dev, T, V, scale)) != FP8_OK) return rc;
+    const float* back = esz == 1 ? scale + 1 : nullptr;
+    const int fz = FP8_E5M2;
+    for (int i = 0; i < c.pieces; ++i) {
+        const int64_t v0 = i * c.cols, cols = V - v0 < c.cols ? V - v0 : c.cols;
+        const uint8_t* wp = reinterpret_cast<const uint8_t*>(w) + v0 * d->ldw * esz;
+        Params z = {};
+        z.M = T; z.N = cols; z.K = K;
+        z.s[0] = scale_inv_x_dev; z.s[1] = scale_inv_w_dev;
+        z.slices = 1;
+        z.D = dz; z.ldd = c.pitch_z;
+        z.target = target_dev; z.first = v0; z.vocab = V;
+        z.lse = lse_dev; z.dloss = dloss_dev; z.dz_scale = esz == 1 ? scale : nullptr;
+        if ((rc = product<MODE_DZ>(esz, d->x_t, d->w_t, Operand{x, d->ldx, false}, Operand{wp, d->ldw, false}, c.pitch_z, esz, z, st)) != FP8_OK) return rc;
+        if (dx) {
+            Params p = {};
+            p.M = T; p.N = K; p.K = cols;
+            p.s[0] = back; p.s[1] = scale_inv_w_dev;
+            const Operand A{dz, c.pitch_z, false}, B{wp, d->ldw, true};
+            if (c.planes) {
+                p.slices = c.slices;
+                p.D = planes; p.ldd = c.pitch_x;
+                rc = i == 0 ? product<MODE_F32>(esz, fz, d->w_t, A, B, c.pitch_x, 4, p, st) : product<MODE_ADD>(esz, fz, d->w_t, A, B, c.pitch_x, 4, p, st);
+            } else {
+                p.slices = 1;
+                p.D = dx; p.ldd = lddx;
+                rc = dx_t == FP8_BF16 ? product<MODE_BF16>(esz, fz, d->w_t, A, B, K, 2, p, st) : product<MODE_F32>(esz, fz, d->w_t, A, B, K, 4, p, st);
+            }
+            if (rc != FP8_OK) return rc;
+        }
+        if (dw) {
+            Params p = {};
+            p.M = cols; p.N = K; p.K = T;
+            p.s[0] = back; p.s[1] = scale_inv_x_dev;
+            p.slices = 1;
+            p.D = reinterpret_cast<uint8_t*>(dw) + v0 * lddw * wo; p.ldd = lddw;
+            const Operand A{dz, c.pitch_z, true}, B{x, d->ldx, true};
+            rc = dw_t == FP8_BF16 ? product<MODE_BF16>(esz, fz, d->x_t, A, B, K, 2, p, st) : product<MODE_F32>(esz, fz, d->x_t, A, B, K, 4, p, st);
+            if (rc != FP8_OK) return rc;
+        }
+    }
+    if (dx && c.planes) {
+        const int64_t octets = T * ((K + 7) / 8);
+        int64_t grid = (octets + 255) / 256;
+        if (grid > (int64_t)sm_count() * 16) grid = (int64_t)sm_count() * 16;
+        rc = dx_t == FP8_BF16 ? launch_small(k_sum_planes<true>, (unsigned)grid, 256u, st, (const float*)planes, c.slices, T, K, c.pitch_x, dx, lddx)
+                              : launch_small(k_sum_planes<false>, (unsigned)grid, 256u, st, (const float*)planes, c.slices, T, K, c.pitch_x, dx, lddx);
+    }
+    return rc;
+}
+
+}  // extern "C"
