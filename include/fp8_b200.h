@@ -486,6 +486,72 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
                          float* norm_dev, void* stream);
 
 /*
+ * AdamW over many tensors — Section 4.1 trains with the optimisers of the higher-precision baselines; parameters, gradients and
+ * the arithmetic stay wide, the copy that the next step's products read is FP8.  One launch over a plan, like fp8_grad_clip:
+ *   coef = norm <= max_norm ? 1 : max_norm / norm      (norm_dev NULL: 1),   g' = g * coef
+ *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in binary32 (square root and reciprocal by the hardware, 1 ulp), p rounded to nearest to p_t.
+ * A norm that is not finite skips the step: parameters, moments and the step counter stay as they are (the copies and their
+ * amax are written from the parameters as they are).  Without norm_dev a gradient that is not finite makes its element NaN.
+ *
+ * States.  FP8_STATE_F32: m and v are n floats.  FP8_STATE_E4M3: n codes each, in blocks of 256 consecutive elements with a
+ * scale each (m_scale, v_scale: ceil(n / 256) floats), value = code * scale, scale = the block's largest magnitude / 448:
+ *   m holds the first moment, rounded to nearest;
+ *   v holds the SQUARE ROOT of the second moment, rounded up or down with the probability of its distance (to nearest it would
+ *     stand still: with beta2 near 1 it moves less than half a step at a time); one that is not zero keeps at least code 1.
+ * The update of p uses the moments before they are rounded.  All zeros (codes and scales) is the state to start from.  A block
+ * in which a moment is not finite holds nothing finite afterwards.  The random numbers are 16 bits per element, a function of
+ * seed, t (both modulo 2^32 words of it) and the element's place in the plan: items are numbered one after the other, each from a
+ * multiple of 256.  The same plan, seed and t give the same bits.
+ *
+ * Copy (NULL: none): the new parameters as stored, in bf16, or as codes encode(p * copy_scale) with saturation, rules of
+ * fp8_quantize; copy_amax_dev (may be NULL; codes only) is OVERWRITTEN with amax of the new parameters, from which the next
+ * step's copy_scale is chosen.
+ *
+ * lr_dev, step_dev take the place of lr, step where they are given, so that a captured call goes on from step to step: step_dev
+ * counts the steps taken; the call uses t = *step_dev + 1 and adds one when it is done.
+ * Plans as those of fp8_grad_clip: made on the host, addresses and sizes must stay.  The workspace must hold zeros before its
+ * first use and is left zeroed; calls that may overlap need plans of their own.  Items need the alignment of their elements
+ * only (32 bytes for binary32, 16 for bf16 and 8 for codes are faster); no two overlap.
+ * beta1, beta2 in [0, 1), eps >= 0, step >= 1, max_norm >= 0 and weight_decay >= 0 finite, else FP8_ERR_UNSUPPORTED.
+ */
+typedef enum { FP8_STATE_F32 = 0, FP8_STATE_E4M3 = 1 } fp8_state;
+typedef struct {
+    const void* g;
+    void* p;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* copy;
+    const float* copy_scale_dev;
+    float* copy_amax_dev;
+    int64_t n;
+    float weight_decay;
+    fp8_wide g_t, p_t;
+    fp8_state state;
+    fp8_store copy_t;
+} fp8_adamw_item;
+typedef struct {
+    int64_t count, chunks, chunk, amaxes;
+    size_t table_bytes, workspace_bytes;
+} fp8_adamw_plan;
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    uint64_t seed;
+    const float* norm_dev;
+    const float* lr_dev;
+    int64_t* step_dev;
+    float max_norm;
+} fp8_adamw_options;
+
+fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_adamw_plan* plan);
+fp8_status fp8_adamw_plan_fill(const fp8_adamw_item* items, const fp8_adamw_plan* plan, void* table_host);
+fp8_status fp8_adamw_step(const fp8_adamw_plan* plan, const void* table_dev, void* workspace_dev, const fp8_adamw_options* o, void* stream);
+
+/*
  * Softmax cross entropy of a vocabulary projection — Sections 3.1 and 4.1: the loss that the language models are trained and
  * evaluated with (perplexity is its exponential), and the first gradient of their backward pass.  The logits never reach
  * memory: the vocabulary is gone through in pieces, forward and backward.

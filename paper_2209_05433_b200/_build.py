@@ -8,7 +8,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfp8_b200.so")
-SOURCES = ["cast.cu", "gemm.cu", "fused.cu", "grads.cu", "loss.cu"]
+SOURCES = ["cast.cu", "gemm.cu", "fused.cu", "grads.cu", "loss.cu", "adamw.cu"]
 HEADERS = ["common.cuh", "codec.cuh", "umma.cuh", "activation.cuh", "octet.cuh", os.path.join("..", "..", "include", "fp8_b200.h")]
 
 NVCC_FLAGS = [

@@ -32,6 +32,7 @@ EXPORTS = ["fp8_amax", "fp8_scale_from_amax", "fp8_quantize", "fp8_quantize_curr
            "fp8_gemm_epilogue", "fp8_gemm_gated", "fp8_gemm_gated_backward",
            "fp8_epilogue_backward", "fp8_epilogue_backward_workspace_bytes",
            "fp8_clip_plan_size", "fp8_clip_plan_fill", "fp8_grad_norm", "fp8_grad_clip",
+           "fp8_adamw_plan_size", "fp8_adamw_plan_fill", "fp8_adamw_step",
            "fp8_cross_entropy_workspace_bytes", "fp8_cross_entropy", "fp8_cross_entropy_backward",
            "fp8_async_status", "fp8_self_test_expire_wait", "fp8_sm_clock_probe", "fp8_status_string", "fp8_launch_count"]
 
@@ -81,6 +82,27 @@ class ClipSizes(ctypes.Structure):
     """fp8_clip_plan of the header"""
     _fields_ = [("count", ctypes.c_int64), ("chunks", ctypes.c_int64), ("table_bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t)]
 
+
+class AdamWItem(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("p", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("copy_scale", ctypes.c_void_p), ("copy_amax", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("g_t", ctypes.c_int), ("p_t", ctypes.c_int), ("state", ctypes.c_int),
+                ("copy_t", ctypes.c_int)]
+
+
+class AdamWSizes(ctypes.Structure):
+    """fp8_adamw_plan of the header"""
+    _fields_ = [("count", ctypes.c_int64), ("chunks", ctypes.c_int64), ("chunk", ctypes.c_int64), ("amaxes", ctypes.c_int64),
+                ("table_bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class AdamWOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int64),
+                ("seed", ctypes.c_uint64), ("norm", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p),
+                ("max_norm", ctypes.c_float)]
+
+
+_pack_adamw = struct.Struct("ddddqQPPPf4x").pack
 
 _lib = None
 
@@ -162,6 +184,12 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.fp8_grad_norm.argtypes = [ctypes.POINTER(ClipSizes), vp, vp, vp, vp]
     lib.fp8_grad_clip.restype = i32
     lib.fp8_grad_clip.argtypes = [ctypes.POINTER(ClipSizes), vp, vp, ctypes.c_float, vp, vp]
+    lib.fp8_adamw_plan_size.restype = i32
+    lib.fp8_adamw_plan_size.argtypes = [ctypes.POINTER(AdamWItem), i64, ctypes.POINTER(AdamWSizes)]
+    lib.fp8_adamw_plan_fill.restype = i32
+    lib.fp8_adamw_plan_fill.argtypes = [ctypes.POINTER(AdamWItem), ctypes.POINTER(AdamWSizes), vp]
+    lib.fp8_adamw_step.restype = i32
+    lib.fp8_adamw_step.argtypes = [ctypes.POINTER(AdamWSizes), vp, vp, vp, vp]
     lib.fp8_cross_entropy_workspace_bytes.restype = i32
     lib.fp8_cross_entropy_workspace_bytes.argtypes = [vp, ctypes.POINTER(sz), ctypes.POINTER(sz)]
     lib.fp8_cross_entropy.restype = i32
@@ -670,6 +698,96 @@ def _here(t: torch.Tensor, name: str) -> torch.Tensor:
     if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
         raise ValueError("%s must be a tensor of the current CUDA device" % name)
     return t
+
+
+STATE_BLOCK = 256            # elements of an 8-bit state that share a scale
+
+
+class AdamWPlan:
+    """The tensors that fp8_adamw_step goes over, laid out once, as ClipPlan does: lists of one length, each tensor contiguous
+    and once in the plan.
+
+    params, grads: float32 or bfloat16.  exp_avgs, exp_avg_sqs: float32, or uint8 codes (E4M3) with one float32 scale for every
+    256 elements in exp_avg_scales, exp_avg_sq_scales; exp_avg_sqs then holds the square root of the second moment.  All of them
+    start from zeros.  weight_decay: one number, or one per tensor.  copies (None, or None for some): bfloat16, or uint8 codes of
+    the format ``fmt`` made with the tensor's element of ``scales``; ``amax_outs`` (None, or None for some) receive the new
+    parameters' amax.  Lists of scales and amax_outs hold one-element tensors."""
+
+    def __init__(self, params: list[torch.Tensor], grads: list[torch.Tensor], exp_avgs: list[torch.Tensor], exp_avg_sqs: list[torch.Tensor],
+                 weight_decay=0.0, exp_avg_scales=None, exp_avg_sq_scales=None, copies=None, fmt: int | None = None, scales=None, amax_outs=None):
+        count = len(params)
+        none = [None] * count
+        columns = [list(params), list(grads), list(exp_avgs), list(exp_avg_sqs)]
+        columns += [none if c is None else list(c) for c in (exp_avg_scales, exp_avg_sq_scales, copies, scales, amax_outs)]
+        decays = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+        if any(len(c) != count for c in columns) or len(decays) != count:
+            raise ValueError("all lists must have one length")
+        self.tensors = columns                                # kept alive
+        device = params[0].device if count else torch.device("cuda", torch.cuda.current_device())
+        items = (AdamWItem * max(1, count))()
+        for it, p, g, m, v, ms, vs, copy, scale, amax, decay in zip(items, *columns, decays):
+            n = p.numel()
+            for t in (p, g, m, v, ms, vs, copy, scale, amax):
+                if t is not None and t.device != device:
+                    raise ValueError("all tensors must be on one device")
+            if g.numel() != n or m.numel() != n or v.numel() != n or (copy is not None and copy.numel() != n):
+                raise ValueError("gradient, moments and copy must have the size of their parameter")
+            it.p, it.p_t, it.g, it.g_t, it.n, it.weight_decay = _dev(p, "parameter"), _wide_of(p), _dev(g, "gradient"), _wide_of(g), n, decay
+            it.m, it.v = _dev(m, "exp_avg"), _dev(v, "exp_avg_sq")
+            if m.dtype != v.dtype or m.dtype not in (torch.float32, torch.uint8):
+                raise TypeError("both moments must be float32, or both uint8 codes")
+            if (m.dtype is torch.uint8) != (ms is not None) or (ms is None) != (vs is None):
+                raise TypeError("8-bit moments need their scales, and only they")
+            if ms is not None:
+                blocks = -(-n // STATE_BLOCK)
+                it.state, it.m_scale, it.v_scale = 1, _vec(ms, blocks, "exp_avg_scales"), _vec(vs, blocks, "exp_avg_sq_scales")
+            if copy is None:
+                if scale is not None or amax is not None:
+                    raise TypeError("scales and amax_outs go with a copy")
+                continue
+            it.copy = _dev(copy, "copy")
+            if copy.dtype is torch.uint8:
+                if fmt not in (E4M3, E5M2) or scale is None:
+                    raise TypeError("a uint8 copy needs its format, E4M3 or E5M2, and its scale")
+                it.copy_t, it.copy_scale = STORE_E4M3 + fmt, _scalar(scale, "scale")
+                it.copy_amax = None if amax is None else _scalar(amax, "amax_out")
+            elif copy.dtype is torch.bfloat16:
+                if scale is not None or amax is not None:
+                    raise TypeError("scales and amax_outs go with a uint8 copy")
+                it.copy_t = STORE_BF16
+            else:
+                raise TypeError("copies must be bfloat16, or uint8 codes")
+        self.sizes = AdamWSizes()
+        _check(load().fp8_adamw_plan_size(items, count, ctypes.byref(self.sizes)), "fp8_adamw_plan_size")
+        host = torch.zeros(max(16, self.sizes.table_bytes), dtype=torch.uint8)
+        _check(load().fp8_adamw_plan_fill(items, ctypes.byref(self.sizes), host.data_ptr()), "fp8_adamw_plan_fill")
+        # the copy from pageable memory returns when the stream has done it, and with it the zeros: any stream may use the plan
+        self.workspace = torch.zeros(self.sizes.workspace_bytes, dtype=torch.uint8, device=device)
+        self.table = host.to(device)
+        self.device = device
+        self._call = (ctypes.byref(self.sizes), self.table.data_ptr(), self.workspace.data_ptr())
+
+
+def fp8_adamw_step(plan: AdamWPlan, lr: float | torch.Tensor, step: int | torch.Tensor, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                   seed: int = 0, norm: torch.Tensor | None = None, max_norm: float | None = None) -> None:
+    """One AdamW step of the plan's tensors.  ``step`` counts from 1; a one-element int64 CUDA tensor holds the steps taken so far
+    instead, and is advanced.  ``lr`` may be a one-element float32 CUDA tensor.  With ``norm`` (what fp8_grad_norm wrote) gradients are
+    scaled by min(1, max_norm / norm), and a norm that is not finite skips the step.  ``seed`` is for 8-bit moments."""
+    if plan.device.index != torch._C._cuda_getDevice():
+        raise ValueError("the plan's tensors must be on the current CUDA device")
+    if (norm is None) != (max_norm is None):
+        raise ValueError("norm and max_norm go together")
+    lr_ptr = step_ptr = norm_ptr = 0
+    if isinstance(lr, torch.Tensor):
+        lr_ptr, lr = _scalar(_here(lr, "lr"), "lr"), 0.0
+    if isinstance(step, torch.Tensor):
+        if step.dtype is not torch.int64 or step.numel() != 1:
+            raise TypeError("step must be an int or a one-element int64 CUDA tensor")
+        step_ptr, step = _here(step, "step").data_ptr(), 1
+    if norm is not None:
+        norm_ptr = _scalar(_here(norm, "norm"), "norm")
+    o = _pack_adamw(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, norm_ptr, lr_ptr, step_ptr, 0.0 if max_norm is None else max_norm)
+    _check(_lib.fp8_adamw_step(*plan._call, o, _stream()), "fp8_adamw_step")
 
 
 def _pitch_of(t: torch.Tensor) -> int:

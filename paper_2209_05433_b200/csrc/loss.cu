@@ -39,7 +39,10 @@ constexpr int MODE_ADD = 4;             // added to what is there, in binary32
 constexpr int ROWS = 128;               // rows of a CTA's tile (one TMEM lane each)
 constexpr int K_BYTES = 128;            // K-block: one 128-byte swizzle row, 128 elements of 8 bits or 64 of 16
 constexpr int K_STEP_BYTES = 32;        // K of one tcgen05.mma
-constexpr int SPLIT_BYTES = 2048;       // of K, in elements of either size: what one use of the accumulator covers
+// Of K, what one use of the accumulator covers.  The tensor core truncates what it adds, once per K_STEP_BYTES: a logit that
+// grows steadily loses up to that many steps times 2^-24 of itself.  bf16 products have more bits to lose and half the steps
+// per use, and their loss was off by 1.1e-6 with 2048 (start: 32-bit sums 7e-7).
+template <int ESZ> constexpr int split_of = ESZ == 1 ? 2048 : 512;
 constexpr int FG = 2;                   // K-blocks consumed per barrier wait
 constexpr int MAX_STAGES = 6;
 constexpr uint32_t A_BYTES = ROWS * K_BYTES;
@@ -115,7 +118,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     constexpr uint32_t STAGE_BYTES = A_BYTES + B_ROWS * K_BYTES;
     constexpr int STAGES = RING_BYTES / STAGE_BYTES;
     static_assert(STAGES % FG == 0 && STAGES <= MAX_STAGES, "ring depth");
-    constexpr int SPLIT = SPLIT_BYTES / KE;                       // K-blocks per use of an accumulator
+    constexpr int SPLIT = split_of<ESZ> / KE;                     // K-blocks per use of an accumulator
     constexpr int NC = BN / 2;                                    // columns of an epilogue thread
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
