@@ -93,17 +93,49 @@ __device__ __forceinline__ uint2 ld2(const void* p) {
     return v;
 }
 
-// Eight values from element i on; `count` of them exist (the others read as 0).
-template <bool BF16>
-__device__ __forceinline__ void load_wide(const void* base, int64_t i, int count, bool vectors, uint32_t (&w)[8]) {
-    if (vectors && count == 8) {
+// A lane's share of a block as it lies in memory.
+template <bool G_BF16, bool P_BF16, bool CODES> struct Raw {
+    static constexpr int STATE = CODES ? 2 : 8;
+    uint32_t g[8], p[8], m[STATE], v[STATE];
+    float ms, vs;
+
+    // i: the lane's first element, block: its block's index
+    __device__ __forceinline__ void fetch(const Entry& e, int64_t i, int64_t block) {
+        fetch_wide<P_BF16>(e.p, i, p);
+        fetch_wide<G_BF16>(e.g, i, g);
+        if (CODES) {
+            const uint2 a = ld2(reinterpret_cast<const uint8_t*>(e.m) + i), b = ld2(reinterpret_cast<const uint8_t*>(e.v) + i);
+            m[0] = a.x; m[1] = a.y; v[0] = b.x; v[1] = b.y;
+            ms = e.m_scale[block];
+            vs = e.v_scale[block];
+        } else {
+            fetch_wide<false>(e.m, i, *reinterpret_cast<uint32_t(*)[8]>(m));
+            fetch_wide<false>(e.v, i, *reinterpret_cast<uint32_t(*)[8]>(v));
+        }
+    }
+    // element by element; `count` of them exist, the others read as 0
+    __device__ __forceinline__ void fetch_some(const Entry& e, int64_t i, int64_t block, int count) {
+        some_wide<P_BF16>(e.p, i, count, p);
+        some_wide<G_BF16>(e.g, i, count, g);
+        if (CODES) {
+            some_codes(e.m, i, count, m);
+            some_codes(e.v, i, count, v);
+            ms = e.m_scale[block];
+            vs = e.v_scale[block];
+        } else {
+            some_wide<false>(e.m, i, count, *reinterpret_cast<uint32_t(*)[8]>(m));
+            some_wide<false>(e.v, i, count, *reinterpret_cast<uint32_t(*)[8]>(v));
+        }
+    }
+    template <bool BF16> static __device__ __forceinline__ void fetch_wide(const void* base, int64_t i, uint32_t (&w)[8]) {
         if (BF16) {
             const uint4 q = ld4(reinterpret_cast<const uint16_t*>(base) + i);
             w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
         } else {
             ld8(reinterpret_cast<const float*>(base) + i, w);
         }
-    } else {
+    }
+    template <bool BF16> static __device__ __forceinline__ void some_wide(const void* base, int64_t i, int count, uint32_t (&w)[8]) {
 #pragma unroll
         for (int j = 0; j < (BF16 ? 4 : 8); ++j) {
             if (BF16) {
@@ -114,53 +146,84 @@ __device__ __forceinline__ void load_wide(const void* base, int64_t i, int count
             }
         }
     }
-}
-template <bool BF16>
-__device__ __forceinline__ void values(const uint32_t (&w)[8], float (&v)[8]) {
+    static __device__ __forceinline__ void some_codes(const void* base, int64_t i, int count, uint32_t (&w)[STATE]) {
+        const uint8_t* at = reinterpret_cast<const uint8_t*>(base) + i;
+        w[0] = w[1] = 0u;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = BF16 ? __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16) : __uint_as_float(w[j]);
+        for (int j = 0; j < 8; ++j) w[j >> 2] |= j < count ? (uint32_t)at[j] << (8 * (j & 3)) : 0u;
+    }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void values(const uint32_t (&w)[8], Pair (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        v[j] = BF16 ? Pair(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u)) : Pair(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
 }
 template <bool BF16>
-__device__ __forceinline__ void store_wide(void* base, int64_t i, int count, bool vectors, const uint32_t (&w)[8]) {
-    if (vectors && count == 8) {
+__device__ __forceinline__ void store_wide(void* base, int64_t i, int count, const uint32_t (&w)[8]) {
+    if (count == 8) {
         if (BF16) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + i) = make_uint4(w[0], w[1], w[2], w[3]);
         else      st8(reinterpret_cast<float*>(base) + i, w);
-    } else {
+    } else {                                                // one by one
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (j >= count) continue;
+            if (j >= (count & 15)) continue;
             if (BF16) reinterpret_cast<uint16_t*>(base)[i + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
             else      reinterpret_cast<uint32_t*>(base)[i + j] = w[j];
         }
     }
 }
-__device__ __forceinline__ uint2 load_codes(const void* base, int64_t i, int count, bool vectors) {
-    const uint8_t* at = reinterpret_cast<const uint8_t*>(base) + i;
-    if (vectors && count == 8) return ld2(at);
-    uint64_t c = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) c |= j < count ? (uint64_t)at[j] << (8 * j) : 0ull;
-    return make_uint2((uint32_t)c, (uint32_t)(c >> 32));
-}
-__device__ __forceinline__ void store_codes(void* base, int64_t i, int count, bool vectors, uint2 c) {
+__device__ __forceinline__ void store_codes(void* base, int64_t i, int count, uint2 c) {
     uint8_t* at = reinterpret_cast<uint8_t*>(base) + i;
-    if (vectors && count == 8) {
+    if (count == 8) {
         *reinterpret_cast<uint2*>(at) = c;
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < count) at[j] = (uint8_t)((j < 4 ? c.x : c.y) >> (8 * (j & 3)));
+        for (int j = 0; j < 8; ++j)
+            if (j < (count & 15)) at[j] = (uint8_t)((j < 4 ? c.x : c.y) >> (8 * (j & 3)));
+    }
 }
-__device__ __forceinline__ void decode8(uint2 c, float scale, float (&v)[8]) {
-    const float2 a = decode_pair<kE4M3>(c.x & 0xFFFFu), b = decode_pair<kE4M3>(c.x >> 16), d = decode_pair<kE4M3>(c.y & 0xFFFFu), e = decode_pair<kE4M3>(c.y >> 16);
-    v[0] = a.x * scale; v[1] = a.y * scale; v[2] = b.x * scale; v[3] = b.y * scale;
-    v[4] = d.x * scale; v[5] = d.y * scale; v[6] = e.x * scale; v[7] = e.y * scale;
+__device__ __forceinline__ void decode8(const uint32_t* c, Pair scale, Pair (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 a = decode_pair<kE4M3>(j & 1 ? c[j >> 1] >> 16 : c[j >> 1] & 0xFFFFu);
+        v[j] = Pair(a.x, a.y) * scale;
+    }
 }
 __device__ __forceinline__ float root(float x) {             // 1 ulp
     float y;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float inverse_root(float x) {     // 2 ulp
+    float y;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Square roots rounded to nearest: the product x / sqrt(x) of the approximation is corrected by its residual over twice the
+// root, which the fused operation gives without error for x above 2^-100; below, and there alone, the last bit may differ.
+// An x that has overflowed gives the largest number, beside which every moment vanishes.
+__device__ __forceinline__ Pair root_nearest(Pair x) {
+    float a, b;
+    x.split(a, b);
+    const Pair q(inverse_root(fmaxf(a, 1.17549435e-38f)), inverse_root(fmaxf(b, 1.17549435e-38f)));
+    const Pair r = x * q;
+    float u, v;
+    r.split(u, v);
+    fma2(fma2(r, Pair(-u, -v), x), q * Pair(0.5f), r).split(a, b);
+    return Pair(fminf(a, 3.402823466e38f), fminf(b, 3.402823466e38f));
+}
+// The halves added one by one: as an addition of pairs it came out fused with the product before it.
+__device__ __forceinline__ Pair sum(Pair a, Pair b) {
+    float x, y, z, w;
+    a.split(x, y);
+    b.split(z, w);
+    return Pair(__fadd_rn(x, z), __fadd_rn(y, w));
+}
+__device__ __forceinline__ void split8(const Pair (&p)[4], float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j].split(v[2 * j], v[2 * j + 1]);
 }
 // largest magnitude of the warp's eight values each; NaN if any is NaN
 __device__ __forceinline__ float warp_most(const float (&v)[8]) {
@@ -171,11 +234,14 @@ __device__ __forceinline__ float to_448(float most) { return most == 0.0f ? 0.0f
 
 // Code of y in [0, 448] rounded up with the probability of its distance from the code below: floor(y / step + u) for 0 <= u < 1.
 // Above the smallest normal value (2^-6) the step is an eighth of the power of two below y, and 8 .. 16 steps make up y, so the
-// number of steps and the exponent add up to the code; below, the steps themselves are the code.
-__device__ __forceinline__ uint32_t encode_chance(float y, float u) {
-    const uint32_t e = max(__float_as_uint(y) >> 23, 121u);
-    const float steps = fmaf(y, __uint_as_float((257u - e) << 23), u);
-    return ((e - 121u) << 3) + (uint32_t)steps;
+// number of steps and the exponent add up to the code; below, the steps themselves are the code.  `chance`: 2^23 + 65536 u.
+// A y that is not zero gets at least code 1.
+__device__ __forceinline__ uint32_t encode_chance(float y, float chance) {
+    const uint32_t bits = __float_as_uint(y), e = max(bits & 0x7F800000u, 121u << 23);          // the power of two below y
+    const float u = fmaf(chance, 1.0f / 65536.0f, -128.0f);
+    const float steps = fmaf(y, __uint_as_float((257u << 23) - e), u);
+    const uint32_t whole = __float_as_uint(__fadd_rz(steps, 8388608.0f));                      // 2^23 + floor(steps)
+    return max((e >> 20) + whole - (121u * 8u + 0x4B000000u), min(bits, 1u));
 }
 
 struct Step {
@@ -184,107 +250,129 @@ struct Step {
     int skip;
 };
 
+// One block of 256 that is in registers: moments, parameters and what is stored.  i: the lane's first element; count: 8, or what
+// the element-wise stores take (16 for eight of them).  Returns the largest magnitude among the parameters, where there is a copy.
+template <bool G_BF16, bool P_BF16, bool CODES>
+__device__ __forceinline__ float update_block(const Params& a, const Entry& e, const Step& s, Raw<G_BF16, P_BF16, CODES>& w, int64_t i, int64_t block, int count,
+                                              float keep, float copy_scale) {
+    Pair p[4], g[4], m[4], v[4], r[4];
+    if (!s.skip) {
+        values<P_BF16>(w.p, p);
+        values<G_BF16>(w.g, g);
+        if (CODES) {
+            decode8(w.m, Pair(w.ms), m);
+            decode8(w.v, Pair(w.vs), r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = r[j] * r[j];
+        } else {
+            values<false>(*reinterpret_cast<uint32_t(*)[8]>(w.m), m);
+            values<false>(*reinterpret_cast<uint32_t(*)[8]>(w.v), v);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const Pair gj = g[j] * Pair(s.coef);
+            m[j] = sum(Pair(a.beta1) * m[j], Pair(a.rest1) * gj);
+            v[j] = sum(Pair(a.beta2) * v[j], Pair(a.rest2) * gj * gj);
+            float x, y;
+            if (CODES) {
+                r[j] = root_nearest(v[j]);
+            } else {
+                v[j].split(x, y);
+                r[j] = Pair(root(x), root(y));
+            }
+            fma2(r[j], Pair(s.root2), Pair(a.eps)).split(x, y);
+            p[j] = fma2(p[j], Pair(keep), Pair(-s.rate) * m[j] * Pair(reciprocal_fast(x), reciprocal_fast(y)));
+        }
+        float f[8];
+        if (CODES) {
+            split8(m, f);
+            const float m_most = warp_most(f);
+            const Pair m_up(to_448(m_most));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (m[j] * m_up).split(f[2 * j], f[2 * j + 1]);
+            store_codes(e.m, i, count, make_uint2(cvt_quad<kE4M3>(f[0], f[1], f[2], f[3]), cvt_quad<kE4M3>(f[4], f[5], f[6], f[7])));
+            split8(r, f);
+            const float r_most = warp_most(f);
+            const Pair r_up(to_448(r_most));
+            uint32_t c[8];
+            const uint32_t pair = (uint32_t)((uint64_t)(e.number + i) >> 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t word = mix((pair + j) * 0x9E3779B1u + s.key);
+                float x, y;
+                (r[j] * r_up).split(x, y);
+                c[2 * j] = encode_chance(fminf(x, 448.0f), __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7610)));
+                c[2 * j + 1] = encode_chance(fminf(y, 448.0f), __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7632)));
+            }
+            auto pack = [](uint32_t q, uint32_t t, uint32_t u, uint32_t o) { return __byte_perm(__byte_perm(q, t, 0x0040), __byte_perm(u, o, 0x0040), 0x5410); };
+            store_codes(e.v, i, count, make_uint2(pack(c[0], c[1], c[2], c[3]), pack(c[4], c[5], c[6], c[7])));
+            if ((threadIdx.x & 31) == 0) {
+                e.m_scale[block] = m_most * (1.0f / 448.0f);
+                e.v_scale[block] = r_most * (1.0f / 448.0f);
+            }
+        } else {
+            uint32_t t[8];
+            split8(m, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = __float_as_uint(f[j]);
+            store_wide<false>(e.m, i, count, t);
+            split8(v, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = __float_as_uint(f[j]);
+            store_wide<false>(e.v, i, count, t);
+        }
+        split8(p, f);
+        if (count < 8) {                                    // what is not there stays out of the amax, whatever eps is
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = j < count ? f[j] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!P_BF16) w.p[j] = __float_as_uint(f[j]);
+            else if ((j & 1) == 0) w.p[j >> 1] = pack_bf16(f[j], f[j + 1]);
+        }
+        store_wide<P_BF16>(e.p, i, count, w.p);
+    }
+    if (!e.has_copy) return 0.0f;
+    float f[8];                                             // of the parameters as stored
+    values<P_BF16>(w.p, p);
+    split8(p, f);
+    if (e.copy_t == FP8_STORE_BF16) {
+        uint32_t t[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) t[j >> 1] = pack_bf16(f[j], f[j + 1]);
+        store_wide<true>(e.copy, i, count, t);
+        return 0.0f;
+    }
+    const float top = most8(f);
+    store_codes(e.copy, i, count, e.copy_t == FP8_STORE_E4M3 ? encode8_as<kE4M3>(f, top, copy_scale, false) : encode8_as<kE5M2>(f, top, copy_scale, false));
+    return top;
+}
+
 template <bool G_BF16, bool P_BF16, bool CODES>
 __device__ __forceinline__ float update_chunk(const Params& a, const Entry& e, const Step& s, int64_t lo, int64_t n) {
-    const int lane = threadIdx.x & 31;
-    const bool vectors = e.vectors != 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float keep = fmaf(-s.lr, e.decay, 1.0f);
     const float copy_scale = e.copy_t >= FP8_STORE_E4M3 && e.has_copy ? __ldg(e.copy_scale) : 1.0f;
+    const int whole = e.vectors ? (int)(n / BLOCK) : 0, blocks = (int)((n + BLOCK - 1) / BLOCK);
+    const int64_t first = lo / BLOCK;                       // chunks are whole blocks
     float most = 0.0f;
-    for (int64_t b = (int64_t)(threadIdx.x >> 5) * BLOCK; b < n; b += WARPS * BLOCK) {
-        const int64_t i = lo + b + lane * 8;
-        const int count = (int)max((int64_t)0, min((int64_t)8, n - b - lane * 8));
-        uint32_t wg[8], wp[8], wm[8], wv[8];
-        uint2 cm, cv;
-        float ms = 0.0f, vs = 0.0f;
-        load_wide<P_BF16>(e.p, i, count, vectors, wp);
-        float p[8];
-        if (!s.skip) {
-            load_wide<G_BF16>(e.g, i, count, vectors, wg);
-            if (CODES) {
-                cm = load_codes(e.m, i, count, vectors);
-                cv = load_codes(e.v, i, count, vectors);
-                ms = e.m_scale[(lo + b) / BLOCK];
-                vs = e.v_scale[(lo + b) / BLOCK];
-            } else {
-                load_wide<false>(e.m, i, count, vectors, wm);
-                load_wide<false>(e.v, i, count, vectors, wv);
-            }
-            float g[8], m[8], v[8], r[8];
-            values<P_BF16>(wp, p);
-            values<G_BF16>(wg, g);
-            if (CODES) {
-                decode8(cm, ms, m);
-                decode8(cv, vs, r);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = r[j] * r[j];
-            } else {
-                values<false>(wm, m);
-                values<false>(wv, v);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float gj = g[j] * s.coef;
-                m[j] = __fadd_rn(__fmul_rn(a.beta1, m[j]), __fmul_rn(a.rest1, gj));
-                v[j] = __fadd_rn(__fmul_rn(a.beta2, v[j]), __fmul_rn(__fmul_rn(a.rest2, gj), gj));
-                r[j] = CODES ? __fsqrt_rn(v[j]) : root(v[j]);
-                p[j] = fmaf(p[j], keep, -s.rate * m[j] * reciprocal_fast(fmaf(r[j], s.root2, a.eps)));
-            }
-            if (count < 8) {                                // what is not there stays out of the amax, whatever eps is
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] = j < count ? p[j] : 0.0f;
-            }
-            if (CODES) {
-                const float m_most = warp_most(m), r_most = warp_most(r);
-                const float m_up = to_448(m_most), r_up = to_448(r_most);
-                float y[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = m[j] * m_up;
-                store_codes(e.m, i, count, vectors, make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7])));
-                uint32_t c[2] = {0u, 0u};
-                const uint32_t pair = (uint32_t)((uint64_t)(e.number + i) >> 1);
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    const uint32_t word = mix((pair + j / 2) * 0x9E3779B1u + s.key);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float u = __uint_as_float(0x3F800000u | (h ? word >> 16 << 7 : (word & 0xFFFFu) << 7)) - 1.0f;
-                        const uint32_t code = max(encode_chance(fminf(r[j + h] * r_up, 448.0f), u), r[j + h] > 0.0f ? 1u : 0u);
-                        c[j >> 2] |= code << (8 * ((j + h) & 3));
-                    }
-                }
-                store_codes(e.v, i, count, vectors, make_uint2(c[0], c[1]));
-                if (lane == 0) {
-                    e.m_scale[(lo + b) / BLOCK] = m_most * (1.0f / 448.0f);
-                    e.v_scale[(lo + b) / BLOCK] = r_most * (1.0f / 448.0f);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { wm[j] = __float_as_uint(m[j]); wv[j] = __float_as_uint(v[j]); }
-                store_wide<false>(e.m, i, count, vectors, wm);
-                store_wide<false>(e.v, i, count, vectors, wv);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (!P_BF16) wp[j] = __float_as_uint(p[j]);
-                else if ((j & 1) == 0) wp[j >> 1] = pack_bf16(p[j], p[j + 1]);
-            }
-            store_wide<P_BF16>(e.p, i, count, vectors, wp);
-        }
-        if (e.has_copy) {                                   // of the parameters as stored
-            values<P_BF16>(wp, p);
-            if (e.copy_t == FP8_STORE_BF16) {
-                uint32_t w[8];
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) w[j >> 1] = pack_bf16(p[j], p[j + 1]);
-                store_wide<true>(e.copy, i, count, vectors, w);
-            } else {
-                const float top = most8(p);
-                most = max_nan(most, top);
-                store_codes(e.copy, i, count, vectors, e.copy_t == FP8_STORE_E4M3 ? encode8_as<kE4M3>(p, top, copy_scale, false)
-                                                                                   : encode8_as<kE5M2>(p, top, copy_scale, false));
-            }
-        }
+    Raw<G_BF16, P_BF16, CODES> now, next;
+    int b = warp;
+    if (CODES && b < whole) now.fetch(e, lo + (int64_t)b * BLOCK + lane * 8, first + b);
+    for (; b < whole; b += WARPS) {
+        // 8-bit moments take longer to work on than to read: the next block is on its way meanwhile
+        if (!CODES) now.fetch(e, lo + (int64_t)b * BLOCK + lane * 8, first + b);
+        else if (b + WARPS < whole) next.fetch(e, lo + (int64_t)(b + WARPS) * BLOCK + lane * 8, first + b + WARPS);
+        most = max_nan(most, update_block<G_BF16, P_BF16, CODES>(a, e, s, now, lo + (int64_t)b * BLOCK + lane * 8, first + b, 8, keep, copy_scale));
+        if (CODES) now = next;
+    }
+#pragma unroll 1
+    for (; b < blocks; b += WARPS) {
+        const int64_t i = lo + (int64_t)b * BLOCK + lane * 8;
+        const int count = (int)max((int64_t)0, min((int64_t)8, lo + n - i));
+        now.fetch_some(e, i, first + b, count);
+        most = max_nan(most, update_block<G_BF16, P_BF16, CODES>(a, e, s, now, i, first + b, count == 8 ? 16 + 8 : count, keep, copy_scale));
     }
     return most;
 }
