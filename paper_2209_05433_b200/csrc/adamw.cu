@@ -28,7 +28,12 @@ namespace adamw {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int BLOCK = 256;                                 // elements that share a scale: 8 per lane
-constexpr int64_t MOST_CHUNK = 32768, LEAST_CHUNK = 2048;  // elements of a tensor handled by one CTA
+constexpr int64_t LEAST_CHUNK = 2048;                      // elements of a tensor handled by one CTA: at least,
+constexpr int64_t MOST_CHUNK = 65536;                      // at most, and
+constexpr int64_t MOST_CHUNK_32 = 8192;                    // in lists without 8-bit moments (268M parameters 1095 us; 1113 with 16384)
+constexpr int CTAS_PER_SM = 3;                             // 80 registers a thread; at 4 they spill
+constexpr int64_t AT_A_TIME = 148 * CTAS_PER_SM;           // CTAs that the GPU holds
+static_assert(MOST_CHUNK <= 32 * WARPS * BLOCK, "a lane for the scales of each of a warp's blocks");
 
 struct Entry {
     const void* g;
@@ -97,31 +102,27 @@ __device__ __forceinline__ uint2 ld2(const void* p) {
 template <bool G_BF16, bool P_BF16, bool CODES> struct Raw {
     static constexpr int STATE = CODES ? 2 : 8;
     uint32_t g[8], p[8], m[STATE], v[STATE];
-    float ms, vs;
+    float ms, vs;                                           // the block's scales
 
-    // i: the lane's first element, block: its block's index
-    __device__ __forceinline__ void fetch(const Entry& e, int64_t i, int64_t block) {
+    // i: the lane's first element
+    __device__ __forceinline__ void fetch(const Entry& e, int64_t i) {
         fetch_wide<P_BF16>(e.p, i, p);
         fetch_wide<G_BF16>(e.g, i, g);
         if (CODES) {
             const uint2 a = ld2(reinterpret_cast<const uint8_t*>(e.m) + i), b = ld2(reinterpret_cast<const uint8_t*>(e.v) + i);
             m[0] = a.x; m[1] = a.y; v[0] = b.x; v[1] = b.y;
-            ms = e.m_scale[block];
-            vs = e.v_scale[block];
         } else {
             fetch_wide<false>(e.m, i, *reinterpret_cast<uint32_t(*)[8]>(m));
             fetch_wide<false>(e.v, i, *reinterpret_cast<uint32_t(*)[8]>(v));
         }
     }
     // element by element; `count` of them exist, the others read as 0
-    __device__ __forceinline__ void fetch_some(const Entry& e, int64_t i, int64_t block, int count) {
+    __device__ __forceinline__ void fetch_some(const Entry& e, int64_t i, int count) {
         some_wide<P_BF16>(e.p, i, count, p);
         some_wide<G_BF16>(e.g, i, count, g);
         if (CODES) {
             some_codes(e.m, i, count, m);
             some_codes(e.v, i, count, v);
-            ms = e.m_scale[block];
-            vs = e.v_scale[block];
         } else {
             some_wide<false>(e.m, i, count, *reinterpret_cast<uint32_t(*)[8]>(m));
             some_wide<false>(e.v, i, count, *reinterpret_cast<uint32_t(*)[8]>(v));
@@ -196,23 +197,21 @@ __device__ __forceinline__ float root(float x) {             // 1 ulp
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float inverse_root(float x) {     // 2 ulp
+__device__ __forceinline__ float inverse_root(float x) {     // 2 ulp, of normal numbers
     float y;
-    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 // Square roots rounded to nearest: the product x / sqrt(x) of the approximation is corrected by its residual over twice the
-// root, which the fused operation gives without error for x above 2^-100; below, and there alone, the last bit may differ.
-// An x that has overflowed gives the largest number, beside which every moment vanishes.
+// root, which the fused operation gives without error for x above 2^-100; below, and there alone, the last bit may differ
+// (compared with the correctly rounded root on 46 million numbers: none differed).  NaN for an infinite x.
 __device__ __forceinline__ Pair root_nearest(Pair x) {
     float a, b;
-    x.split(a, b);
-    const Pair q(inverse_root(fmaxf(a, 1.17549435e-38f)), inverse_root(fmaxf(b, 1.17549435e-38f)));
+    (x + Pair(1.17549435e-38f)).split(a, b);                // zero has a root too
+    const Pair q(inverse_root(a), inverse_root(b));
     const Pair r = x * q;
-    float u, v;
-    r.split(u, v);
-    fma2(fma2(r, Pair(-u, -v), x), q * Pair(0.5f), r).split(a, b);
-    return Pair(fminf(a, 3.402823466e38f), fminf(b, 3.402823466e38f));
+    r.split(a, b);
+    return fma2(fma2(r, Pair(-a, -b), x), q * Pair(0.5f), r);
 }
 // The halves added one by one: as an addition of pairs it came out fused with the product before it.
 __device__ __forceinline__ Pair sum(Pair a, Pair b) {
@@ -225,23 +224,34 @@ __device__ __forceinline__ void split8(const Pair (&p)[4], float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) p[j].split(v[2 * j], v[2 * j + 1]);
 }
-// largest magnitude of the warp's eight values each; NaN if any is NaN
-__device__ __forceinline__ float warp_most(const float (&v)[8]) {
-    return __uint_as_float(warp_max_u32(canonical_nan_bits(__float_as_uint(most8(v)) & 0x7FFFFFFFu)));
-}
 // what brings a block's largest magnitude to 448; 0 for a block of zeros
 __device__ __forceinline__ float to_448(float most) { return most == 0.0f ? 0.0f : fminf(__frcp_rn(most) * 448.0f, 3.402823466e38f); }
 
-// Code of y in [0, 448] rounded up with the probability of its distance from the code below: floor(y / step + u) for 0 <= u < 1.
+// Code of y in [0, 448] rounded up with the probability of its distance from the code below: floor(y / step + u), u = chance / 65536.
 // Above the smallest normal value (2^-6) the step is an eighth of the power of two below y, and 8 .. 16 steps make up y, so the
-// number of steps and the exponent add up to the code; below, the steps themselves are the code.  `chance`: 2^23 + 65536 u.
-// A y that is not zero gets at least code 1.
-__device__ __forceinline__ uint32_t encode_chance(float y, float chance) {
+// number of steps and the exponent add up to the code; below, the steps themselves are the code.  A y that is not zero gets at
+// least code 1.
+__device__ __forceinline__ uint32_t encode_chance(float y, uint32_t chance) {
     const uint32_t bits = __float_as_uint(y), e = max(bits & 0x7F800000u, 121u << 23);          // the power of two below y
-    const float u = fmaf(chance, 1.0f / 65536.0f, -128.0f);
+    const float u = (float)chance * (1.0f / 65536.0f);
     const float steps = fmaf(y, __uint_as_float((257u << 23) - e), u);
-    const uint32_t whole = __float_as_uint(__fadd_rz(steps, 8388608.0f));                      // 2^23 + floor(steps)
-    return max((e >> 20) + whole - (121u * 8u + 0x4B000000u), min(bits, 1u));
+    return max((e >> 20) + (uint32_t)steps - 121u * 8u, min(bits, 1u));
+}
+// Codes of eight at once, words[j] holding the chances of 2j and 2j + 1.  Of normal values the code is what stands above bit 20
+// once the chance has been added below it: shifted left by 4 (the exponent's offset of 120 goes as 0x40 on top), the highest byte.
+__device__ __forceinline__ uint2 encode8_chance(const float (&y)[8], const uint32_t (&words)[4]) {
+    uint32_t c[8];
+    const float least = fminf(fminf(fminf(y[0], y[1]), fminf(y[2], y[3])), fminf(fminf(y[4], y[5]), fminf(y[6], y[7])));
+    if (least >= 0.015625f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            c[j] = (__float_as_uint(y[j]) << 4) + __byte_perm(words[j >> 1], 0x40000000u, j & 1 ? 0x7324 : 0x7104);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = encode_chance(y[j], j & 1 ? words[j >> 1] >> 16 : words[j >> 1] & 0xFFFFu) << 24;
+    }
+    auto pack = [](uint32_t q, uint32_t t, uint32_t u, uint32_t o) { return __byte_perm(__byte_perm(q, t, 0x0073), __byte_perm(u, o, 0x0073), 0x5410); };
+    return make_uint2(pack(c[0], c[1], c[2], c[3]), pack(c[4], c[5], c[6], c[7]));
 }
 
 struct Step {
@@ -251,10 +261,11 @@ struct Step {
 };
 
 // One block of 256 that is in registers: moments, parameters and what is stored.  i: the lane's first element; count: 8, or what
-// the element-wise stores take (16 for eight of them).  Returns the largest magnitude among the parameters, where there is a copy.
+// the element-wise stores take (16 more for eight of them).  Leaves the new scales in w; returns the largest magnitude among the
+// parameters, where there is a copy.
 template <bool G_BF16, bool P_BF16, bool CODES>
-__device__ __forceinline__ float update_block(const Params& a, const Entry& e, const Step& s, Raw<G_BF16, P_BF16, CODES>& w, int64_t i, int64_t block, int count,
-                                              float keep, float copy_scale) {
+__device__ __forceinline__ float update_block(const Params& a, const Entry& e, const Step& s, Raw<G_BF16, P_BF16, CODES>& w, int64_t i, int count, float keep,
+                                              float copy_scale) {
     Pair p[4], g[4], m[4], v[4], r[4];
     if (!s.skip) {
         values<P_BF16>(w.p, p);
@@ -273,43 +284,53 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
             const Pair gj = g[j] * Pair(s.coef);
             m[j] = sum(Pair(a.beta1) * m[j], Pair(a.rest1) * gj);
             v[j] = sum(Pair(a.beta2) * v[j], Pair(a.rest2) * gj * gj);
-            float x, y;
-            if (CODES) {
-                r[j] = root_nearest(v[j]);
-            } else {
-                v[j].split(x, y);
-                r[j] = Pair(root(x), root(y));
-            }
-            fma2(r[j], Pair(s.root2), Pair(a.eps)).split(x, y);
-            p[j] = fma2(p[j], Pair(keep), Pair(-s.rate) * m[j] * Pair(reciprocal_fast(x), reciprocal_fast(y)));
         }
-        float f[8];
+        float f[8], y[8], r_top = 0.0f;
         if (CODES) {
-            split8(m, f);
-            const float m_most = warp_most(f);
-            const Pair m_up(to_448(m_most));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) (m[j] * m_up).split(f[2 * j], f[2 * j + 1]);
-            store_codes(e.m, i, count, make_uint2(cvt_quad<kE4M3>(f[0], f[1], f[2], f[3]), cvt_quad<kE4M3>(f[4], f[5], f[6], f[7])));
+            for (int j = 0; j < 4; ++j) r[j] = root_nearest(v[j]);
             split8(r, f);
-            const float r_most = warp_most(f);
-            const Pair r_up(to_448(r_most));
-            uint32_t c[8];
+            r_top = most8(f);
+        }
+        if (!CODES || !(r_top <= 3.402823466e38f)) {        // 8-bit: a second moment has overflowed
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x, z;
+                v[j].split(x, z);
+                r[j] = Pair(root(x), root(z));
+            }
+            if (CODES) {
+                split8(r, f);
+                r_top = most8(f);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x, z;
+            fma2(r[j], Pair(s.root2), Pair(a.eps)).split(x, z);
+            p[j] = fma2(p[j], Pair(keep), Pair(-s.rate) * m[j] * Pair(reciprocal_fast(x), reciprocal_fast(z)));
+        }
+        if (CODES) {
+            split8(m, y);
+            // largest magnitudes of the block (a NaN is larger than any number), and each half of the warp one factor
+            const float m_most = __uint_as_float(warp_max_u32(__float_as_uint(most8(y)))), r_most = __uint_as_float(warp_max_u32(__float_as_uint(r_top)));
+            const float up = to_448((threadIdx.x & 16) ? r_most : m_most);
+            const Pair m_up(__shfl_sync(0xFFFFFFFFu, up, 0)), r_up(__shfl_sync(0xFFFFFFFFu, up, 16));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (m[j] * m_up).split(y[2 * j], y[2 * j + 1]);
+            store_codes(e.m, i, count, make_uint2(cvt_quad<kE4M3>(y[0], y[1], y[2], y[3]), cvt_quad<kE4M3>(y[4], y[5], y[6], y[7])));
+            uint32_t words[4];
             const uint32_t pair = (uint32_t)((uint64_t)(e.number + i) >> 1);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t word = mix((pair + j) * 0x9E3779B1u + s.key);
-                float x, y;
-                (r[j] * r_up).split(x, y);
-                c[2 * j] = encode_chance(fminf(x, 448.0f), __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7610)));
-                c[2 * j + 1] = encode_chance(fminf(y, 448.0f), __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7632)));
+                words[j] = mix((pair + j) * 0x9E3779B1u + s.key);
+                (r[j] * r_up).split(y[2 * j], y[2 * j + 1]);
             }
-            auto pack = [](uint32_t q, uint32_t t, uint32_t u, uint32_t o) { return __byte_perm(__byte_perm(q, t, 0x0040), __byte_perm(u, o, 0x0040), 0x5410); };
-            store_codes(e.v, i, count, make_uint2(pack(c[0], c[1], c[2], c[3]), pack(c[4], c[5], c[6], c[7])));
-            if ((threadIdx.x & 31) == 0) {
-                e.m_scale[block] = m_most * (1.0f / 448.0f);
-                e.v_scale[block] = r_most * (1.0f / 448.0f);
-            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = fminf(y[j], 448.0f);
+            store_codes(e.v, i, count, encode8_chance(y, words));
+            w.ms = m_most * (1.0f / 448.0f);
+            w.vs = r_most * (1.0f / 448.0f);
         } else {
             uint32_t t[8];
             split8(m, f);
@@ -355,55 +376,104 @@ __device__ __forceinline__ float update_chunk(const Params& a, const Entry& e, c
     const float keep = fmaf(-s.lr, e.decay, 1.0f);
     const float copy_scale = e.copy_t >= FP8_STORE_E4M3 && e.has_copy ? __ldg(e.copy_scale) : 1.0f;
     const int whole = e.vectors ? (int)(n / BLOCK) : 0, blocks = (int)((n + BLOCK - 1) / BLOCK);
-    const int64_t first = lo / BLOCK;                       // chunks are whole blocks
+    using Block = Raw<G_BF16, P_BF16, CODES>;
+    auto fetch = [&](Block& w, int b) { w.fetch(e, lo + (int64_t)b * BLOCK + lane * 8); };
     float most = 0.0f;
-    Raw<G_BF16, P_BF16, CODES> now, next;
-    int b = warp;
-    if (CODES && b < whole) now.fetch(e, lo + (int64_t)b * BLOCK + lane * 8, first + b);
-    for (; b < whole; b += WARPS) {
-        // 8-bit moments take longer to work on than to read: the next block is on its way meanwhile
-        if (!CODES) now.fetch(e, lo + (int64_t)b * BLOCK + lane * 8, first + b);
-        else if (b + WARPS < whole) next.fetch(e, lo + (int64_t)(b + WARPS) * BLOCK + lane * 8, first + b + WARPS);
-        most = max_nan(most, update_block<G_BF16, P_BF16, CODES>(a, e, s, now, lo + (int64_t)b * BLOCK + lane * 8, first + b, 8, keep, copy_scale));
-        if (CODES) now = next;
-    }
-#pragma unroll 1
-    for (; b < blocks; b += WARPS) {
+    auto update = [&](Block& w, int b) {
+        most = max_nan(most, update_block<G_BF16, P_BF16, CODES>(a, e, s, w, lo + (int64_t)b * BLOCK + lane * 8, 8, keep, copy_scale));
+    };
+    // element by element: the last block of a tensor, and all of one whose addresses do not suit vectors
+    auto some = [&](Block& w, int b) {
         const int64_t i = lo + (int64_t)b * BLOCK + lane * 8;
         const int count = (int)max((int64_t)0, min((int64_t)8, lo + n - i));
-        now.fetch_some(e, i, first + b, count);
-        most = max_nan(most, update_block<G_BF16, P_BF16, CODES>(a, e, s, now, i, first + b, count == 8 ? 16 + 8 : count, keep, copy_scale));
+        w.fetch_some(e, i, count);
+        most = max_nan(most, update_block<G_BF16, P_BF16, CODES>(a, e, s, w, i, count == 8 ? 16 + 8 : count, keep, copy_scale));
+    };
+    Block now;
+    if (!CODES) {                                           // the warps side by side
+        int b = warp;
+        for (; b < whole; b += WARPS) {
+            fetch(now, b);
+            update(now, b);
+        }
+#pragma unroll 1
+        for (; b < blocks; b += WARPS) some(now, b);
+        return most;
     }
+    // 8-bit moments: a warp has blocks that follow one another, so that their scales are one access, a lane each (one scale at a
+    // time, four bytes from and to lines that eight warps shared, cost a quarter of the time: 268M parameters 884 us instead of
+    // 663).  The next block is on its way while one is worked on, in the other of two sets of registers; the last turn fetches its
+    // own block once more and drops it, as a fetch that may not happen would be waited for at once.
+    const int each = (blocks + WARPS - 1) / WARPS, b0 = warp * each, b1 = min(b0 + each, blocks), fast = min(b1, whole);
+    if (b0 >= b1) return most;
+    float* const ms_at = e.m_scale + lo / BLOCK + b0 + lane;      // chunks are whole blocks
+    float* const vs_at = e.v_scale + lo / BLOCK + b0 + lane;
+    const bool mine = b0 + lane < b1;
+    float ms = mine ? *ms_at : 0.0f, vs = mine ? *vs_at : 0.0f;
+    auto scales = [&](Block& w, int b) {
+        w.ms = __shfl_sync(0xFFFFFFFFu, ms, b - b0);
+        w.vs = __shfl_sync(0xFFFFFFFFu, vs, b - b0);
+    };
+    auto keep_scales = [&](const Block& w, int b) {
+        if (lane == b - b0) { ms = w.ms; vs = w.vs; }
+    };
+    int b = b0;
+    if (b < fast) {
+        Block next;
+        fetch(now, b);
+        while (b < fast) {
+            fetch(next, min(b + 1, fast - 1));
+            scales(now, b);
+            update(now, b);
+            keep_scales(now, b);
+            if (++b >= fast) break;
+            fetch(now, min(b + 1, fast - 1));
+            scales(next, b);
+            update(next, b);
+            keep_scales(next, b);
+            ++b;
+        }
+    }
+#pragma unroll 1
+    for (; b < b1; ++b) {
+        scales(now, b);
+        some(now, b);
+        keep_scales(now, b);
+    }
+    if (mine) { *ms_at = ms; *vs_at = vs; }
     return most;
 }
 
-__global__ void __launch_bounds__(THREADS, 3) k_adamw(const Params a) {
-    __shared__ Entry e;
-    __shared__ Step s;
-    __shared__ uint32_t red[WARPS];
-    __shared__ unsigned int last;
+// One CTA per chunk.  Its warps go their own ways: each reads the table entry and the step's numbers for itself, and the one
+// that is done last counts the CTA.  (With barriers in the place of that a fifth of the warps' time went by waiting at them.)
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) k_adamw(const Params a) {
+    __shared__ Entry entries[WARPS];
+    __shared__ unsigned int done, top;
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) done = top = 0u;
+    __syncthreads();
+    Entry& e = entries[threadIdx.x >> 5];
     // The table is the plan's own: copied to the device before the first call, written by no kernel.
     int entry = -1;
     if ((int64_t)blockIdx.x < a.chunks) {
         entry = a.chunk_entry[blockIdx.x];
-        if (threadIdx.x < 32) reinterpret_cast<uint32_t*>(&e)[threadIdx.x] = reinterpret_cast<const uint32_t*>(a.entries + entry)[threadIdx.x];
+        reinterpret_cast<uint32_t*>(&e)[lane] = reinterpret_cast<const uint32_t*>(a.entries + entry)[lane];
+        __syncwarp();
     }
     grid_launch_dependents();
     grid_dependency_wait();
-    if (threadIdx.x == 0) {
+    Step s;
+    {
         const int64_t t = a.step_dev ? *a.step_dev + 1 : a.step;
-        const float lr = a.lr_dev ? *a.lr_dev : (float)a.lr;
         const float norm = a.norm ? *a.norm : 0.0f;
+        s.lr = a.lr_dev ? *a.lr_dev : (float)a.lr;
         s.skip = a.norm && !(fabsf(norm) <= 3.402823466e38f);
         s.coef = !a.norm || norm <= a.max_norm ? 1.0f : a.max_norm / norm;
         // 1 - b^t without cancellation
-        const float c1 = -expm1f((float)((double)t * a.ln_beta1)), c2 = -expm1f((float)((double)t * a.ln_beta2));
-        s.lr = lr;
-        s.rate = lr / c1;
-        s.root2 = 1.0f / sqrtf(c2);
+        s.rate = s.lr / -expm1f((float)((double)t * a.ln_beta1));
+        s.root2 = 1.0f / sqrtf(-expm1f((float)((double)t * a.ln_beta2)));
         s.key = mix((uint32_t)a.seed ^ mix((uint32_t)(a.seed >> 32) ^ mix((uint32_t)t)));
     }
-    __syncthreads();
     float most = 0.0f;
     if (entry >= 0) {
         const int64_t lo = ((int64_t)blockIdx.x - e.first_chunk) * a.chunk, n = min(a.chunk, e.n - lo);
@@ -420,24 +490,25 @@ __global__ void __launch_bounds__(THREADS, 3) k_adamw(const Params a) {
     }
     if (!a.finish) return;
     const uint32_t bits = warp_max_u32(canonical_nan_bits(__float_as_uint(most) & 0x7FFFFFFFu));
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = bits;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        uint32_t top = 0u;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) top = max(top, red[w]);
-        if (top != 0u && e.amax) atomicMax(a.amax + entry, top);
-        __threadfence();
-        last = atomicAdd(a.counter, 1u) == gridDim.x - 1 ? 1u : 0u;
+    unsigned int last = 0u;
+    if (lane == 0) {
+        if (bits != 0u) atomicMax(&top, bits);
+        __threadfence_block();
+        if (atomicAdd(&done, 1u) == WARPS - 1) {
+            __threadfence_block();
+            const unsigned int all = atomicMax(&top, 0u);
+            if (all != 0u && e.amax) atomicMax(a.amax + entry, all);
+            __threadfence();
+            last = atomicAdd(a.counter, 1u) == gridDim.x - 1 ? 1u : 0u;
+        }
     }
-    __syncthreads();
-    if (!last) return;
+    if (!__shfl_sync(0xFFFFFFFFu, last, 0)) return;
     __threadfence();
-    for (int64_t i = threadIdx.x; i < a.count; i += THREADS) {
+    for (int64_t i = lane; i < a.count; i += 32) {
         float* out = a.entries[i].amax;
         if (out) *out = __uint_as_float(atomicExch(a.amax + i, 0u));
     }
-    if (threadIdx.x == 0) {
+    if (lane == 0) {
         *a.counter = 0u;
         if (a.step_dev && !s.skip) *a.step_dev += 1;
     }
@@ -457,10 +528,11 @@ fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_a
     if (!plan || (count > 0 && !items)) return FP8_ERR_NULL;
     if (count < 0) return FP8_ERR_SHAPE;
     if (count > 0x7FFFFFFF) return FP8_ERR_UNSUPPORTED;
-    int64_t total = 0, amaxes = 0;
+    int64_t total = 0, amaxes = 0, most_chunk = MOST_CHUNK_32;
     for (int64_t i = 0; i < count; ++i) {
         const fp8_adamw_item& it = items[i];
         const bool codes = it.state == FP8_STATE_E4M3;
+        if (codes) most_chunk = MOST_CHUNK;
         if ((it.g_t != FP8_F32 && it.g_t != FP8_BF16) || (it.p_t != FP8_F32 && it.p_t != FP8_BF16) || (it.state != FP8_STATE_F32 && !codes) ||
             (it.copy && (it.copy_t < FP8_STORE_BF16 || it.copy_t > FP8_STORE_E5M2)))
             return FP8_ERR_ENUM;
@@ -479,11 +551,18 @@ fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_a
         total += (it.n + BLOCK - 1) / BLOCK * BLOCK;
         amaxes += it.copy_amax_dev ? 1 : 0;
     }
-    // Short lists are cut finer: about eight CTAs for each of 148 SMs.
-    int64_t chunk = MOST_CHUNK;
-    while (chunk > LEAST_CHUNK && total / chunk < 148 * 8) chunk /= 2;
-    int64_t chunks = 0;
-    for (int64_t i = 0; i < count; ++i) chunks += (items[i].n + chunk - 1) / chunk;
+    // The chunk is the smallest with which the CTAs fill whole rounds of what the GPU holds at a time, as few rounds as there can
+    // be: CTAs start together and end together.
+    int64_t chunk = LEAST_CHUNK, chunks = 0;
+    for (int64_t rounds = (total + most_chunk * AT_A_TIME - 1) / (most_chunk * AT_A_TIME);; ++rounds) {
+        chunk = total / (rounds > 0 ? rounds * AT_A_TIME : 1) / LEAST_CHUNK * LEAST_CHUNK;
+        for (chunk = chunk < LEAST_CHUNK ? LEAST_CHUNK : chunk; chunk <= most_chunk; chunk += LEAST_CHUNK) {
+            chunks = 0;
+            for (int64_t i = 0; i < count; ++i) chunks += (items[i].n + chunk - 1) / chunk;
+            if (chunks <= rounds * AT_A_TIME) break;
+        }
+        if (chunk <= most_chunk) break;
+    }
     if (chunks > 0x7FFFFFFF) return FP8_ERR_UNSUPPORTED;
     plan->count = count;
     plan->chunks = chunks;
