@@ -694,12 +694,6 @@ def fp8_grad_clip(plan: ClipPlan, max_norm: float, norm_out: torch.Tensor) -> No
     _check(load().fp8_grad_clip(*plan._call, max_norm, _scalar(norm_out, "norm_out"), _stream()), "fp8_grad_clip")
 
 
-def _here(t: torch.Tensor, name: str) -> torch.Tensor:
-    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
-        raise ValueError("%s must be a tensor of the current CUDA device" % name)
-    return t
-
-
 STATE_BLOCK = 256            # elements of an 8-bit state that share a scale
 
 
@@ -764,8 +758,14 @@ class AdamWPlan:
         # the copy from pageable memory returns when the stream has done it, and with it the zeros: any stream may use the plan
         self.workspace = torch.zeros(self.sizes.workspace_bytes, dtype=torch.uint8, device=device)
         self.table = host.to(device)
-        self.device = device
+        self.device = device.index if device.index is not None else torch.cuda.current_device()
         self._call = (ctypes.byref(self.sizes), self.table.data_ptr(), self.workspace.data_ptr())
+
+
+def _here(t: torch.Tensor, name: str) -> torch.Tensor:
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must be a tensor of the current CUDA device" % name)
+    return t
 
 
 def fp8_adamw_step(plan: AdamWPlan, lr: float | torch.Tensor, step: int | torch.Tensor, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -773,7 +773,7 @@ def fp8_adamw_step(plan: AdamWPlan, lr: float | torch.Tensor, step: int | torch.
     """One AdamW step of the plan's tensors.  ``step`` counts from 1; a one-element int64 CUDA tensor holds the steps taken so far
     instead, and is advanced.  ``lr`` may be a one-element float32 CUDA tensor.  With ``norm`` (what fp8_grad_norm wrote) gradients are
     scaled by min(1, max_norm / norm), and a norm that is not finite skips the step.  ``seed`` is for 8-bit moments."""
-    if plan.device.index != torch._C._cuda_getDevice():
+    if plan.device != torch._C._cuda_getDevice():
         raise ValueError("the plan's tensors must be on the current CUDA device")
     if (norm is None) != (max_norm is None):
         raise ValueError("norm and max_norm go together")
@@ -792,60 +792,83 @@ def fp8_adamw_step(plan: AdamWPlan, lr: float | torch.Tensor, step: int | torch.
 
 def _pitch_of(t: torch.Tensor) -> int:
     """Row pitch in elements; of a single row, whose stride means nothing, one that suits any alignment."""
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else -(-cols // 16) * 16
 
 
-def _vocabulary_operand(t: torch.Tensor, fmt: int | None, name: str) -> int:
-    """fp8_operand of a 2-D operand with contiguous rows: uint8 codes of format fmt, or bfloat16 with fmt None"""
-    _here(t, name)
-    if t.dim() != 2 or t.stride(1) != 1:
-        raise ValueError("%s must be a 2-D tensor with unit inner stride" % name)
-    if t.dtype is torch.uint8:
-        if fmt not in (E4M3, E5M2):
+def _vocabulary_operand(t: torch.Tensor, fmt: int | None, device: int, name: str) -> tuple[int, int, int, int]:
+    """(rows, columns, pitch, fp8_operand) of an operand with contiguous rows: uint8 codes of format fmt, or bfloat16 with fmt None"""
+    if t.dim() != 2 or t.get_device() != device:
+        raise ValueError("%s must be a 2-D tensor of the current CUDA device" % name)
+    pitch, inner = t.stride()
+    rows, cols = t.shape
+    if inner != 1:
+        raise ValueError("%s must have unit inner stride" % name)
+    if rows <= 1:
+        pitch = -(-cols // 16) * 16
+    dtype = t.dtype
+    if dtype is torch.uint8:
+        if fmt != E4M3 and fmt != E5M2:
             raise TypeError("the codes of %s need their format, E4M3 or E5M2" % name)
-        return fmt
-    if t.dtype is not torch.bfloat16 or fmt is not None:
+        return rows, cols, pitch, fmt
+    if dtype is not torch.bfloat16 or fmt is not None:
         raise TypeError("%s must be uint8 codes with their format, or bfloat16 with format None" % name)
-    return OPERAND_BF16
+    return rows, cols, pitch, OPERAND_BF16
 
 
-def _per_token(t: torch.Tensor, dtype: torch.dtype, tokens: int, name: str) -> int:
-    _here(t, name)
-    if t.dtype is not dtype or t.shape != (tokens,) or not t.is_contiguous():
-        raise TypeError("%s must be a contiguous %s tensor with %d elements" % (name, dtype, tokens))
+def _per_token(t: torch.Tensor, dtype: torch.dtype, tokens: int, device: int, name: str) -> int:
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != tokens or not t.is_contiguous() or t.get_device() != device:
+        raise TypeError("%s must be a contiguous %s tensor of %d elements on the current CUDA device" % (name, dtype, tokens))
     return t.data_ptr()
 
 
-def _cross_entropy_args(x, fx, w, fw, scale_inv_x, scale_inv_w):
-    x_t, w_t = _vocabulary_operand(x, fx, "x"), _vocabulary_operand(w, fw, "w")
-    tokens, width = x.shape
-    vocab, width_w = w.shape
-    if width != width_w:
-        raise ValueError("x has rows of %d, w of %d" % (width, width_w))
-    d = _pack_cross_entropy(tokens, width, vocab, x_t, w_t, _pitch_of(x), _pitch_of(w))
-    sx = None if scale_inv_x is None else _scalar(_here(scale_inv_x, "scale_inv_x"), "scale_inv_x")
-    sw = None if scale_inv_w is None else _scalar(_here(scale_inv_w, "scale_inv_w"), "scale_inv_w")
-    return tokens, width, vocab, d, (x.data_ptr(), w.data_ptr(), sx, sw)
+def _scale_here(t: torch.Tensor | None, device: int, name: str) -> int | None:
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError("%s must be a tensor of the current CUDA device" % name)
+    return _scalar(t, name)
+
+
+def _gradient_args(t: torch.Tensor | None, rows: int, cols: int, device: int, name: str) -> tuple:
+    """(address, fp8_wide, pitch) of a gradient, or of none"""
+    if t is None:
+        return None, BF16, cols
+    if t.get_device() != device or t.dim() != 2:
+        raise ValueError("%s must be a 2-D tensor of the current CUDA device" % name)
+    return t.data_ptr(), _wide2d(t, (rows, cols), name), _pitch_of(t)
+
+
+_loss_workspace_bytes: dict = {}              # (descriptor without its pitches, device) -> bytes of (forward, backward)
+
+
+def _loss_workspaces(tokens: int, width: int, vocab: int, x_t: int, w_t: int, device: int) -> tuple[int, int]:
+    key = (tokens, width, vocab, x_t, w_t, device)
+    sizes = _loss_workspace_bytes.get(key)
+    if sizes is None:
+        forward, backward = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        _check((_lib or load()).fp8_cross_entropy_workspace_bytes(_pack_cross_entropy(tokens, width, vocab, x_t, w_t, 0, 0), ctypes.byref(forward),
+                                                                  ctypes.byref(backward)), "fp8_cross_entropy_workspace_bytes")
+        if len(_loss_workspace_bytes) >= 1024:
+            _loss_workspace_bytes.clear()
+        sizes = _loss_workspace_bytes[key] = (forward.value, backward.value)
+    return sizes
 
 
 def cross_entropy_workspace_bytes(tokens: int, width: int, vocab: int, bf16: bool = False) -> tuple[int, int]:
     """Workspace bytes of (fp8_cross_entropy, fp8_cross_entropy_backward) on the current device."""
     t = OPERAND_BF16 if bf16 else E4M3
-    forward, backward = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check((_lib or load()).fp8_cross_entropy_workspace_bytes(_pack_cross_entropy(tokens, width, vocab, t, t, 0, 0), ctypes.byref(forward), ctypes.byref(backward)),
-           "fp8_cross_entropy_workspace_bytes")
-    return forward.value, backward.value
+    return _loss_workspaces(tokens, width, vocab, t, t, torch._C._cuda_getDevice())
 
 
-def _loss_workspace(d: bytes, which: int, device: torch.device, workspace: torch.Tensor | None) -> tuple:
-    """(address, bytes, what keeps it alive).  Its contents mean nothing, so it comes from torch's allocator for this call:
-    memory that goes back to it is handed out on this stream alone, or belongs to the graph that is being captured."""
-    if workspace is not None:
-        return _dev(_here(workspace, "workspace"), "workspace"), workspace.numel() * workspace.element_size(), workspace
-    sizes = (ctypes.c_size_t(0), ctypes.c_size_t(0))
-    _check((_lib or load()).fp8_cross_entropy_workspace_bytes(d, ctypes.byref(sizes[0]), ctypes.byref(sizes[1])), "fp8_cross_entropy_workspace_bytes")
-    ws = torch.empty(max(16, sizes[which].value), dtype=torch.uint8, device=device)
-    return ws.data_ptr(), ws.numel(), ws
+def _loss_workspace(need: int, device: int, workspace: torch.Tensor | None) -> torch.Tensor:
+    """The caller's workspace, or one for this call.  Its contents mean nothing, so it comes from torch's allocator each time:
+    memory that goes back there is handed out on this stream alone, or belongs to the graph that is being captured."""
+    if workspace is None:
+        return torch.empty(need if need > 16 else 16, dtype=torch.uint8, device="cuda")
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor of the current CUDA device")
+    return workspace
 
 
 def fp8_cross_entropy(x: torch.Tensor, fx: int | None, w: torch.Tensor, fw: int | None, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
@@ -856,11 +879,18 @@ def fp8_cross_entropy(x: torch.Tensor, fx: int | None, w: torch.Tensor, fw: int 
     target is int64; a token whose target is outside 0 .. vocab - 1 does not count (loss 0).  loss and lse are float32, one
     element per token; the backward pass reads lse.  ``workspace`` of cross_entropy_workspace_bytes(...)[0] bytes is taken from
     torch's allocator where none is given."""
-    tokens, _, _, d, operands = _cross_entropy_args(x, fx, w, fw, scale_inv_x, scale_inv_w)
-    target_ptr = _per_token(target, torch.int64, tokens, "target")
-    loss_ptr, lse_ptr = _per_token(loss, torch.float32, tokens, "loss"), _per_token(lse, torch.float32, tokens, "lse")
-    ws, nbytes, _keep = _loss_workspace(d, 0, x.device, workspace)
-    _check(_lib.fp8_cross_entropy(d, *operands, target_ptr, loss_ptr, lse_ptr, ws, nbytes, _stream()), "fp8_cross_entropy")
+    device = torch._C._cuda_getDevice()
+    tokens, width, ldx, x_t = _vocabulary_operand(x, fx, device, "x")
+    vocab, width_w, ldw, w_t = _vocabulary_operand(w, fw, device, "w")
+    if width != width_w:
+        raise ValueError("x has rows of %d, w of %d" % (width, width_w))
+    need, _ = _loss_workspaces(tokens, width, vocab, x_t, w_t, device)
+    ws = _loss_workspace(need, device, workspace)
+    _check(_lib.fp8_cross_entropy(_pack_cross_entropy(tokens, width, vocab, x_t, w_t, ldx, ldw), x.data_ptr(), w.data_ptr(),
+                                  _scale_here(scale_inv_x, device, "scale_inv_x"), _scale_here(scale_inv_w, device, "scale_inv_w"),
+                                  _per_token(target, torch.int64, tokens, device, "target"), _per_token(loss, torch.float32, tokens, device, "loss"),
+                                  _per_token(lse, torch.float32, tokens, device, "lse"), ws.data_ptr(), ws.nbytes,
+                                  torch._C._cuda_getCurrentRawStream(device)), "fp8_cross_entropy")
 
 
 def fp8_cross_entropy_backward(x: torch.Tensor, fx: int | None, w: torch.Tensor, fw: int | None, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
@@ -869,13 +899,19 @@ def fp8_cross_entropy_backward(x: torch.Tensor, fx: int | None, w: torch.Tensor,
     """Gradients of sum(dloss * loss): dx [tokens, width] and dw [vocab, width], float32 or bfloat16 each, overwritten; None
     leaves one out.  ``lse`` is what fp8_cross_entropy wrote, ``dloss`` one float32 factor per token (1 / tokens for a mean).  The
     gradient of the logits passes through E5M2 codes (FP8 operands) or bfloat16, a piece of the vocabulary at a time."""
-    tokens, width, vocab, d, operands = _cross_entropy_args(x, fx, w, fw, scale_inv_x, scale_inv_w)
-    target_ptr = _per_token(target, torch.int64, tokens, "target")
-    lse_ptr, dloss_ptr = _per_token(lse, torch.float32, tokens, "lse"), _per_token(dloss, torch.float32, tokens, "dloss")
-    dx_args = (None, BF16, width) if dx is None else (_here(dx, "dx").data_ptr(), _wide2d(dx, (tokens, width), "dx"), _pitch_of(dx))
-    dw_args = (None, BF16, width) if dw is None else (_here(dw, "dw").data_ptr(), _wide2d(dw, (vocab, width), "dw"), _pitch_of(dw))
-    ws, nbytes, _keep = _loss_workspace(d, 1, x.device, workspace)
-    _check(_lib.fp8_cross_entropy_backward(d, *operands, target_ptr, lse_ptr, dloss_ptr, *dx_args, *dw_args, ws, nbytes, _stream()), "fp8_cross_entropy_backward")
+    device = torch._C._cuda_getDevice()
+    tokens, width, ldx, x_t = _vocabulary_operand(x, fx, device, "x")
+    vocab, width_w, ldw, w_t = _vocabulary_operand(w, fw, device, "w")
+    if width != width_w:
+        raise ValueError("x has rows of %d, w of %d" % (width, width_w))
+    _, need = _loss_workspaces(tokens, width, vocab, x_t, w_t, device)
+    ws = _loss_workspace(need, device, workspace)
+    _check(_lib.fp8_cross_entropy_backward(_pack_cross_entropy(tokens, width, vocab, x_t, w_t, ldx, ldw), x.data_ptr(), w.data_ptr(),
+                                           _scale_here(scale_inv_x, device, "scale_inv_x"), _scale_here(scale_inv_w, device, "scale_inv_w"),
+                                           _per_token(target, torch.int64, tokens, device, "target"), _per_token(lse, torch.float32, tokens, device, "lse"),
+                                           _per_token(dloss, torch.float32, tokens, device, "dloss"), *_gradient_args(dx, tokens, width, device, "dx"),
+                                           *_gradient_args(dw, vocab, width, device, "dw"), ws.data_ptr(), ws.nbytes,
+                                           torch._C._cuda_getCurrentRawStream(device)), "fp8_cross_entropy_backward")
 
 
 TIMEOUT = 7                                   # FP8_ERR_TIMEOUT

@@ -19,6 +19,7 @@
 #include <stdint.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "activation.cuh"
 #include "codec.cuh"
@@ -32,25 +33,26 @@ using namespace gemm;
 
 constexpr int MODE_STATS = 0;           // (maximum, sum of exponentials) of a row's columns, and the target's logit
 constexpr int MODE_DZ = 1;              // gradient of the logits
-constexpr int MODE_BF16 = 2;            // the scaled product, rounded
-constexpr int MODE_F32 = 3;             // the scaled product
-constexpr int MODE_ADD = 4;             // added to what is there, in binary32
+constexpr int MODE_OUT = 2;             // the scaled product itself, of one or two independent products:
+enum : int { OUT_ROUNDED = 0, OUT_WIDE = 1, OUT_ADDED = 2 };     // as bf16, as binary32, or added to what is there
 
 constexpr int ROWS = 128;               // rows of a CTA's tile (one TMEM lane each)
 constexpr int K_BYTES = 128;            // K-block: one 128-byte swizzle row, 128 elements of 8 bits or 64 of 16
 constexpr int K_STEP_BYTES = 32;        // K of one tcgen05.mma
 // Of K, what one use of the accumulator covers.  The tensor core truncates what it adds, once per K_STEP_BYTES: a logit that
 // grows steadily loses up to that many steps times 2^-24 of itself.  bf16 products have more bits to lose and half the steps
-// per use, and their loss was off by 1.1e-6 with 2048 (start: 32-bit sums 7e-7).
-template <int ESZ> constexpr int split_of = ESZ == 1 ? 2048 : 512;
+// per use: with 2048 their loss was off by 6e-6 in root mean square (sums in binary32: 4e-6), with 512 by 1.5e-6 (FP8: 5e-7).  The
+// gradient of the logits takes the same, so that its logits are those of the sum; the products behind it are rounded coarsely.
+template <int ESZ, int MODE> constexpr int split_of = ESZ == 1 || MODE == MODE_OUT ? 2048 : 512;
 constexpr int FG = 2;                   // K-blocks consumed per barrier wait
-constexpr int MAX_STAGES = 6;
+constexpr int MAX_STAGES = 12;
 constexpr uint32_t A_BYTES = ROWS * K_BYTES;
 constexpr uint32_t RING_BYTES = 196608;
 constexpr uint32_t BOX_BYTES = 4096;    // 32 rows x 128 B: staging of one epilogue warp
 constexpr int EPI_BASE = 4, EPI_WARPS = 8, THREADS = 32 * (EPI_BASE + EPI_WARPS);
 constexpr int REGS_FRONT = 56, REGS_EPILOGUE = 224;      // 128 x 56 + 256 x 224 = 64512, the launch's 384 x 168
-constexpr uint32_t SMEM_BYTES = RING_BYTES + EPI_WARPS * BOX_BYTES + 256 + 1024;
+constexpr uint32_t SMEM_BARRIERS = 512;
+constexpr uint32_t SMEM_BYTES = RING_BYTES + EPI_WARPS * BOX_BYTES + SMEM_BARRIERS + 1024;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int GROUP_M = 16;             // row tiles that advance together over the columns
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
@@ -58,30 +60,38 @@ constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 // codes written to the error latch
 enum : uint32_t { L_WAIT_EMPTY = 49, L_WAIT_FULL = 50, L_WAIT_ACC_EMPTY = 51, L_WAIT_ACC_FULL = 52 };
 
-struct Params {
+struct Product {
     int64_t M, N, K;
     const float* s[2];                  // factors of the product; null counts as 1
-    uint32_t idesc;
-    int tiles_m, tiles_n;
-    int slices, slice_blocks;           // K in slices of slice_blocks K-blocks, each with an output plane of its own
-    int a_mn, b_mn;                     // operand stored with its M (N) index contiguous
     void* D;
     int64_t ldd;                        // elements
-    int ragged;                         // rows of D do not end on 16 bytes
+    int out, ragged;                    // what is stored; rows of D do not end on 16 bytes
+    uint32_t idesc;
+    int tiles_m, tiles_n, tiles;        // tiles: of all slices
+    int k_blocks, slices, slice_blocks; // K in slices of slice_blocks K-blocks, each with an output plane of its own
+    int a_mn, b_mn;                     // operand stored with its M (N) index contiguous
+};
+struct Params {
+    Product q[2];
+    int products;
+    int full, rest, extra;              // how the tiles of two products are dealt out, see item_at
+    int stages;                         // of the ring (one CTA per tile)
+    uint32_t a_bytes;                   // A's part of a stage (one CTA per tile)
     const int64_t* target;
     int64_t first, vocab;               // vocabulary column of the first column here; all columns of the vocabulary
     float2* part;                       // [2 tiles_n][M]
     float* logit;                       // [M]: the target's, times log2(e)
     const float* lse;
     const float* dloss;
-    const float* dz_scale;              // scale of dz's codes; null: dz is bf16
+    float* dz_scale;                    // written: scale of dz's codes and its inverse
 };
 
 struct alignas(8) Barriers {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full[2], acc_empty[2];
     uint32_t tmem_base, abort_flag;
+    uint32_t most[EPI_WARPS];
 };
-static_assert(sizeof(Barriers) <= 256, "barrier block too large");
+static_assert(sizeof(Barriers) <= SMEM_BARRIERS, "barrier block too large");
 
 __device__ __forceinline__ void mma_bf16(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -106,19 +116,41 @@ __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm
     tn = r / rows;
 }
 
+// The j-th item of a worker: a tile of one of the products.  The first product, the one with the longer K, is dealt out in rounds
+// of all workers; in its last round only `rest` of them get a tile.  The others take `extra` tiles of the second product
+// meanwhile, and the remaining ones are dealt out in rounds again: all workers end at about the same time.
+__device__ __forceinline__ bool item_at(const Params& p, int j, int worker, int workers, int& which, int& t) {
+    which = 0;
+    t = worker + j * workers;
+    if (t < p.q[0].tiles) return true;
+    if (p.products == 1) return false;
+    which = 1;
+    const bool late = worker >= p.rest;
+    int i = j - p.full - (late ? 0 : 1);
+    if (late) {
+        if (i < p.extra) {
+            t = i * (workers - p.rest) + worker - p.rest;
+            return true;
+        }
+        i -= p.extra;
+    }
+    t = p.extra * (workers - p.rest) + i * workers + worker;
+    return t < p.q[1].tiles;
+}
+
 // ESZ: bytes of an operand's element (1: FP8, 2: bf16).  CG: CTAs of a tile.  BN: its columns.
 template <int ESZ, int CG, int BN, int MODE>
 __global__ void __launch_bounds__(THREADS, 1)
 k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_d,
-             const Params p) {
+             const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_d1,
+             const __grid_constant__ Params p) {
     constexpr int KE = K_BYTES / ESZ;                             // elements of a K-block
     constexpr int MNE = 128 / ESZ;                                // M or N elements of a 128-byte row of an MN-major box
     constexpr uint32_t MN_BOX = (uint32_t)KE * 128;               // such a box: MNE elements x one K-block
     constexpr int B_ROWS = BN / CG;                               // columns of the tile that this CTA loads
-    constexpr uint32_t STAGE_BYTES = A_BYTES + B_ROWS * K_BYTES;
-    constexpr int STAGES = RING_BYTES / STAGE_BYTES;
-    static_assert(STAGES % FG == 0 && STAGES <= MAX_STAGES, "ring depth");
-    constexpr int SPLIT = split_of<ESZ> / KE;                     // K-blocks per use of an accumulator
+    const uint32_t a_bytes = CG == 2 ? A_BYTES : p.a_bytes, stage_bytes = a_bytes + B_ROWS * K_BYTES;
+    const uint32_t stages = CG == 2 ? RING_BYTES / (A_BYTES + B_ROWS * K_BYTES) : (uint32_t)p.stages;
+    constexpr int SPLIT = split_of<ESZ, MODE> / KE;                   // K-blocks per use of an accumulator
     constexpr int NC = BN / 2;                                    // columns of an epilogue thread
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -129,11 +161,9 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_ctarank() : 0u;       // 0 = leader of the pair
     const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
-    const int plane_tiles = p.tiles_m * p.tiles_n, tiles = plane_tiles * p.slices;
-    const int k_blocks = (int)((p.K + KE - 1) / KE);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), FG * CG); mbar_init(smem_u32(&bars->empty[s]), 1); }
+        for (uint32_t s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars->full[s]), FG * CG); mbar_init(smem_u32(&bars->empty[s]), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars->acc_full[a]), 1); mbar_init(smem_u32(&bars->acc_empty[a]), EPI_WARPS * CG); }
         bars->abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -163,20 +193,25 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         uint32_t stage = 0, phase = 0;
         bool ok = true;
         const uint64_t keep = policy_evict_last();
-        int nth = 0;
-        for (int t = worker; t < tiles && ok; t += workers) {
+        int which, t;
+        for (int j = 0; ok && item_at(p, j, worker, workers, which, t); ++j) {
+            const Product& q = p.q[which];
+            const CUtensorMap* ma = which ? &map_a1 : &map_a;
+            const CUtensorMap* mb = which ? &map_b1 : &map_b;
             int tm, tn;
-            const int slice = t / plane_tiles;
-            tile_at(t - slice * plane_tiles, p.tiles_m, p.tiles_n, tm, tn);
+            const int plane_tiles = q.tiles_m * q.tiles_n, slice = q.slices > 1 ? t / plane_tiles : 0;
+            tile_at(t - slice * plane_tiles, q.tiles_m, q.tiles_n, tm, tn);
             const int m0 = (tm * CG + (int)rank) * ROWS, n0 = tn * BN + (int)rank * B_ROWS;
-            const int kb0 = slice * p.slice_blocks, kn = min(p.slice_blocks, k_blocks - kb0);
+            const int kb0 = slice * q.slice_blocks, kn = min(q.slice_blocks, q.k_blocks - kb0);
             const int kn_pad = (kn + FG - 1) / FG * FG;
-            const bool backwards = (nth++ & 1) != 0;              // every second tile starts where the last one ended: L2 still has it
+            // Every second round starts at the end of K where the last one ended: L2 still has it.  The round is the tile's own, not the
+            // worker's count: a product's bits do not depend on what else is in the launch.
+            const bool backwards = (t / workers & 1) != 0;
             for (int kb = 0; kb < kn_pad; ++kb) {
                 ok = mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, L_WAIT_EMPTY);
                 if (!ok) break;
                 if (lane == 0) {
-                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + A_BYTES;
+                    const uint32_t sa = ring + stage * stage_bytes, sb = sa + a_bytes;
                     const uint32_t bar = smem_u32(&bars->full[stage / FG]);
                     const uint32_t full = CG == 2 ? map_to_cta(bar, 0) : bar;          // the leader's
                     if (kb < kn) {
@@ -185,19 +220,19 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                             if (CG == 2) tma_load_3d_pair(dst, map, c0, c1, 0, full, keep);
                             else         tma_load_3d(dst, map, c0, c1, 0, full, keep);
                         };
-                        if (CG == 2) mbar_arrive_expect_tx_cluster(full, STAGE_BYTES);
-                        else         mbar_arrive_expect_tx(full, STAGE_BYTES);
-                        if (p.a_mn) {
+                        if (CG == 2) mbar_arrive_expect_tx_cluster(full, stage_bytes);
+                        else         mbar_arrive_expect_tx(full, stage_bytes);
+                        if (MODE == MODE_OUT && q.a_mn) {
 #pragma unroll
-                            for (int j = 0; j < ROWS / MNE; ++j) load(sa + j * MN_BOX, &map_a, m0 * ESZ + j * 128, k * KE);
+                            for (int i = 0; i < ROWS / MNE; ++i) load(sa + i * MN_BOX, ma, m0 * ESZ + i * 128, k * KE);
                         } else {
-                            load(sa, &map_a, k * K_BYTES, m0);
+                            load(sa, ma, k * K_BYTES, m0);
                         }
-                        if (p.b_mn) {
+                        if (MODE == MODE_OUT && q.b_mn) {
 #pragma unroll
-                            for (int j = 0; j < B_ROWS / MNE; ++j) load(sb + j * MN_BOX, &map_b, n0 * ESZ + j * 128, k * KE);
+                            for (int i = 0; i < B_ROWS / MNE; ++i) load(sb + i * MN_BOX, mb, n0 * ESZ + i * 128, k * KE);
                         } else {
-                            load(sb, &map_b, k * K_BYTES, n0);
+                            load(sb, mb, k * K_BYTES, n0);
                         }
                     } else if (CG == 2) {
                         mbar_arrive_cluster(full);                // padding block: nothing to load
@@ -206,19 +241,23 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     }
                 }
                 __syncwarp();
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
         // ---- tensor core (leader only)
         uint32_t stage = 0, phase = 0;
         bool ok = rank == 0;
-        int it = 0;
-        // K-major: groups of 8 rows 1024 B apart, 32 B per step.  MN-major: groups of 8 k 1024 B apart, boxes MN_BOX apart.
-        const uint32_t a_step = p.a_mn ? K_STEP_BYTES / ESZ * 128 : K_STEP_BYTES, a_lbo = p.a_mn ? MN_BOX : 16;
-        const uint32_t b_step = p.b_mn ? K_STEP_BYTES / ESZ * 128 : K_STEP_BYTES, b_lbo = p.b_mn ? MN_BOX : 16;
-        for (int t = worker; t < tiles && ok; t += workers) {
-            const int kb0 = t / plane_tiles * p.slice_blocks, kn = min(p.slice_blocks, k_blocks - kb0);
+        int it = 0, which, t;
+        for (int j = 0; ok && item_at(p, j, worker, workers, which, t); ++j) {
+            const Product& q = p.q[which];
+            // K-major: groups of 8 rows 1024 B apart, 32 B per step.  MN-major: groups of 8 k 1024 B apart, boxes MN_BOX apart.
+            const bool a_mn = MODE == MODE_OUT && q.a_mn, b_mn = MODE == MODE_OUT && q.b_mn;
+            const uint32_t a_step = a_mn ? K_STEP_BYTES / ESZ * 128 : K_STEP_BYTES, a_lbo = a_mn ? MN_BOX : 16;
+            const uint32_t b_step = b_mn ? K_STEP_BYTES / ESZ * 128 : K_STEP_BYTES, b_lbo = b_mn ? MN_BOX : 16;
+            const uint32_t idesc = q.idesc;
+            const int slice = q.slices > 1 ? t / (q.tiles_m * q.tiles_n) : 0;
+            const int kn = min(q.slice_blocks, q.k_blocks - slice * q.slice_blocks);
             const int kn_pad = (kn + FG - 1) / FG * FG;
             for (int kc = 0; kc < kn_pad && ok; kc += SPLIT, ++it) {
                 const uint32_t acc = (uint32_t)it & 1u;
@@ -236,17 +275,19 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         for (int h = 0; h < FG; ++h) {
                             const uint32_t st = stage + h;
                             if (kb + h < kn) {
-                                const uint32_t sa = ring + st * STAGE_BYTES, sb = sa + A_BYTES;
+                                // With few rows A's part of a stage holds those alone, and the rows behind them are whatever
+                                // follows it in the stage: every row of a product is its own, and theirs are not looked at.
+                                const uint32_t sa = ring + st * stage_bytes, sb = sa + a_bytes;
 #pragma unroll
                                 for (int k = 0; k < K_BYTES / K_STEP_BYTES; ++k) {
                                     const uint64_t da = smem_desc(sa + k * a_step, a_lbo, 1024), db = smem_desc(sb + k * b_step, b_lbo, 1024);
                                     const uint32_t more = ((kb - kc) | h | k) != 0 ? 1u : 0u;
                                     if (ESZ == 1) {
-                                        if (CG == 2) tc_mma_f8_pair(tmem_d, da, db, p.idesc, more);
-                                        else         tc_mma_f8(tmem_d, da, db, p.idesc, more);
+                                        if (CG == 2) tc_mma_f8_pair(tmem_d, da, db, idesc, more);
+                                        else         tc_mma_f8(tmem_d, da, db, idesc, more);
                                     } else {
-                                        if (CG == 2) mma_bf16_pair(tmem_d, da, db, p.idesc, more);
-                                        else         mma_bf16(tmem_d, da, db, p.idesc, more);
+                                        if (CG == 2) mma_bf16_pair(tmem_d, da, db, idesc, more);
+                                        else         mma_bf16(tmem_d, da, db, idesc, more);
                                     }
                                 }
                             }
@@ -261,7 +302,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     }
                     __syncwarp();
                     stage += FG;
-                    if (stage == STAGES) { stage = 0; phase ^= 1u; }
+                    if (stage == stages) { stage = 0; phase ^= 1u; }
                 }
             }
         }
@@ -269,30 +310,53 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     } else {
         // ---- epilogue: a warp has 32 rows and half of the tile's columns, a thread one row of them
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPILOGUE));
-        const int q = warp & 3, half = (warp - EPI_BASE) >> 2;
-        float alpha = (p.s[0] ? __ldg(p.s[0]) : 1.0f) * (p.s[1] ? __ldg(p.s[1]) : 1.0f);
-        if (MODE == MODE_STATS || MODE == MODE_DZ) alpha *= LOG2E;
-        const float dz_scale = MODE == MODE_DZ && p.dz_scale ? __ldg(p.dz_scale) : 1.0f;
+        const int q4 = warp & 3, half = (warp - EPI_BASE) >> 2;
+        float dz_scale = 1.0f;
+        if (MODE == MODE_DZ && ESZ == 1) {
+            // the scale of dz's codes: |dz| is at most the |dloss| of a token that counts
+            uint32_t bits = 0u;
+#pragma unroll 4
+            for (int64_t i = threadIdx.x - 32 * EPI_BASE; i < p.q[0].M; i += 32 * EPI_WARPS) {
+                const int64_t target = __ldg(p.target + i);
+                const uint32_t b = __float_as_uint(__ldg(p.dloss + i)) & 0x7FFFFFFFu;
+                if (target >= 0 && target < p.vocab) bits = max(bits, b);
+            }
+            bits = warp_max_u32(bits);
+            if (lane == 0) bars->most[warp - EPI_BASE] = bits;
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
+#pragma unroll
+            for (int i = 0; i < EPI_WARPS; ++i) bits = max(bits, bars->most[i]);
+            const float a = __uint_as_float(bits);                // a NaN is above every number
+            if (a > 0.0f && a <= 3.402823466e38f) dz_scale = fminf(57344.0f / a, 3.402823466e38f);
+            if (blockIdx.x == 0 && threadIdx.x == 32 * EPI_BASE) {
+                p.dz_scale[0] = dz_scale;
+                p.dz_scale[1] = 1.0f / dz_scale;
+            }
+        }
         const uint32_t box = ring + RING_BYTES + (uint32_t)(warp - EPI_BASE) * BOX_BYTES;
         const uint32_t box_row = box + lane * 128;
         const uint64_t out_policy = MODE == MODE_DZ ? policy_evict_last() : policy_evict_first();      // dz is read next
         bool ok = true;
-        int it = 0;
+        int it = 0, which, t;
         float v[NC];
-        for (int t = worker; t < tiles && ok; t += workers) {
+        for (int j = 0; ok && item_at(p, j, worker, workers, which, t); ++j) {
+            const Product& q = p.q[which];
+            const CUtensorMap* md = which ? &map_d1 : &map_d;
             int tm, tn;
-            const int slice = t / plane_tiles;
-            tile_at(t - slice * plane_tiles, p.tiles_m, p.tiles_n, tm, tn);
-            const int kb0 = slice * p.slice_blocks, kn = min(p.slice_blocks, k_blocks - kb0);
+            const int plane_tiles = q.tiles_m * q.tiles_n, slice = q.slices > 1 ? t / plane_tiles : 0;
+            tile_at(t - slice * plane_tiles, q.tiles_m, q.tiles_n, tm, tn);
+            const int kb0 = slice * q.slice_blocks, kn = min(q.slice_blocks, q.k_blocks - kb0);
             const int kn_pad = (kn + FG - 1) / FG * FG;
-            const int64_t row0 = ((int64_t)tm * CG + rank) * ROWS + q * 32, row = row0 + lane;
+            const int64_t row0 = ((int64_t)tm * CG + rank) * ROWS + q4 * 32, row = row0 + lane;
             const int64_t col0 = (int64_t)tn * BN + half * NC;                 // first column of this warp
-            const bool row_ok = row < p.M;
-            const int cols = (int)max((int64_t)0, min((int64_t)NC, p.N - col0));
+            const bool row_ok = row < q.M;
+            const int cols = (int)max((int64_t)0, min((int64_t)NC, q.N - col0));
+            float alpha = (q.s[0] ? __ldg(q.s[0]) : 1.0f) * (q.s[1] ? __ldg(q.s[1]) : 1.0f);
+            if (MODE != MODE_OUT) alpha *= LOG2E;
             int rel = -1;                                         // the target's column among this thread's, if it is there
             bool counted = false;
             float g = 0.0f, lse2 = 0.0f;
-            if ((MODE == MODE_STATS || MODE == MODE_DZ) && row_ok) {
+            if (MODE != MODE_OUT && row_ok) {
                 const int64_t target = __ldg(p.target + row), at = target - p.first - col0;
                 counted = target >= 0 && target < p.vocab;
                 if (at >= 0 && at < cols) rel = (int)at;
@@ -306,16 +370,20 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 ok = mbar_wait(smem_u32(&bars->acc_full[acc]), ((uint32_t)it >> 1) & 1u, abort_flag, L_WAIT_ACC_FULL);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q * 32) << 16) + half * NC;
-                const bool more = kc != 0;
+                const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q4 * 32) << 16) + half * NC;
 #pragma unroll
                 for (int c = 0; c < NC; c += 64) {                // two loads in flight, one wait for both
                     uint32_t r[2][32];
                     tc_ld32(taddr + c, r[0]);
                     tc_ld32(taddr + c + 32, r[1]);
                     tc_wait_ld();
+                    if (kc == 0) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) v[c + i] = (more ? v[c + i] : 0.0f) + __uint_as_float(r[i >> 5][i & 31]);
+                        for (int i = 0; i < 64; ++i) v[c + i] = __uint_as_float(r[i >> 5][i & 31]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) v[c + i] += __uint_as_float(r[i >> 5][i & 31]);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -326,14 +394,16 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             }
             if (!ok) break;
             if (MODE == MODE_STATS) {
-                if (row0 >= p.M) continue;                        // the whole warp
+                if (row0 >= q.M) continue;                        // the whole warp
                 float top = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    v[i] *= alpha;
-                    if (i >= cols) v[i] = -INFINITY;
-                    top = fmaxf(top, v[i]);
+                for (int i = 0; i < NC; ++i) v[i] *= alpha;
+                if (cols < NC) {                                  // the tile at the right edge
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) v[i] = i < cols ? v[i] : -INFINITY;
                 }
+#pragma unroll
+                for (int i = 0; i < NC; ++i) top = fmaxf(top, v[i]);
                 if (__any_sync(0xFFFFFFFFu, rel >= 0)) {
                     float z = 0.0f;
 #pragma unroll
@@ -345,82 +415,88 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int i = 0; i < NC; ++i) s[i & 3] += exp2_fast(v[i] - shift);
-                if (row_ok) p.part[(int64_t)(2 * tn + half) * p.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+                if (row_ok) p.part[(int64_t)(2 * tn + half) * q.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
                 continue;
             }
-            constexpr int OSZ = MODE == MODE_DZ ? ESZ : MODE == MODE_BF16 ? 2 : 4;
-            constexpr int BOX_COLS = 128 / OSZ, SUBS = BOX_COLS / 32, WORDS = 8 * OSZ;
+            // OSZ bytes of an element in boxes of 128 bytes a row
+            auto store = [&](auto size) {
+                constexpr int OSZ = decltype(size)::value;
+                constexpr int BOX_COLS = 128 / OSZ, SUBS = BOX_COLS / 32, WORDS = 8 * OSZ;
 #pragma unroll
-            for (int c = 0; c < NC; c += BOX_COLS) {
-                const int64_t col = col0 + c;
-                // A box over the right edge is clipped by the TMA unit in units of 16 bytes: where rows end elsewhere, plain
-                // stores write it.  dz and the planes of dx have rows of whole boxes.
-                const bool by_hand = (MODE == MODE_BF16 || MODE == MODE_F32) && p.ragged && col + BOX_COLS > p.N;
-                if (!by_hand) {
-                    if (lane == 0) bulk_wait_read<0>();
-                    __syncwarp();
-                }
+                for (int c = 0; c < NC; c += BOX_COLS) {
+                    const int64_t col = col0 + c;
+                    // A box over the right edge is clipped by the TMA unit in units of 16 bytes: where rows end elsewhere, plain
+                    // stores write it.  dz and the planes of dx have rows of whole boxes.
+                    const bool by_hand = MODE == MODE_OUT && q.ragged && col + BOX_COLS > q.N;
+                    if (!by_hand) {
+                        if (lane == 0) bulk_wait_read<0>();
+                        __syncwarp();
+                    }
 #pragma unroll
-                for (int sub = 0; sub < SUBS; ++sub) {
-                    float y[32];
-                    uint32_t w[WORDS];
-                    const int base = c + sub * 32;
-                    if (MODE == MODE_DZ) {
+                    for (int sub = 0; sub < SUBS; ++sub) {
+                        float y[32];
+                        uint32_t w[WORDS];
+                        const int base = c + sub * 32;
+                        if (MODE == MODE_DZ) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) y[i] = exp2_fast(fmaf(v[base + i], alpha, -lse2));
-                        if (__any_sync(0xFFFFFFFFu, rel >= base && rel < base + 32)) {
+                            for (int i = 0; i < 32; ++i) y[i] = exp2_fast(fmaf(v[base + i], alpha, -lse2));
+                            if (__any_sync(0xFFFFFFFFu, rel >= base && rel < base + 32)) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] -= base + i == rel ? 1.0f : 0.0f;
+                                for (int i = 0; i < 32; ++i) y[i] -= base + i == rel ? 1.0f : 0.0f;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[i] *= g;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[i] = v[base + i] * alpha;
                         }
+                        if (OSZ == 4) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) y[i] *= g;
-                    } else {
+                            for (int i = 0; i < WORDS; ++i) w[i] = __float_as_uint(y[i % 32]);
+                        } else if (OSZ == 2) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) y[i] = v[base + i] * alpha;
-                    }
-                    if (OSZ == 4) {
+                            for (int i = 0; i < WORDS; ++i) w[i] = pack_bf16(y[2 * i % 32], y[(2 * i + 1) % 32]);
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < WORDS; ++i) w[i] = __float_as_uint(y[i % 32]);
-                    } else if (OSZ == 2) {
+                            for (int i = 0; i < WORDS; ++i) w[i] = cvt_quad<kE5M2>(y[4 * i % 32], y[(4 * i + 1) % 32], y[(4 * i + 2) % 32], y[(4 * i + 3) % 32]);
+                        }
+                        if (MODE == MODE_DZ && !counted) {        // whatever its logits are
 #pragma unroll
-                        for (int i = 0; i < WORDS; ++i) w[i] = pack_bf16(y[2 * i % 32], y[(2 * i + 1) % 32]);
-                    } else {
+                            for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+                        }
+                        if (by_hand) {
+                            if (row_ok) {
 #pragma unroll
-                        for (int i = 0; i < WORDS; ++i) w[i] = cvt_quad<kE5M2>(y[4 * i % 32], y[(4 * i + 1) % 32], y[(4 * i + 2) % 32], y[(4 * i + 3) % 32]);
-                    }
-                    if (MODE == MODE_DZ && !counted) {            // whatever its logits are
+                                for (int i = 0; i < 32; ++i) {
+                                    if (col + sub * 32 + i >= q.N) continue;
+                                    const int64_t at = row * q.ldd + col + sub * 32 + i;
+                                    if (OSZ == 4) reinterpret_cast<uint32_t*>(q.D)[at] = w[i % WORDS];
+                                    else          reinterpret_cast<uint16_t*>(q.D)[at] = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
+                                }
+                            }
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < WORDS; ++i) w[i] = 0u;
-                    }
-                    if (by_hand) {
-                        if (row_ok) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                if (col + sub * 32 + i >= p.N) continue;
-                                const int64_t at = row * p.ldd + col + sub * 32 + i;
-                                if (OSZ == 4) reinterpret_cast<uint32_t*>(p.D)[at] = w[i % WORDS];
-                                else          reinterpret_cast<uint16_t*>(p.D)[at] = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
+                            for (int i = 0; i < WORDS / 4; ++i) {
+                                const int pos = sub * (WORDS / 4) + i;
+                                st_shared_v4(box_row + ((pos ^ (lane & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                             }
                         }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < WORDS / 4; ++j) {
-                            const int pos = sub * (WORDS / 4) + j;
-                            st_shared_v4(box_row + ((pos ^ (lane & 7)) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                    }
+                    if (by_hand) continue;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (row0 < q.M && col < q.N) {
+                            if (OSZ == 4 && q.out == OUT_ADDED) tma_add_3d(md, box, (int)col, (int)row0, slice);
+                            else                                tma_store_3d(md, box, (int)(col * OSZ), (int)row0, slice, out_policy);
                         }
+                        bulk_commit();
                     }
                 }
-                if (by_hand) continue;
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    if (row0 < p.M && col < p.N) {
-                        if (MODE == MODE_ADD) tma_add_3d(&map_d, box, (int)col, (int)row0, slice);
-                        else                  tma_store_3d(&map_d, box, (int)(col * OSZ), (int)row0, slice, out_policy);
-                    }
-                    bulk_commit();
-                }
-            }
+            };
+            if (MODE == MODE_DZ) store(std::integral_constant<int, ESZ>());
+            else if (q.out == OUT_ROUNDED) store(std::integral_constant<int, 2>());
+            else store(std::integral_constant<int, 4>());
         }
         if (MODE != MODE_STATS && lane == 0) bulk_wait_all();
     }
@@ -435,66 +511,46 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
 }
 
-// Joins the pairs of 32 rows: lane = row, the warps take every 32nd pair, then a warp joins what the warps have of a row.
-__global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const float* logit, int64_t parts, int64_t M,
+// Joins the pairs of a row.  A block has `rows` rows, a power of two up to 32 that spares few rows nothing but their share of the
+// threads: each row has 1024 / rows threads, which take every so-many-th pair and join theirs in a tree.
+__global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const float* logit, int64_t parts, int64_t M, int rows,
                                                     const int64_t* target, int64_t vocab, float* loss, float* lse) {
-    __shared__ float2 got[32][33];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ float2 got[1024];
+    const int row_in = threadIdx.x & (rows - 1), across = 1024 / rows, slot = threadIdx.x / rows;
     grid_launch_dependents();
     grid_dependency_wait();
     auto join = [](float2 a, float2 b) {
         const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
         return make_float2(top, a.y * exp2_fast(a.x - shift) + b.y * exp2_fast(b.x - shift));
     };
-    const int64_t mine = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t row = (int64_t)blockIdx.x * rows + row_in;
     float2 sum = make_float2(-INFINITY, 0.0f);
-    if (mine < M) {
-        for (int64_t i0 = warp; i0 < parts; i0 += 32 * 8) {
+    if (row < M) {
+        for (int64_t i0 = slot; i0 < parts; i0 += across * 8) {
             float2 w[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = i0 + 32 * j < parts ? part[(i0 + 32 * j) * M + mine] : make_float2(-INFINITY, 0.0f);
+            for (int j = 0; j < 8; ++j) w[j] = i0 + across * j < parts ? part[(i0 + across * j) * M + row] : make_float2(-INFINITY, 0.0f);
+            float top = sum.x;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = join(sum, w[j]);
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, w[j].x);
+            const float shift = top == -INFINITY ? 0.0f : top;
+            float s = sum.y * exp2_fast(sum.x - shift);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += w[j].y * exp2_fast(w[j].x - shift);
+            sum = make_float2(top, s);
         }
     }
-    got[warp][lane] = sum;
-    __syncthreads();
-    sum = got[lane][warp];
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const float2 other = make_float2(__shfl_xor_sync(0xFFFFFFFFu, sum.x, d), __shfl_xor_sync(0xFFFFFFFFu, sum.y, d));
-        sum = join(sum, other);
+    got[threadIdx.x] = sum;
+    for (int d = 512; d >= rows; d >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < d) got[threadIdx.x] = sum = join(sum, got[threadIdx.x + d]);
     }
-    const int64_t row = (int64_t)blockIdx.x * 32 + warp;
-    if (lane == 0 && row < M) {
-        const float l2 = sum.x + log2f(sum.y);
+    if (threadIdx.x < rows && row < M) {
+        const float l2 = log2f(sum.y);
         const int64_t t = target[row];
-        lse[row] = l2 * LN2;
-        loss[row] = t >= 0 && t < vocab ? (l2 - logit[row]) * LN2 : 0.0f;
-    }
-}
-
-// The scale of dz's codes: |dz| is at most |dloss| of a counted token.  out[0] = scale, out[1] = 1 / scale.
-__global__ void __launch_bounds__(1024) k_dz_scale(const float* dloss, const int64_t* target, int64_t M, int64_t vocab, float* out) {
-    __shared__ uint32_t most[32];
-    grid_launch_dependents();
-    grid_dependency_wait();
-    uint32_t bits = 0u;
-    for (int64_t i = threadIdx.x; i < M; i += 1024) {
-        const int64_t t = target[i];
-        if (t >= 0 && t < vocab) bits = max(bits, canonical_nan_bits(__float_as_uint(dloss[i]) & 0x7FFFFFFFu));
-    }
-    bits = warp_max_u32(bits);
-    if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = bits;
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        const float a = __uint_as_float(warp_max_u32(most[threadIdx.x]));
-        if (threadIdx.x == 0) {
-            float s = 1.0f;
-            if (a > 0.0f && a <= 3.402823466e38f) s = fminf(57344.0f / a, 3.402823466e38f);
-            out[0] = s;
-            out[1] = 1.0f / s;
-        }
+        lse[row] = (sum.x + l2) * LN2;
+        // the largest logit and the target's are near each other where the loss is small: their difference first
+        loss[row] = t >= 0 && t < vocab ? ((sum.x - logit[row]) + l2) * LN2 : 0.0f;
     }
 }
 
@@ -544,8 +600,10 @@ struct Operand {
     bool mn;
 };
 
+struct Maps { CUtensorMap a, b, d; };
+
 template <int ESZ, int CG, int BN, int MODE>
-static fp8_status launch(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& md, const Params& p, int64_t tiles, cudaStream_t st) {
+static fp8_status launch(const Maps* m, Params p, cudaStream_t st) {
     auto k = k_vocabulary<ESZ, CG, BN, MODE>;
     constexpr int MAX_DEVICES = 64;
     static std::mutex mu;
@@ -578,9 +636,18 @@ static fp8_status launch(const CUtensorMap& ma, const CUtensorMap& mb, const CUt
             if (dev >= 0 && dev < MAX_DEVICES) cached_workers[dev] = workers;
         }
     }
+    const int64_t tiles = (int64_t)p.q[0].tiles + (p.products > 1 ? p.q[1].tiles : 0);
     if ((int64_t)workers > tiles) workers = (int)tiles;
+    p.full = p.q[0].tiles / workers;
+    p.rest = p.q[0].tiles % workers;
+    p.extra = 0;
+    if (p.products > 1 && p.rest > 0) {                           // a last round of the first product lasts as long as so many tiles of the second
+        const int others = workers - p.rest, lasts = (p.q[0].slice_blocks + p.q[1].slice_blocks / 2) / p.q[1].slice_blocks;
+        p.extra = lasts < p.q[1].tiles / others ? lasts : p.q[1].tiles / others;
+    }
     cfg.gridDim = dim3(workers * CG);
-    if (cudaLaunchKernelEx(&cfg, k, ma, mb, md, p) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
+    const Maps& m1 = m[p.products - 1];
+    if (cudaLaunchKernelEx(&cfg, k, m[0].a, m[0].b, m[0].d, m1.a, m1.b, m1.d, p) != cudaSuccess) { (void)cudaGetLastError(); return FP8_ERR_CUDA; }
     count_launches(1);
     return launch_status();
 }
@@ -604,37 +671,59 @@ static int few_rows_width(int64_t N) {
     return narrow < wide ? 128 : 256;
 }
 
-// One product of the kernel above: p holds M, N, K, the factors, the output and what its mode reads.
-template <int MODE>
-static fp8_status product(int esz, int fa, int fb, const Operand& A, const Operand& B, int64_t out_cols, int out_size, Params p, cudaStream_t st) {
-    const int cg = p.M > ROWS ? 2 : 1;
-    const int bn = MODE == MODE_STATS && cg == 1 ? few_rows_width(p.N) : 256;
+// Fills in what follows from a product's sizes, layouts and formats, and its tensor maps.  q holds M, N, K, the factors, D, ldd,
+// `out` and the wanted slices; a_rows: rows of A that a CTA loads.
+static bool lay_out(Product& q, Maps& m, int esz, int fa, int fb, const Operand& A, const Operand& B, int cg, int bn, int a_rows, int64_t out_cols, int out_size) {
     const int ke = K_BYTES / esz;
-    CUtensorMap ma, mb, md;
-    auto map = [&](CUtensorMap* m, const Operand& o, int64_t mn, uint32_t rows) {
-        return o.mn ? make_map(m, o.p, (uint64_t)(mn * esz), (uint64_t)p.K, (uint64_t)(o.ld * esz), 1, 0, 128, (uint32_t)ke)
-                    : make_map(m, o.p, (uint64_t)(p.K * esz), (uint64_t)mn, (uint64_t)(o.ld * esz), 1, 0, K_BYTES, rows);
+    auto map = [&](CUtensorMap* t, const Operand& o, int64_t mn, int rows) {
+        return o.mn ? make_map(t, o.p, (uint64_t)(mn * esz), (uint64_t)q.K, (uint64_t)(o.ld * esz), 1, 0, 128, (uint32_t)ke)
+                    : make_map(t, o.p, (uint64_t)(q.K * esz), (uint64_t)mn, (uint64_t)(o.ld * esz), 1, 0, K_BYTES, (uint32_t)rows);
     };
-    if (!map(&ma, A, p.M, ROWS) || !map(&mb, B, p.N, (uint32_t)(bn / cg))) return FP8_ERR_CUDA;
-    if (MODE == MODE_STATS) md = ma;                              // not used
-    else if (!make_plane_map(&md, p.D, out_cols, p.M, p.ldd, p.slices, out_size, MODE == MODE_ADD)) return FP8_ERR_CUDA;
-    p.ragged = (out_cols * out_size & 15) != 0 ? 1 : 0;
-    p.a_mn = A.mn ? 1 : 0;
-    p.b_mn = B.mn ? 1 : 0;
-    p.tiles_m = (int)((p.M + ROWS * cg - 1) / (ROWS * cg));
-    p.tiles_n = (int)((p.N + bn - 1) / bn);
-    const int64_t blocks = (p.K + ke - 1) / ke;
-    p.slice_blocks = (int)((blocks + p.slices - 1) / p.slices);
-    p.slices = (int)((blocks + p.slice_blocks - 1) / p.slice_blocks);
+    if (!map(&m.a, A, q.M, a_rows) || !map(&m.b, B, q.N, bn / cg)) return false;
+    if (!q.D) m.d = m.a;                                          // nothing is stored through it
+    else if (!make_plane_map(&m.d, q.D, out_cols, q.M, q.ldd, q.slices, out_size, q.out == OUT_ADDED)) return false;
+    q.ragged = (out_cols * out_size & 15) != 0 ? 1 : 0;
+    q.a_mn = A.mn ? 1 : 0;
+    q.b_mn = B.mn ? 1 : 0;
+    q.tiles_m = (int)((q.M + ROWS * cg - 1) / (ROWS * cg));
+    q.tiles_n = (int)((q.N + bn - 1) / bn);
+    q.k_blocks = (int)((q.K + ke - 1) / ke);
+    q.slice_blocks = (q.k_blocks + q.slices - 1) / q.slices;
+    q.slices = (q.k_blocks + q.slice_blocks - 1) / q.slice_blocks;
+    q.tiles = q.tiles_m * q.tiles_n * q.slices;
     // binary32 accumulator; formats (bf16 is 1), layouts, N / 8, M / 16
-    p.idesc = (1u << 4) | ((uint32_t)(esz == 2 ? 1 : fa) << 7) | ((uint32_t)(esz == 2 ? 1 : fb) << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
+    q.idesc = (1u << 4) | ((uint32_t)(esz == 2 ? 1 : fa) << 7) | ((uint32_t)(esz == 2 ? 1 : fb) << 10) | ((uint32_t)q.a_mn << 15) | ((uint32_t)q.b_mn << 16) |
               ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(ROWS * cg >> 4) << 24);
-    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.slices;
-    if (cg == 2) return esz == 1 ? launch<1, 2, 256, MODE>(ma, mb, md, p, tiles, st) : launch<2, 2, 256, MODE>(ma, mb, md, p, tiles, st);
+    return true;
+}
+
+// The product x . w^T with the epilogue of MODE_STATS or MODE_DZ (D: dz, of pitch q.ldd = out_cols).
+template <int MODE>
+static fp8_status logits(const fp8_cross_entropy_desc* d, const void* x, const void* w, Params& p, cudaStream_t st) {
+    Product& q = p.q[0];
+    const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
+    const int cg = q.M > ROWS ? 2 : 1, bn = MODE == MODE_STATS && cg == 1 ? few_rows_width(q.N) : 256;
+    const int a_rows = cg == 2 ? ROWS : (int)round_up(q.M, 8);
+    Maps m;
+    q.slices = 1;
+    if (!lay_out(q, m, esz, d->x_t, d->w_t, Operand{x, d->ldx, false}, Operand{w, d->ldw, false}, cg, bn, a_rows, q.ldd, esz)) return FP8_ERR_CUDA;
+    p.products = 1;
+    p.a_bytes = (uint32_t)a_rows * K_BYTES;
+    p.stages = (int)(RING_BYTES / (p.a_bytes + (uint32_t)(bn / cg) * K_BYTES)) / FG * FG;
+    if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+    if (cg == 2) return esz == 1 ? launch<1, 2, 256, MODE>(&m, p, st) : launch<2, 2, 256, MODE>(&m, p, st);
     if constexpr (MODE == MODE_STATS) {
-        if (bn == 128) return esz == 1 ? launch<1, 1, 128, MODE>(ma, mb, md, p, tiles, st) : launch<2, 1, 128, MODE>(ma, mb, md, p, tiles, st);
+        if (bn == 128) return esz == 1 ? launch<1, 1, 128, MODE>(&m, p, st) : launch<2, 1, 128, MODE>(&m, p, st);
     }
-    return esz == 1 ? launch<1, 1, 256, MODE>(ma, mb, md, p, tiles, st) : launch<2, 1, 256, MODE>(ma, mb, md, p, tiles, st);
+    return esz == 1 ? launch<1, 1, 256, MODE>(&m, p, st) : launch<2, 1, 256, MODE>(&m, p, st);
+}
+
+// One product, or two in one launch.
+static fp8_status products(int esz, int cg, const Maps* m, Params& p, cudaStream_t st) {
+    p.a_bytes = A_BYTES;
+    p.stages = (int)(RING_BYTES / (A_BYTES + 256 * K_BYTES)) / FG * FG;
+    if (cg == 2) return esz == 1 ? launch<1, 2, 256, MODE_OUT>(m, p, st) : launch<2, 2, 256, MODE_OUT>(m, p, st);
+    return esz == 1 ? launch<1, 1, 256, MODE_OUT>(m, p, st) : launch<2, 1, 256, MODE_OUT>(m, p, st);
 }
 
 template <typename... KArgs, typename... Args>
@@ -748,18 +837,18 @@ fp8_status fp8_cross_entropy(const fp8_cross_entropy_desc* d, const void* x, con
     if (workspace_bytes < forward_bytes(T, V)) return FP8_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) return FP8_ERR_ALIGN;
     cudaStream_t st = (cudaStream_t)stream;
-    const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
     Params p = {};
-    p.M = T; p.N = V; p.K = d->width;
-    p.s[0] = scale_inv_x_dev; p.s[1] = scale_inv_w_dev;
-    p.slices = 1;
+    Product& q = p.q[0];
+    q.M = T; q.N = V; q.K = d->width;
+    q.s[0] = scale_inv_x_dev; q.s[1] = scale_inv_w_dev;
     p.target = target_dev; p.vocab = V;
     p.part = reinterpret_cast<float2*>(workspace_dev);
     p.logit = reinterpret_cast<float*>(p.part + parts_of(T, V) * T);
-    const int bn = T > ROWS ? 256 : few_rows_width(V);
-    if ((rc = product<MODE_STATS>(esz, d->x_t, d->w_t, Operand{x, d->ldx, false}, Operand{w, d->ldw, false}, 0, 0, p, st)) != FP8_OK) return rc;
-    return launch_small(k_loss_join, (unsigned)((T + 31) / 32), 1024u, st, (const float2*)p.part, (const float*)p.logit, 2 * ((V + bn - 1) / bn), T, target_dev, V,
-                        loss_dev, lse_dev);
+    if ((rc = logits<MODE_STATS>(d, x, w, p, st)) != FP8_OK) return rc;
+    int rows = 32;
+    while (rows > T) rows /= 2;
+    return launch_small(k_loss_join, (unsigned)((T + rows - 1) / rows), 1024u, st, (const float2*)p.part, (const float*)p.logit, (int64_t)q.tiles_n * 2, T, rows,
+                        target_dev, V, loss_dev, lse_dev);
 }
 
 fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const void* x, const void* w, const float* scale_inv_x_dev, const float* scale_inv_w_dev,
@@ -797,46 +886,47 @@ fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const voi
     float* scale = reinterpret_cast<float*>(ws);
     void* dz = ws + 256;
     float* planes = reinterpret_cast<float*>(ws + 256 + c.z_bytes);
-    if (esz == 1 && (rc = launch_small(k_dz_scale, 1u, 1024u, st, dloss_dev, target_dev, T, V, scale)) != FP8_OK) return rc;
     const float* back = esz == 1 ? scale + 1 : nullptr;
-    const int fz = FP8_E5M2;
+    const int fz = FP8_E5M2, cg = T > ROWS ? 2 : 1;
     for (int i = 0; i < c.pieces; ++i) {
         const int64_t v0 = i * c.cols, cols = V - v0 < c.cols ? V - v0 : c.cols;
         const uint8_t* wp = reinterpret_cast<const uint8_t*>(w) + v0 * d->ldw * esz;
         Params z = {};
-        z.M = T; z.N = cols; z.K = K;
-        z.s[0] = scale_inv_x_dev; z.s[1] = scale_inv_w_dev;
-        z.slices = 1;
-        z.D = dz; z.ldd = c.pitch_z;
+        z.q[0].M = T; z.q[0].N = cols; z.q[0].K = K;
+        z.q[0].s[0] = scale_inv_x_dev; z.q[0].s[1] = scale_inv_w_dev;
+        z.q[0].D = dz; z.q[0].ldd = c.pitch_z;
         z.target = target_dev; z.first = v0; z.vocab = V;
-        z.lse = lse_dev; z.dloss = dloss_dev; z.dz_scale = esz == 1 ? scale : nullptr;
-        if ((rc = product<MODE_DZ>(esz, d->x_t, d->w_t, Operand{x, d->ldx, false}, Operand{wp, d->ldw, false}, c.pitch_z, esz, z, st)) != FP8_OK) return rc;
+        z.lse = lse_dev; z.dloss = dloss_dev; z.dz_scale = scale;
+        if ((rc = logits<MODE_DZ>(d, x, wp, z, st)) != FP8_OK) return rc;
+        // the two products that read dz: one launch
+        Product of_x = {}, of_w = {};
+        Maps mx, mw;
         if (dx) {
-            Params p = {};
-            p.M = T; p.N = K; p.K = cols;
-            p.s[0] = back; p.s[1] = scale_inv_w_dev;
+            of_x.M = T; of_x.N = K; of_x.K = cols;
+            of_x.s[0] = back; of_x.s[1] = scale_inv_w_dev;
+            of_x.slices = c.slices;
             const Operand A{dz, c.pitch_z, false}, B{wp, d->ldw, true};
-            if (c.planes) {
-                p.slices = c.slices;
-                p.D = planes; p.ldd = c.pitch_x;
-                rc = i == 0 ? product<MODE_F32>(esz, fz, d->w_t, A, B, c.pitch_x, 4, p, st) : product<MODE_ADD>(esz, fz, d->w_t, A, B, c.pitch_x, 4, p, st);
-            } else {
-                p.slices = 1;
-                p.D = dx; p.ldd = lddx;
-                rc = dx_t == FP8_BF16 ? product<MODE_BF16>(esz, fz, d->w_t, A, B, K, 2, p, st) : product<MODE_F32>(esz, fz, d->w_t, A, B, K, 4, p, st);
-            }
-            if (rc != FP8_OK) return rc;
+            of_x.out = c.planes ? (i == 0 ? OUT_WIDE : OUT_ADDED) : dx_t == FP8_BF16 ? OUT_ROUNDED : OUT_WIDE;
+            of_x.D = c.planes ? planes : dx;
+            of_x.ldd = c.planes ? c.pitch_x : lddx;
+            if (!lay_out(of_x, mx, esz, fz, d->w_t, A, B, cg, 256, ROWS, c.planes ? c.pitch_x : K, of_x.out == OUT_ROUNDED ? 2 : 4)) return FP8_ERR_CUDA;
         }
         if (dw) {
-            Params p = {};
-            p.M = cols; p.N = K; p.K = T;
-            p.s[0] = back; p.s[1] = scale_inv_x_dev;
-            p.slices = 1;
-            p.D = reinterpret_cast<uint8_t*>(dw) + v0 * lddw * wo; p.ldd = lddw;
+            of_w.M = cols; of_w.N = K; of_w.K = T;
+            of_w.s[0] = back; of_w.s[1] = scale_inv_x_dev;
+            of_w.slices = 1;
+            of_w.D = reinterpret_cast<uint8_t*>(dw) + v0 * lddw * wo; of_w.ldd = lddw;
+            of_w.out = dw_t == FP8_BF16 ? OUT_ROUNDED : OUT_WIDE;
             const Operand A{dz, c.pitch_z, true}, B{x, d->ldx, true};
-            rc = dw_t == FP8_BF16 ? product<MODE_BF16>(esz, fz, d->x_t, A, B, K, 2, p, st) : product<MODE_F32>(esz, fz, d->x_t, A, B, K, 4, p, st);
-            if (rc != FP8_OK) return rc;
+            if (!lay_out(of_w, mw, esz, fz, d->x_t, A, B, cg, 256, ROWS, K, wo)) return FP8_ERR_CUDA;
         }
+        Params p = {};
+        Maps m[2];
+        const bool x_first = dx && (!dw || of_x.slice_blocks >= of_w.slice_blocks);      // the longer K first
+        p.products = dx && dw ? 2 : 1;
+        p.q[0] = x_first ? of_x : of_w; m[0] = x_first ? mx : mw;
+        p.q[1] = x_first ? of_w : of_x; m[1] = x_first ? mw : mx;
+        if ((rc = products(esz, cg, m, p, st)) != FP8_OK) return rc;
     }
     if (dx && c.planes) {
         const int64_t octets = T * ((K + 7) / 8);
