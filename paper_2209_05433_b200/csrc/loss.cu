@@ -771,7 +771,7 @@ static Cut cut_of(int64_t T, int64_t K, int64_t V, int esz) {
     return c;
 }
 
-static int64_t parts_of(int64_t T, int64_t V) { return 2 * ((V + 127) / 128); }      // of either tile width
+static int64_t parts_of(int64_t T, int64_t V) { return 2 * (T > ROWS ? (V + 255) / 256 : (V + 127) / 128); }      // few rows: of either tile width
 static size_t forward_bytes(int64_t T, int64_t V) { return T > 0 ? (size_t)parts_of(T, V) * (size_t)T * 8 + (size_t)T * 4 : 0; }
 static size_t backward_bytes(int64_t T, int64_t K, int64_t V, int esz) {
     if (T <= 0) return 0;
@@ -835,7 +835,9 @@ fp8_status fp8_cross_entropy(const fp8_cross_entropy_desc* d, const void* x, con
     if (!target_dev || !loss_dev || !lse_dev || !workspace_dev) return FP8_ERR_NULL;
     if ((rc = check_operands(d, x, w, scale_inv_x_dev, scale_inv_w_dev)) != FP8_OK) return rc;
     if (workspace_bytes < forward_bytes(T, V)) return FP8_ERR_SHAPE;
-    if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) return FP8_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(workspace_dev) & 15u) || (reinterpret_cast<uintptr_t>(target_dev) & 7u) ||
+        ((reinterpret_cast<uintptr_t>(loss_dev) | reinterpret_cast<uintptr_t>(lse_dev)) & 3u))
+        return FP8_ERR_ALIGN;
     cudaStream_t st = (cudaStream_t)stream;
     Params p = {};
     Product& q = p.q[0];
@@ -879,7 +881,9 @@ fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const voi
     if ((rc = check_operands(d, x, w, scale_inv_x_dev, scale_inv_w_dev)) != FP8_OK) return rc;
     const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
     if (workspace_bytes < backward_bytes(T, K, V, esz)) return FP8_ERR_SHAPE;
-    if (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) return FP8_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(workspace_dev) & 15u) || (reinterpret_cast<uintptr_t>(target_dev) & 7u) ||
+        ((reinterpret_cast<uintptr_t>(lse_dev) | reinterpret_cast<uintptr_t>(dloss_dev)) & 3u))
+        return FP8_ERR_ALIGN;
     if (!dx && !dw) return FP8_OK;
     const Cut c = cut_of(T, K, V, esz);
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);

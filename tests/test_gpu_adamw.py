@@ -211,3 +211,151 @@ def test_state_from_zeros_and_zero_gradients():
     api.fp8_adamw_step(api.AdamWPlan([p], [torch.ones(3, device=DEV)], [z(F32, 3)], [z(F32, 3)], copies=[copy], fmt=E4, scales=[_scalar(1.0)], amax_outs=[amax]), 0.5, 1, eps=0.0)
     _ok()
     assert bool(((p - 0.5).abs() < 1e-5).all()) and float(amax) == float(p.abs().max())
+
+
+def test_a_norm_that_is_not_finite_skips_the_step():
+    g = _gen(6)
+    for bad in (float("nan"), float("inf")):
+        ts = [Tensors(n, F32, BF, codes, E4, g, shift=s) for n, s in ((5000, 0), (777, 1)) for codes in (False, True)]
+        count = torch.tensor([4], device=DEV)
+        api.fp8_adamw_step(_plan(ts), 1e-2, count, norm=_scalar(bad), max_norm=1.0)
+        _ok()
+        assert int(count) == 4
+        for t in ts:
+            assert all(torch.equal(getattr(t, k), t.old[k]) for k in ("p", "m", "v"))
+            assert not t.codes or (torch.equal(t.ms, t.old_scales[0]) and torch.equal(t.vs, t.old_scales[1]))
+            _check_copy(t)
+
+
+def test_gradients_that_are_not_finite_without_a_norm():
+    """32-bit moments: their element alone; 8-bit: their block's moments; the rest of the tensor as if nothing had been"""
+    n = 1000
+    for codes in (False, True):
+        a, b = (Tensors(n, F32, F32, codes, None, _gen(8)) for _ in range(2))
+        a.g[300], a.g[700] = float("nan"), float("inf")
+        api.fp8_adamw_step(_plan([a]), 1e-2, 3, seed=5)
+        api.fp8_adamw_step(_plan([b]), 1e-2, 3, seed=5)
+        _ok()
+        hit = torch.zeros(n, dtype=torch.bool, device=DEV)
+        hit[300] = hit[700] = True
+        assert bool(torch.isnan(a.p[hit]).all()) and torch.equal(a.p[~hit], b.p[~hit])
+        if codes:
+            assert bool((~torch.isfinite(a.ms[1:3])).all()) and torch.equal(a.ms[[0, 3]], b.ms[[0, 3]]) and torch.equal(a.v[:256], b.v[:256])
+        else:
+            assert torch.equal(a.m[~hit], b.m[~hit]) and torch.equal(a.v[~hit], b.v[~hit])
+
+
+@pytest.mark.parametrize("codes", [False, True], ids=["32bit", "8bit"])
+def test_second_moments_that_overflow_stop_their_elements(codes):
+    a = Tensors(600, F32, F32, codes, None, _gen(9), decay=0.0)
+    a.g[40] = 1e25
+    api.fp8_adamw_step(_plan([a]), 1e-2, 3, beta2=0.9)
+    _ok()
+    assert bool(torch.isfinite(a.p).all()) and float(a.p[40]) == float(a.old["p"][40])
+
+
+def test_captured_steps_go_on_with_the_counter_and_the_rate():
+    """a replayed step reads its rate and counts for itself: the same bits as plain steps"""
+    make = lambda: [Tensors(n, F32, BF, codes, E4, _gen(20 + n), start=False) for n in (3000, 70000) for codes in (False, True)]  # noqa: E731
+    plain, played = make(), make()
+    plan = _plan(plain)
+    lrs = [1e-3, 2e-3, 5e-4, 1e-3]
+    for i, lr in enumerate(lrs):
+        api.fp8_adamw_step(plan, lr, i + 1, seed=77, norm=_scalar(2.0), max_norm=1.0)
+    plan, lr, count, norm = _plan(played), _scalar(0.0), torch.tensor([0], device=DEV), _scalar(2.0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        api.fp8_adamw_step(plan, lr, count, seed=77, norm=norm, max_norm=1.0)
+    for v in lrs:
+        lr.fill_(v)
+        g.replay()
+    _ok()
+    assert int(count) == len(lrs)
+    for a, b in zip(plain, played):
+        for k in ("p", "m", "v", "copy", "amax"):
+            assert torch.equal(getattr(a, k), getattr(b, k)), k
+        assert not a.codes or (torch.equal(a.ms, b.ms) and torch.equal(a.vs, b.vs))
+
+
+def test_plans_on_two_streams_at_once():
+    sets = [[Tensors(n, F32, BF, True, E4, _gen(30 + n + 7 * i)) for n in (100000, 5000)] for i in range(2)]
+    want = [[Tensors(n, F32, BF, True, E4, _gen(30 + n + 7 * i)) for n in (100000, 5000)] for i in range(2)]
+    for ts in want:
+        plan = _plan(ts)
+        for i in range(6):
+            api.fp8_adamw_step(plan, 1e-3, i + 1, seed=3)
+    torch.cuda.synchronize()
+    plans, streams = [_plan(ts) for ts in sets], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for plan, s in zip(plans, streams):
+            with torch.cuda.stream(s):
+                api.fp8_adamw_step(plan, 1e-3, i + 1, seed=3)
+    _ok()
+    for a, b in zip(sum(sets, []), sum(want, [])):
+        assert all(torch.equal(getattr(a, k), getattr(b, k)) for k in ("p", "m", "v", "ms", "vs", "copy", "amax"))
+
+
+def test_eight_bit_second_moments_follow_their_mean():
+    """With a gradient of constant magnitude r goes to that magnitude, from below and from above, although a step moves it by far
+    less than the distance of two codes.  Rounding by chance leaves the mean of r alone and adds at most step^2 / 4 to the mean
+    of r^2, step <= r / 8, in each step; v forgets (1 - b2) of itself meanwhile, so the mean square is between v and
+    v (1 + b2 / (1 - b2) / 256) = 1.19 v for b2 = 0.98.  The mean over 65536 elements, whose squares scatter by less than v,
+    is within 5 standard deviations, 0.02 v, of its own.  (600 steps: what is left of the start is below 2e-3.)"""
+    n, b2, mag = 65536, 0.98, 3e-4
+    for r0 in (0.0, 4e-3):
+        p, g = torch.zeros(n, device=DEV), torch.full((n,), mag, device=DEV)
+        m, v, ms, vs = torch.zeros(n, dtype=U8, device=DEV), torch.zeros(n, dtype=U8, device=DEV), torch.zeros(256, device=DEV), torch.zeros(256, device=DEV)
+        if r0:
+            v.fill_(0x7E)
+            vs.fill_(r0 / 448)
+        plan = api.AdamWPlan([p], [g], [m], [v], exp_avg_scales=[ms], exp_avg_sq_scales=[vs])
+        for i in range(600):
+            api.fp8_adamw_step(plan, 0.0, i + 1, beta2=b2, seed=11)
+        _ok()
+        r = v.view(F8[E4]).double().view(256, 256) * vs.double()[:, None]
+        want = mag ** 2 + (r0 ** 2 - mag ** 2) * b2 ** 600
+        assert -0.02 <= float(r.square().mean()) / want - 1 <= 0.21
+
+
+def test_more_than_2_to_the_31_parameters():
+    n = 2 ** 31 + 1000
+    z = lambda dt: torch.zeros(n, dtype=dt, device=DEV)  # noqa: E731
+    p, g, m, v = z(BF), z(BF), z(U8), z(U8)
+    blocks = -(-n // 256)
+    ms, vs = torch.zeros(blocks, device=DEV), torch.zeros(blocks, device=DEV)
+    at = [0, 2 ** 31 - 300, 2 ** 31 + 5, n - 1]
+    for i in at:
+        g[i] = 1.0 + i % 7
+    copy, amax = z(U8), _scalar(0.0)
+    api.fp8_adamw_step(api.AdamWPlan([p], [g], [m], [v], exp_avg_scales=[ms], exp_avg_sq_scales=[vs], copies=[copy], fmt=E4, scales=[_scalar(1.0)], amax_outs=[amax]), 0.5, 1)
+    _ok()
+    for i in at:
+        assert abs(float(p[i]) + 0.5) < 0.01 and float(amax) == abs(float(p[i])) and int(copy[i]) == 0xB0 and int(m[i]) == 0x7E and int(v[i]) == 0x7E
+    for t in (p, m, v, copy):
+        assert int(torch.count_nonzero(t)) == len(at)
+
+
+def test_refusals_of_the_binding():
+    f, u = torch.zeros(300, device=DEV), torch.zeros(300, dtype=U8, device=DEV)
+    s = torch.zeros(2, device=DEV)
+    for bad in (dict(exp_avg_scales=[s], exp_avg_sq_scales=[s]), dict(copies=[u]), dict(copies=[u], fmt=7, scales=[_scalar(1.0)]), dict(copies=[f]),
+                dict(copies=[f.to(BF)], scales=[_scalar(1.0)]), dict(scales=[_scalar(1.0)]), dict(copies=[u[:200]], fmt=E4, scales=[_scalar(1.0)])):
+        with pytest.raises((TypeError, ValueError)):
+            api.AdamWPlan([f], [f], [f], [f], **bad)
+    with pytest.raises((TypeError, ValueError)):
+        api.AdamWPlan([f], [f], [u], [u])
+    with pytest.raises((TypeError, ValueError)):
+        api.AdamWPlan([f], [f], [u], [u], exp_avg_scales=[s[:1]], exp_avg_sq_scales=[s])
+    with pytest.raises(ValueError):
+        api.AdamWPlan([f[::2]], [f[::2]], [f[::2]], [f[::2]])
+    plan = api.AdamWPlan([f], [f.clone()], [f.clone()], [f.clone()])
+    for bad in (dict(step=0), dict(step=1, beta1=1.0), dict(step=1, eps=-1.0)):
+        with pytest.raises(api.Fp8Error):
+            api.fp8_adamw_step(plan, 1e-3, **bad)
+    with pytest.raises(ValueError):
+        api.fp8_adamw_step(plan, 1e-3, 1, norm=_scalar(1.0))
+    with pytest.raises(TypeError):
+        api.fp8_adamw_step(plan, 1e-3, torch.zeros(1, device=DEV))
+    _ok()

@@ -164,3 +164,205 @@ def test_backward(case):
     p.backward(dx, None)
     p.backward(None, dw)                                          # one at a time: the same bits
     assert torch.equal(dx, first[0]) and torch.equal(dw, first[1])
+
+
+@pytest.mark.parametrize("shape", [(5, 24, 37), (130, 16, 300)])
+def test_gradients_are_the_derivatives_of_the_loss(shape):
+    """dx and dw against central differences of sum(dloss * loss) in binary64 (step 1e-4: truncation below 1e-8 of the
+    magnitudes): off by the rounding of dz to bf16, 2^-8 of each, and by the bounds above."""
+    T, K, V = shape
+    p = Problem(T, K, V, None, None, ignored=0.0)
+    dx, dw = torch.empty(T, K, device=DEV), torch.empty(V, K, device=DEV)
+    p.forward()
+    p.backward(dx, dw)
+    _ok()
+    x, w, g = p.x64, p.w64, p.dloss.double()
+    z = x @ w.T
+    pr = torch.softmax(z, 1)
+    dz = (pr - torch.nn.functional.one_hot(p.target, V)) * g[:, None]
+
+    def total(x, w):
+        z = x @ w.T
+        return ((torch.logsumexp(z, 1) - z.gather(1, p.target[:, None]).squeeze(1)) * g).sum()
+
+    h, gen = 1e-4, _gen(9)
+    for name, got, a, tol in (("dx", dx, x, dz.abs() @ w.abs()), ("dw", dw, w, dz.abs().T @ x.abs())):
+        for _ in range(20):
+            way = torch.randn(a.shape, generator=gen, device=DEV, dtype=torch.float64)
+            diff = (total(a + h * way, w) - total(a - h * way, w) if name == "dx" else total(x, a + h * way) - total(x, a - h * way)) / (2 * h)
+            bound = 1.05 * 2.0 ** -8 * (tol * way.abs()).sum() + 1e-6
+            assert abs(float((got.double() * way).sum() - diff)) <= float(bound), name
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_special_values(T):
+    """NaN and infinities stay in the rows of the tokens that have them, and out of what does not count"""
+    K, V = 32, 700
+    p = Problem(T, K, V, None, None, ignored=0.0)
+    p.x[0, 3] = float("nan")
+    p.x[1, 0] = float("inf")                                     # logits of both signs, infinite
+    p.target[2] = -100
+    p.forward()
+    assert bool(torch.isnan(p.loss[:2]).all()) and bool(torch.isnan(p.lse[:2]).all())
+    assert float(p.loss[2]) == 0.0 and bool(torch.isfinite(p.lse[2]))
+    assert bool(torch.isfinite(p.loss[2:]).all())
+    p.target[0] = V                                              # the NaN token does not count any more: its loss and its gradient are zero
+    p.forward()
+    assert float(p.loss[0]) == 0.0 and bool(torch.isnan(p.lse[0]))
+    dx = torch.empty(T, K, device=DEV)
+    p.backward(dx, None)
+    _ok()
+    assert not dx[0].any() and bool(torch.isnan(dx[1]).all()) and not dx[2].any()
+    assert bool(torch.isfinite(dx[3:]).all()) and (T == 3 or bool(dx[3:].any()))
+    # a row of logits that are all minus infinity, and one whose logits are as large as they get
+    x, w = torch.zeros(2, 16, device=DEV, dtype=BF), torch.zeros(300, 16, device=DEV, dtype=BF)
+    x[0, 0], x[1, 0] = float("-inf"), 1e18
+    w[:, 0] = 1.0
+    w[7, 0] = 2.0
+    t, loss, lse = torch.tensor([5, 7], device=DEV), torch.empty(2, device=DEV), torch.empty(2, device=DEV)
+    api.fp8_cross_entropy(x, None, w, None, t, loss, lse)
+    _ok()
+    assert float(lse[0]) == float("-inf") and bool(torch.isnan(loss[0]))
+    assert float(loss[1]) == 0.0 and abs(float(lse[1]) / 2e18 - 1) < 0.01
+
+
+def test_nothing_counts_and_nothing_is_there():
+    p = Problem(40, 64, 500, E4, E4, ignored=1.1)
+    (dx, all_dx), (dw, all_dw) = _matrix(40, 64, BF), _matrix(500, 64, BF)
+    p.forward()
+    p.backward(dx, dw)
+    _ok()
+    assert not p.loss.any() and not dx.any() and not dw.any() and bool(torch.isfinite(p.lse).all())
+    none = torch.empty(0, device=DEV)
+    api.fp8_cross_entropy(p.x[:0], E4, p.w, E4, torch.empty(0, dtype=torch.int64, device=DEV), none, none, scale_inv_x=p.sx, scale_inv_w=p.sw)
+    dw.fill_(3.0)
+    api.fp8_cross_entropy_backward(p.x[:0], E4, p.w, E4, torch.empty(0, dtype=torch.int64, device=DEV), none, none, dx[:0], dw, scale_inv_x=p.sx, scale_inv_w=p.sw)
+    _ok()
+    assert not dw.any() and _guards_kept(dw, all_dw)
+
+
+def test_gradient_factors_of_every_size():
+    """dloss of zero, of 1e-30 and of 1e30: the codes' scale follows the largest; not finite: the scale is 1 and the rows say so"""
+    for factor in (1e-30, 1.0, 1e30):
+        p = Problem(64, 96, 300, E4, E4, ignored=0.0)
+        p.dloss.mul_(factor)
+        p.dloss[5] = 0.0
+        dx, dw = torch.empty(64, 96, device=DEV), torch.empty(300, 96, device=DEV)
+        p.forward()
+        p.backward(dx, dw)
+        _ok()
+        p.check_backward(dx, dw)
+        assert not dx[5].any()
+    p.dloss.zero_()
+    p.backward(dx, dw)
+    assert not dx.any() and not dw.any()
+    p.dloss[3] = float("nan")
+    p.backward(dx, None)
+    _ok()
+    assert bool(torch.isnan(dx[3]).all()) and not dx[4:].any()
+
+
+def test_captured_calls_replay_on_new_inputs():
+    """two graphs of the same call, replayed on the inputs of two problems: the bits of plain calls"""
+    problems = [Problem(200, 130, 3000, E4, E4, seed=s) for s in (0, 7)]
+    shape = lambda: (torch.empty(200, 136, dtype=BF, device=DEV)[:, :130], torch.empty(3000, 136, dtype=BF, device=DEV)[:, :130])  # noqa: E731
+    want = []
+    for r in problems:
+        dx, dw = shape()
+        r.forward()
+        r.backward(dx, dw)
+        want.append((r.loss.clone(), dx, dw))
+    p, (dx, dw) = Problem(200, 130, 3000, E4, E4, seed=1), shape()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    _ok()
+    for g in graphs:
+        with torch.cuda.graph(g):
+            p.forward()
+            p.backward(dx, dw)
+    for r, (loss, wx, ww) in zip(problems, want):
+        for to, of in ((p.x, r.x), (p.w, r.w), (p.target, r.target), (p.dloss, r.dloss)):
+            to.copy_(of)
+        for g in graphs:
+            dx.fill_(9.0), dw.fill_(9.0), p.loss.fill_(9.0)
+            g.replay()
+            _ok()
+            assert torch.equal(p.loss, loss) and torch.equal(dx, wx) and torch.equal(dw, ww)
+
+
+def test_two_streams_at_once():
+    a, b = Problem(300, 256, 4000, None, None), Problem(37, 512, 9000, E4, E4)
+    streams, out = (torch.cuda.Stream(), torch.cuda.Stream()), []
+    for r in (a, b):
+        dx, dw = torch.empty(r.T, r.K, dtype=BF, device=DEV), torch.empty(r.V, r.K, dtype=BF, device=DEV)
+        r.forward()
+        r.backward(dx, dw)
+        out.append((r.loss.clone(), dx.clone(), dw.clone()))
+    torch.cuda.synchronize()
+    got = [(torch.empty_like(o[1]), torch.empty_like(o[2])) for o in out]
+    for _ in range(5):
+        for r, s, (dx, dw) in zip((a, b), streams, got):
+            with torch.cuda.stream(s):
+                r.forward()
+                r.backward(dx, dw)
+    _ok()
+    for r, o, (dx, dw) in zip((a, b), out, got):
+        assert torch.equal(r.loss, o[0]) and torch.equal(dx, o[1]) and torch.equal(dw, o[2])
+
+
+def test_rows_that_are_slices_of_wider_ones():
+    """operands and gradients with pitches above their width; single rows and columns of any stride"""
+    T, K, V = 70, 48, 600
+    p = Problem(T, K, V, E4, E4)
+    wide = torch.full((T, 256), 0x7F, dtype=torch.uint8, device=DEV)
+    wide[:, 64:64 + K] = p.x
+    dx_all = torch.full((T, 128), 5.0, device=DEV, dtype=BF)
+    dx, dw, flat = dx_all[:, 16:16 + K], torch.empty(V, K, device=DEV), torch.empty(T, K, device=DEV, dtype=BF)
+    p.forward()
+    p.backward(flat, None)
+    loss = p.loss.clone()
+    p.x = wide[:, 64:64 + K]
+    p.forward()
+    p.backward(dx, dw)
+    _ok()
+    assert torch.equal(p.loss, loss) and torch.equal(dx, flat) and bool((dx_all[:, :16] == 5).all()) and bool((dx_all[:, 16 + K:] == 5).all())
+    p.check_backward(dx, dw)
+    for bad in (p.x[:, 1:], p.x[::1, ::2], wide.t()):
+        with pytest.raises((ValueError, TypeError, api.Fp8Error)):
+            api.fp8_cross_entropy(bad, E4, p.w[:, :bad.shape[1]], E4, p.target, p.loss, p.lse, scale_inv_x=p.sx, scale_inv_w=p.sw)
+
+
+def test_more_than_2_to_the_31_weights():
+    """offsets that pass 32 bits: a projection of 2.3e9 codes; the last rows of the vocabulary are the ones that matter"""
+    T, K, V = 3, 16384, 140000
+    g = _gen(1)
+    x = torch.randn(T, K, generator=g, device=DEV).to(F8[E4]).view(torch.uint8)
+    w = torch.randint(0, 0x38, (V, K), generator=g, device=DEV, dtype=torch.uint8)          # 0 .. 0.94
+    w[1::2] |= 0x80
+    target = torch.tensor([V - 1, 7, V - 77], device=DEV)
+    loss, lse, one = torch.empty(T, device=DEV), torch.empty(T, device=DEV), _scalar(2.0 ** -6)
+    api.fp8_cross_entropy(x, E4, w, E4, target, loss, lse, scale_inv_x=one, scale_inv_w=_scalar(1.0))
+    dx, dw = torch.empty(T, K, dtype=BF, device=DEV), torch.empty(V, K, dtype=BF, device=DEV)
+    dloss = torch.full((T,), 1.0 / T, device=DEV)
+    api.fp8_cross_entropy_backward(x, E4, w, E4, target, lse, dloss, dx, dw, scale_inv_x=one, scale_inv_w=_scalar(1.0))
+    _ok()
+    x64 = x.view(F8[E4]).double()
+    z = torch.cat([x64 @ part.view(F8[E4]).double().T for part in w.split(20000)], 1) * 2.0 ** -6
+    s = torch.cat([x64.abs() @ part.view(F8[E4]).double().abs().T for part in w.split(20000)], 1) * 2.0 ** -6
+    want = torch.logsumexp(z, 1)
+    tol = 1e-5 * s.max(1)[0] + 2.0 ** -16 + 2.0 ** -20 * want.abs()
+    assert bool(((lse.double() - want).abs() <= tol).all())
+    rows = torch.arange(T, device=DEV)
+    assert bool(((loss.double() - (want - z[rows, target])).abs() <= 2 * tol).all())
+    dz = torch.exp(z - want[:, None])
+    dz[rows, target] -= 1
+    dz /= T
+    back = torch.zeros(T, K, dtype=torch.float64, device=DEV)
+    mags = torch.zeros_like(back)
+    for i, part in enumerate(w.split(20000)):
+        v = part.view(F8[E4]).double()
+        back += dz[:, i * 20000:i * 20000 + v.shape[0]] @ v
+        mags += dz.abs()[:, i * 20000:i * 20000 + v.shape[0]] @ v.abs()
+    assert bool(((dx.double() - back).abs() <= 0.135 * mags).all())                          # every term to 2^-3 and the logit's error
+    for lo, hi in ((0, 300), (V - 300, V)):
+        v = dz[:, lo:hi].T @ (x64 * 2.0 ** -6)
+        assert bool(((dw[lo:hi].double() - v).abs() <= 0.135 * (dz[:, lo:hi].abs().T @ (x64.abs() * 2.0 ** -6)) + 1e-12).all())
