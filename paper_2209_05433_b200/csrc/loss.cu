@@ -48,12 +48,14 @@ constexpr int FG = 2;                   // K-blocks consumed per barrier wait
 constexpr int MAX_STAGES = 12;
 constexpr uint32_t A_BYTES = ROWS * K_BYTES;
 constexpr uint32_t RING_BYTES = 196608;
-constexpr uint32_t BOX_BYTES = 4096;    // 32 rows x 128 B: staging of one epilogue warp
+constexpr uint32_t BOX_BYTES = 4096;    // 32 rows x 128 B: staging of an epilogue warp
+constexpr int MOST_BOXES = 3;           // of a warp, two stages of the ring in exchange for two of them
 constexpr int EPI_BASE = 4, EPI_WARPS = 8, THREADS = 32 * (EPI_BASE + EPI_WARPS);
 constexpr int REGS_FRONT = 56, REGS_EPILOGUE = 224;      // 128 x 56 + 256 x 224 = 64512, the launch's 384 x 168
 constexpr uint32_t SMEM_BARRIERS = 512;
 constexpr uint32_t SMEM_BYTES = RING_BYTES + EPI_WARPS * BOX_BYTES + SMEM_BARRIERS + 1024;
 constexpr uint32_t TMEM_COLS = 512;
+constexpr int SHORT_K = 8;              // K-blocks of a product that is bound by its output
 constexpr int GROUP_M = 16;             // row tiles that advance together over the columns
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
@@ -75,7 +77,8 @@ struct Params {
     Product q[2];
     int products;
     int full, rest, extra;              // how the tiles of two products are dealt out, see item_at
-    int stages;                         // of the ring (one CTA per tile)
+    int stages;                         // of the ring
+    int boxes;                          // staging boxes of an epilogue warp
     uint32_t a_bytes;                   // A's part of a stage (one CTA per tile)
     const int64_t* target;
     int64_t first, vocab;               // vocabulary column of the first column here; all columns of the vocabulary
@@ -149,7 +152,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     constexpr uint32_t MN_BOX = (uint32_t)KE * 128;               // such a box: MNE elements x one K-block
     constexpr int B_ROWS = BN / CG;                               // columns of the tile that this CTA loads
     const uint32_t a_bytes = CG == 2 ? A_BYTES : p.a_bytes, stage_bytes = a_bytes + B_ROWS * K_BYTES;
-    const uint32_t stages = CG == 2 ? RING_BYTES / (A_BYTES + B_ROWS * K_BYTES) : (uint32_t)p.stages;
+    const uint32_t stages = CG == 2 && MODE != MODE_OUT ? RING_BYTES / (A_BYTES + B_ROWS * K_BYTES) : (uint32_t)p.stages;
     constexpr int SPLIT = split_of<ESZ, MODE> / KE;                   // K-blocks per use of an accumulator
     constexpr int NC = BN / 2;                                    // columns of an epilogue thread
     extern __shared__ uint8_t smem_raw[];
@@ -333,8 +336,11 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 p.dz_scale[1] = 1.0f / dz_scale;
             }
         }
-        const uint32_t box = ring + RING_BYTES + (uint32_t)(warp - EPI_BASE) * BOX_BYTES;
-        const uint32_t box_row = box + lane * 128;
+        // one staging box after the ring, or three that start where it ends early
+        const bool three = MODE == MODE_OUT && p.boxes == MOST_BOXES;
+        const uint32_t boxes = three ? ring + RING_BYTES - 16u * BOX_BYTES + (uint32_t)(warp - EPI_BASE) * (MOST_BOXES * BOX_BYTES)
+                                     : ring + RING_BYTES + (uint32_t)(warp - EPI_BASE) * BOX_BYTES;
+        uint32_t box = boxes, box_row = box + lane * 128;
         const uint64_t out_policy = MODE == MODE_DZ ? policy_evict_last() : policy_evict_first();      // dz is read next
         bool ok = true;
         int it = 0, which, t;
@@ -428,8 +434,11 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     // A box over the right edge is clipped by the TMA unit in units of 16 bytes: where rows end elsewhere, plain
                     // stores write it.  dz and the planes of dx have rows of whole boxes.
                     const bool by_hand = MODE == MODE_OUT && q.ragged && col + BOX_COLS > q.N;
-                    if (!by_hand) {
-                        if (lane == 0) bulk_wait_read<0>();
+                    if (!by_hand) {                               // what was last stored from this box has left it
+                        if (lane == 0) {
+                            if (three) bulk_wait_read<MOST_BOXES - 1>();
+                            else       bulk_wait_read<0>();
+                        }
                         __syncwarp();
                     }
 #pragma unroll
@@ -491,6 +500,10 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                             else                                tma_store_3d(md, box, (int)(col * OSZ), (int)row0, slice, out_policy);
                         }
                         bulk_commit();
+                    }
+                    if (three) {
+                        box = box == boxes + (MOST_BOXES - 1) * BOX_BYTES ? boxes : box + BOX_BYTES;
+                        box_row = box + lane * 128;
                     }
                 }
             };
@@ -642,7 +655,9 @@ static fp8_status launch(const Maps* m, Params p, cudaStream_t st) {
     p.rest = p.q[0].tiles % workers;
     p.extra = 0;
     if (p.products > 1 && p.rest > 0) {                           // a last round of the first product lasts as long as so many tiles of the second
-        const int others = workers - p.rest, lasts = (p.q[0].slice_blocks + p.q[1].slice_blocks / 2) / p.q[1].slice_blocks;
+        // (a tile takes no less than its epilogue, about SHORT_K K-blocks)
+        const int k0 = p.q[0].slice_blocks > SHORT_K ? p.q[0].slice_blocks : SHORT_K, k1 = p.q[1].slice_blocks > SHORT_K ? p.q[1].slice_blocks : SHORT_K;
+        const int others = workers - p.rest, lasts = (k0 + k1 / 2) / k1;
         p.extra = lasts < p.q[1].tiles / others ? lasts : p.q[1].tiles / others;
     }
     cfg.gridDim = dim3(workers * CG);
@@ -718,12 +733,13 @@ static fp8_status logits(const fp8_cross_entropy_desc* d, const void* x, const v
     return esz == 1 ? launch<1, 1, 256, MODE>(&m, p, st) : launch<2, 1, 256, MODE>(&m, p, st);
 }
 
-// One product, or two in one launch.
-static fp8_status products(int esz, int cg, const Maps* m, Params& p, cudaStream_t st) {
-    p.a_bytes = A_BYTES;
-    p.stages = (int)(RING_BYTES / (A_BYTES + 256 * K_BYTES)) / FG * FG;
-    if (cg == 2) return esz == 1 ? launch<1, 2, 256, MODE_OUT>(m, p, st) : launch<2, 2, 256, MODE_OUT>(m, p, st);
-    return esz == 1 ? launch<1, 1, 256, MODE_OUT>(m, p, st) : launch<2, 1, 256, MODE_OUT>(m, p, st);
+// One product, or two in one launch, on CTA pairs.  Short sums are bound by their output: where one of them has at most SHORT_K
+// K-blocks, two stages of the ring become staging boxes, whose stores drain while the next boxes are filled.
+static fp8_status products(int esz, const Maps* m, Params& p, cudaStream_t st) {
+    const bool is_short = p.q[0].slice_blocks <= SHORT_K || (p.products > 1 && p.q[1].slice_blocks <= SHORT_K);
+    p.boxes = is_short ? MOST_BOXES : 1;
+    p.stages = (int)(RING_BYTES / (2 * A_BYTES)) - (is_short ? 2 : 0);
+    return esz == 1 ? launch<1, 2, 256, MODE_OUT>(m, p, st) : launch<2, 2, 256, MODE_OUT>(m, p, st);
 }
 
 template <typename... KArgs, typename... Args>
@@ -754,8 +770,7 @@ static Cut cut_of(int64_t T, int64_t K, int64_t V, int esz) {
     c.cols = round_up((V + c.pieces - 1) / c.pieces, 256);
     c.pieces = (int)((V + c.cols - 1) / c.cols);
     // few rows: dx has few tiles and a long contraction, cut so that the SMs have a tile each
-    const int cg = T > ROWS ? 2 : 1;
-    const int64_t tiles = (T + ROWS * cg - 1) / (ROWS * cg) * ((K + 255) / 256), workers = sm_count() / cg;
+    const int64_t tiles = (T + 255) / 256 * ((K + 255) / 256), workers = sm_count() / 2;
     int64_t slices = workers / (tiles > 0 ? tiles : 1);
     const int64_t longest = c.cols / 1024;                        // a slice has at least 1024 of K
     if (slices > longest) slices = longest;
@@ -891,7 +906,7 @@ fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const voi
     void* dz = ws + 256;
     float* planes = reinterpret_cast<float*>(ws + 256 + c.z_bytes);
     const float* back = esz == 1 ? scale + 1 : nullptr;
-    const int fz = FP8_E5M2, cg = T > ROWS ? 2 : 1;
+    const int fz = FP8_E5M2;
     for (int i = 0; i < c.pieces; ++i) {
         const int64_t v0 = i * c.cols, cols = V - v0 < c.cols ? V - v0 : c.cols;
         const uint8_t* wp = reinterpret_cast<const uint8_t*>(w) + v0 * d->ldw * esz;
@@ -913,7 +928,7 @@ fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const voi
             of_x.out = c.planes ? (i == 0 ? OUT_WIDE : OUT_ADDED) : dx_t == FP8_BF16 ? OUT_ROUNDED : OUT_WIDE;
             of_x.D = c.planes ? planes : dx;
             of_x.ldd = c.planes ? c.pitch_x : lddx;
-            if (!lay_out(of_x, mx, esz, fz, d->w_t, A, B, cg, 256, ROWS, c.planes ? c.pitch_x : K, of_x.out == OUT_ROUNDED ? 2 : 4)) return FP8_ERR_CUDA;
+            if (!lay_out(of_x, mx, esz, fz, d->w_t, A, B, 2, 256, ROWS, c.planes ? c.pitch_x : K, of_x.out == OUT_ROUNDED ? 2 : 4)) return FP8_ERR_CUDA;
         }
         if (dw) {
             of_w.M = cols; of_w.N = K; of_w.K = T;
@@ -922,7 +937,7 @@ fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const voi
             of_w.D = reinterpret_cast<uint8_t*>(dw) + v0 * lddw * wo; of_w.ldd = lddw;
             of_w.out = dw_t == FP8_BF16 ? OUT_ROUNDED : OUT_WIDE;
             const Operand A{dz, c.pitch_z, true}, B{x, d->ldx, true};
-            if (!lay_out(of_w, mw, esz, fz, d->x_t, A, B, cg, 256, ROWS, K, wo)) return FP8_ERR_CUDA;
+            if (!lay_out(of_w, mw, esz, fz, d->x_t, A, B, 2, 256, ROWS, K, wo)) return FP8_ERR_CUDA;
         }
         Params p = {};
         Maps m[2];
@@ -930,7 +945,7 @@ fp8_status fp8_cross_entropy_backward(const fp8_cross_entropy_desc* d, const voi
         p.products = dx && dw ? 2 : 1;
         p.q[0] = x_first ? of_x : of_w; m[0] = x_first ? mx : mw;
         p.q[1] = x_first ? of_w : of_x; m[1] = x_first ? mw : mx;
-        if ((rc = products(esz, cg, m, p, st)) != FP8_OK) return rc;
+        if ((rc = products(esz, m, p, st)) != FP8_OK) return rc;
     }
     if (dx && c.planes) {
         const int64_t octets = T * ((K + 7) / 8);
