@@ -55,7 +55,8 @@ constexpr int REGS_FRONT = 56, REGS_EPILOGUE = 224;      // 128 x 56 + 256 x 224
 constexpr uint32_t SMEM_BARRIERS = 512;
 constexpr uint32_t SMEM_BYTES = RING_BYTES + EPI_WARPS * BOX_BYTES + SMEM_BARRIERS + 1024;
 constexpr uint32_t TMEM_COLS = 512;
-constexpr int SHORT_K = 8;              // K-blocks of a product that is bound by its output
+constexpr int SHORT_K = 4;              // K-blocks of a product that is bound by its output
+constexpr int EPILOGUE_K = 8;           // K-blocks in whose time a tile's epilogue is done
 constexpr int GROUP_M = 16;             // row tiles that advance together over the columns
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
@@ -104,6 +105,7 @@ __device__ __forceinline__ void mma_bf16_pair(uint32_t tmem_d, uint64_t a, uint6
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+__device__ __forceinline__ void call_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
     asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -170,6 +172,12 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars->acc_full[a]), 1); mbar_init(smem_u32(&bars->acc_empty[a]), EPI_WARPS * CG); }
         bars->abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2 && lane == 0) {                                 // on their way while the barriers are made
+        call_map(&map_a);
+        call_map(&map_b);
+        if (MODE != MODE_STATS) call_map(&map_d);
+        if (MODE == MODE_OUT && p.products > 1) { call_map(&map_a1); call_map(&map_b1); call_map(&map_d1); }
     }
     if (warp == 1) {
         if (CG == 2) {
@@ -655,8 +663,8 @@ static fp8_status launch(const Maps* m, Params p, cudaStream_t st) {
     p.rest = p.q[0].tiles % workers;
     p.extra = 0;
     if (p.products > 1 && p.rest > 0) {                           // a last round of the first product lasts as long as so many tiles of the second
-        // (a tile takes no less than its epilogue, about SHORT_K K-blocks)
-        const int k0 = p.q[0].slice_blocks > SHORT_K ? p.q[0].slice_blocks : SHORT_K, k1 = p.q[1].slice_blocks > SHORT_K ? p.q[1].slice_blocks : SHORT_K;
+        const int k0 = p.q[0].slice_blocks > EPILOGUE_K ? p.q[0].slice_blocks : EPILOGUE_K;
+        const int k1 = p.q[1].slice_blocks > EPILOGUE_K ? p.q[1].slice_blocks : EPILOGUE_K;
         const int others = workers - p.rest, lasts = (k0 + k1 / 2) / k1;
         p.extra = lasts < p.q[1].tiles / others ? lasts : p.q[1].tiles / others;
     }
@@ -734,7 +742,8 @@ static fp8_status logits(const fp8_cross_entropy_desc* d, const void* x, const v
 }
 
 // One product, or two in one launch, on CTA pairs.  Short sums are bound by their output: where one of them has at most SHORT_K
-// K-blocks, two stages of the ring become staging boxes, whose stores drain while the next boxes are filled.
+// K-blocks, two stages of the ring become staging boxes, whose stores drain while the next boxes are filled (300 tokens, width
+// 8192, vocabulary 32000, FP8: backward pass 411 -> 343 us; with 8 K-blocks the other product's shorter ring costs more: 1001 tokens 560 -> 589).
 static fp8_status products(int esz, const Maps* m, Params& p, cudaStream_t st) {
     const bool is_short = p.q[0].slice_blocks <= SHORT_K || (p.products > 1 && p.q[1].slice_blocks <= SHORT_K);
     p.boxes = is_short ? MOST_BOXES : 1;
@@ -769,15 +778,18 @@ static Cut cut_of(int64_t T, int64_t K, int64_t V, int esz) {
     c.pieces = (int)((V + most - 1) / most);
     c.cols = round_up((V + c.pieces - 1) / c.pieces, 256);
     c.pieces = (int)((V + c.cols - 1) / c.cols);
-    // few rows: dx has few tiles and a long contraction, cut so that the SMs have a tile each
+    // Few rows: dx has few tiles and a long contraction.  It is cut into slices while that pays: a pair needs about 0.25 us for a
+    // K-block it waits for, the planes of several slices cost a launch and their traffic.
     const int64_t tiles = (T + 255) / 256 * ((K + 255) / 256), workers = sm_count() / 2;
-    int64_t slices = workers / (tiles > 0 ? tiles : 1);
-    const int64_t longest = c.cols / 1024;                        // a slice has at least 1024 of K
-    if (slices > longest) slices = longest;
-    if (slices > 16) slices = 16;
     const int64_t ke = K_BYTES / esz, blocks = ((V < c.cols ? V : c.cols) + ke - 1) / ke;
-    const int64_t each = (blocks + (slices < 1 ? 1 : slices) - 1) / (slices < 1 ? 1 : slices);
-    c.slices = (int)((blocks + each - 1) / each);                 // as `product` counts them for the first piece, which writes every plane
+    const double plane_us = (c.pieces > 1 ? 0.0 : 4.0), each_us = 8.0 * (double)T * (double)K / 4e6;
+    double best = 0.0;
+    c.slices = 1;
+    for (int64_t s = 1; s <= 16 && s <= blocks && (s == 1 || tiles * s <= workers); ++s) {
+        const int64_t each = (blocks + s - 1) / s;
+        const double us = 0.25 * (double)each + (s > 1 ? plane_us + each_us * (double)s : 0.0);
+        if (s == 1 || us < best) { best = us; c.slices = (int)((blocks + each - 1) / each); }      // as lay_out counts them for the first piece, which writes every plane
+    }
     c.planes = c.slices > 1 || c.pieces > 1;
     c.pitch_z = c.cols;
     c.pitch_x = round_up(K, 32);
