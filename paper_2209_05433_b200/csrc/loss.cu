@@ -68,7 +68,8 @@ struct Product {
     const float* s[2];                  // factors of the product; null counts as 1
     void* D;
     int64_t ldd;                        // elements
-    int out, ragged;                    // what is stored; rows of D do not end on 16 bytes
+    int out;                            // what is stored
+    int64_t whole;                      // columns of D up to the last 16-byte boundary
     uint32_t idesc;
     int tiles_m, tiles_n, tiles;        // tiles: of all slices
     int k_blocks, slices, slice_blocks; // K in slices of slice_blocks K-blocks, each with an output plane of its own
@@ -106,6 +107,11 @@ __device__ __forceinline__ void mma_bf16_pair(uint32_t tmem_d, uint64_t a, uint6
                  ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void call_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
     asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -350,6 +356,8 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                                      : ring + RING_BYTES + (uint32_t)(warp - EPI_BASE) * BOX_BYTES;
         uint32_t box = boxes, box_row = box + lane * 128;
         const uint64_t out_policy = MODE == MODE_DZ ? policy_evict_last() : policy_evict_first();      // dz is read next
+        auto factor = [](const Product& q) { return (q.s[0] ? __ldg(q.s[0]) : 1.0f) * (q.s[1] ? __ldg(q.s[1]) : 1.0f); };
+        const float alpha0 = factor(p.q[0]) * (MODE != MODE_OUT ? LOG2E : 1.0f), alpha1 = MODE == MODE_OUT ? factor(p.q[1]) : 1.0f;
         bool ok = true;
         int it = 0, which, t;
         float v[NC];
@@ -365,8 +373,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const int64_t col0 = (int64_t)tn * BN + half * NC;                 // first column of this warp
             const bool row_ok = row < q.M;
             const int cols = (int)max((int64_t)0, min((int64_t)NC, q.N - col0));
-            float alpha = (q.s[0] ? __ldg(q.s[0]) : 1.0f) * (q.s[1] ? __ldg(q.s[1]) : 1.0f);
-            if (MODE != MODE_OUT) alpha *= LOG2E;
+            const float alpha = MODE == MODE_OUT && which ? alpha1 : alpha0;
             int rel = -1;                                         // the target's column among this thread's, if it is there
             bool counted = false;
             float g = 0.0f, lse2 = 0.0f;
@@ -432,6 +439,8 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (row_ok) p.part[(int64_t)(2 * tn + half) * q.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
                 continue;
             }
+            bool tail = false;                                    // this row's last columns are here, in `rest`
+            uint4 rest = make_uint4(0u, 0u, 0u, 0u);
             // OSZ bytes of an element in boxes of 128 bytes a row
             auto store = [&](auto size) {
                 constexpr int OSZ = decltype(size)::value;
@@ -439,16 +448,11 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                 for (int c = 0; c < NC; c += BOX_COLS) {
                     const int64_t col = col0 + c;
-                    // A box over the right edge is clipped by the TMA unit in units of 16 bytes: where rows end elsewhere, plain
-                    // stores write it.  dz and the planes of dx have rows of whole boxes.
-                    const bool by_hand = MODE == MODE_OUT && q.ragged && col + BOX_COLS > q.N;
-                    if (!by_hand) {                               // what was last stored from this box has left it
-                        if (lane == 0) {
-                            if (three) bulk_wait_read<MOST_BOXES - 1>();
-                            else       bulk_wait_read<0>();
-                        }
-                        __syncwarp();
+                    if (lane == 0) {                              // what was last stored from this box has left it
+                        if (three) bulk_wait_read<MOST_BOXES - 1>();
+                        else       bulk_wait_read<0>();
                     }
+                    __syncwarp();
 #pragma unroll
                     for (int sub = 0; sub < SUBS; ++sub) {
                         float y[32];
@@ -481,29 +485,20 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                             for (int i = 0; i < WORDS; ++i) w[i] = 0u;
                         }
-                        if (by_hand) {
-                            if (row_ok) {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    if (col + sub * 32 + i >= q.N) continue;
-                                    const int64_t at = row * q.ldd + col + sub * 32 + i;
-                                    if (OSZ == 4) reinterpret_cast<uint32_t*>(q.D)[at] = w[i % WORDS];
-                                    else          reinterpret_cast<uint16_t*>(q.D)[at] = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
-                                }
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < WORDS / 4; ++i) {
-                                const int pos = sub * (WORDS / 4) + i;
-                                st_shared_v4(box_row + ((pos ^ (lane & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-                            }
+                        for (int i = 0; i < WORDS / 4; ++i) {
+                            const int pos = sub * (WORDS / 4) + i;
+                            st_shared_v4(box_row + ((pos ^ (lane & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                         }
                     }
-                    if (by_hand) continue;
+                    if (MODE == MODE_OUT && q.whole < q.N && col <= q.whole && col + BOX_COLS > q.whole) {
+                        rest = ld_shared_v4(box_row + ((((int)(q.whole - col) * OSZ / 16) ^ (lane & 7)) << 4));
+                        tail = row_ok;
+                    }
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        if (row0 < q.M && col < q.N) {
+                        if (row0 < q.M && col < q.whole) {
                             if (OSZ == 4 && q.out == OUT_ADDED) tma_add_3d(md, box, (int)col, (int)row0, slice);
                             else                                tma_store_3d(md, box, (int)(col * OSZ), (int)row0, slice, out_policy);
                         }
@@ -518,6 +513,22 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (MODE == MODE_DZ) store(std::integral_constant<int, ESZ>());
             else if (q.out == OUT_ROUNDED) store(std::integral_constant<int, 2>());
             else store(std::integral_constant<int, 4>());
+            // The TMA unit clips in units of 16 bytes: the map ends with the last whole one of a row, and the few columns behind it,
+            // where there are any, are written one by one.  Last of the tile: a box's fence would wait for them.
+            if (tail) {
+                const int count = (int)(q.N - q.whole);
+                if (q.out == OUT_ROUNDED) {
+                    uint16_t* to = reinterpret_cast<uint16_t*>(q.D) + row * q.ldd + q.whole;
+#pragma unroll
+                    for (int i = 0; i < 7; ++i)
+                        if (i < count) to[i] = (uint16_t)((i < 2 ? rest.x : i < 4 ? rest.y : i < 6 ? rest.z : rest.w) >> (16 * (i & 1)));
+                } else {
+                    uint32_t* to = reinterpret_cast<uint32_t*>(q.D) + row * q.ldd + q.whole;
+#pragma unroll
+                    for (int i = 0; i < 3; ++i)
+                        if (i < count) to[i] = i == 0 ? rest.x : i == 1 ? rest.y : rest.z;
+                }
+            }
         }
         if (MODE != MODE_STATS && lane == 0) bulk_wait_all();
     }
@@ -702,10 +713,11 @@ static bool lay_out(Product& q, Maps& m, int esz, int fa, int fb, const Operand&
         return o.mn ? make_map(t, o.p, (uint64_t)(mn * esz), (uint64_t)q.K, (uint64_t)(o.ld * esz), 1, 0, 128, (uint32_t)ke)
                     : make_map(t, o.p, (uint64_t)(q.K * esz), (uint64_t)mn, (uint64_t)(o.ld * esz), 1, 0, K_BYTES, (uint32_t)rows);
     };
+    q.whole = out_cols * out_size / 16 * 16 / (out_size > 0 ? out_size : 1);
     if (!map(&m.a, A, q.M, a_rows) || !map(&m.b, B, q.N, bn / cg)) return false;
     if (!q.D) m.d = m.a;                                          // nothing is stored through it
-    else if (!make_plane_map(&m.d, q.D, out_cols, q.M, q.ldd, q.slices, out_size, q.out == OUT_ADDED)) return false;
-    q.ragged = (out_cols * out_size & 15) != 0 ? 1 : 0;
+    else if (q.whole == 0) m.d = m.a;                             // rows of less than 16 bytes
+    else if (!make_plane_map(&m.d, q.D, q.whole, q.M, q.ldd, q.slices, out_size, q.out == OUT_ADDED)) return false;
     q.a_mn = A.mn ? 1 : 0;
     q.b_mn = B.mn ? 1 : 0;
     q.tiles_m = (int)((q.M + ROWS * cg - 1) / (ROWS * cg));
