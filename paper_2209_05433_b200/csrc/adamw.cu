@@ -522,6 +522,7 @@ using namespace fp8b200;
 extern "C" {
 
 static bool beta_ok(double b) { return b >= 0.0 && b < 1.0; }
+static bool chunk_ok(int64_t n) { return n >= adamw::LEAST_CHUNK && n <= adamw::MOST_CHUNK && n % adamw::LEAST_CHUNK == 0; }
 
 fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_adamw_plan* plan) {
     using namespace fp8b200::adamw;
@@ -539,7 +540,7 @@ fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_a
         if (it.n < 0) return FP8_ERR_SHAPE;
         const bool coded = it.copy && it.copy_t >= FP8_STORE_E4M3;
         if (it.n > 0 && (!it.g || !it.p || !it.m || !it.v || (codes && (!it.m_scale || !it.v_scale)))) return FP8_ERR_NULL;
-        if ((coded && !it.copy_scale_dev) || (it.copy_amax_dev && !coded)) return FP8_ERR_NULL;
+        if ((coded && !it.copy_scale_dev) || (it.copy_amax_dev && !coded && it.n > 0)) return FP8_ERR_NULL;      // an empty copy has no address, but an amax of 0
         const uintptr_t fours = reinterpret_cast<uintptr_t>(it.m_scale) | reinterpret_cast<uintptr_t>(it.v_scale) | reinterpret_cast<uintptr_t>(it.copy_scale_dev) |
                                 reinterpret_cast<uintptr_t>(it.copy_amax_dev) |
                                 (codes ? 0 : reinterpret_cast<uintptr_t>(it.m) | reinterpret_cast<uintptr_t>(it.v)) |
@@ -576,7 +577,7 @@ fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_a
 fp8_status fp8_adamw_plan_fill(const fp8_adamw_item* items, const fp8_adamw_plan* plan, void* table_host) {
     using namespace fp8b200::adamw;
     if (!plan || (plan->table_bytes > 0 && !table_host) || (plan->count > 0 && !items)) return FP8_ERR_NULL;
-    if (plan->chunk < LEAST_CHUNK) return FP8_ERR_SHAPE;
+    if (!chunk_ok(plan->chunk)) return FP8_ERR_SHAPE;
     Entry* e = reinterpret_cast<Entry*>(table_host);
     int32_t* map = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(table_host) + plan->count * (int64_t)sizeof(Entry));
     int64_t chunk = 0, number = 0;
@@ -605,7 +606,7 @@ fp8_status fp8_adamw_plan_fill(const fp8_adamw_item* items, const fp8_adamw_plan
 fp8_status fp8_adamw_step(const fp8_adamw_plan* plan, const void* table_dev, void* workspace_dev, const fp8_adamw_options* o, void* stream) {
     using namespace fp8b200::adamw;
     if (!plan || !o) return FP8_ERR_NULL;
-    if (plan->count < 0 || plan->chunks < 0 || plan->chunks > 0x7FFFFFFF || plan->chunk < LEAST_CHUNK) return FP8_ERR_SHAPE;
+    if (plan->count < 0 || plan->chunks < 0 || plan->chunks > 0x7FFFFFFF || !chunk_ok(plan->chunk)) return FP8_ERR_SHAPE;
     if (!workspace_dev || (plan->count > 0 && !table_dev)) return FP8_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(table_dev) & 15u) || (reinterpret_cast<uintptr_t>(workspace_dev) & 15u) || (reinterpret_cast<uintptr_t>(o->norm_dev) & 3u) ||
         (reinterpret_cast<uintptr_t>(o->lr_dev) & 3u) || (reinterpret_cast<uintptr_t>(o->step_dev) & 7u))

@@ -359,3 +359,17 @@ def test_refusals_of_the_binding():
     with pytest.raises(TypeError):
         api.fp8_adamw_step(plan, 1e-3, torch.zeros(1, device=DEV))
     _ok()
+
+
+def test_empty_tensors_and_empty_plans():
+    e, amax, count = torch.empty(0, device=DEV), _scalar(5.0), torch.tensor([8], device=DEV)
+    api.fp8_adamw_step(api.AdamWPlan([], [], [], []), 1e-3, count)
+    assert int(count) == 9
+    api.fp8_adamw_step(api.AdamWPlan([], [], [], []), 1e-3, 1)
+    p = torch.ones(10, device=DEV)
+    z = torch.zeros(10, device=DEV)
+    plan = api.AdamWPlan([e, p, e], [e, z, e], [e, z.clone(), e], [e, z.clone(), e], copies=[torch.empty(0, dtype=U8, device=DEV), None, None], fmt=E4,
+                         scales=[_scalar(1.0), None, None], amax_outs=[amax, None, None])
+    api.fp8_adamw_step(plan, 1e-3, count)
+    _ok()
+    assert float(amax) == 0.0 and int(count) == 10 and bool((p == 1).all())

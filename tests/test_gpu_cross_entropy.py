@@ -366,3 +366,38 @@ def test_more_than_2_to_the_31_weights():
     for lo, hi in ((0, 300), (V - 300, V)):
         v = dz[:, lo:hi].T @ (x64 * 2.0 ** -6)
         assert bool(((dw[lo:hi].double() - v).abs() <= 0.135 * (dz[:, lo:hi].abs().T @ (x64.abs() * 2.0 ** -6)) + 1e-12).all())
+
+
+@pytest.mark.parametrize("fx", [E4, None])
+def test_the_smallest_vocabularies_and_widths(fx):
+    """more rows than a tile has, on one, two and nine columns, widths of one and of a few bytes"""
+    for T, K, V in ((200, 16, 1), (300, 1, 2), (129, 3, 9), (1, 5, 3)):
+        p = Problem(T, K, V, fx, fx)
+        (dx, all_dx), (dw, all_dw) = _matrix(T, K, F32), _matrix(V, K, BF)
+        p.forward()
+        p.backward(dx, dw)
+        _ok()
+        p.check_forward()
+        p.check_backward(dx, dw)
+        assert _guards_kept(dx, all_dx) and _guards_kept(dw, all_dw)
+
+
+def test_workspaces_of_the_caller():
+    p = Problem(150, 64, 2000, E4, E4)
+    forward, backward = api.cross_entropy_workspace_bytes(150, 64, 2000)
+    dx, dw = torch.empty(150, 64, device=DEV), torch.empty(2000, 64, device=DEV)
+    p.forward()
+    p.backward(dx, dw)
+    want = p.loss.clone(), dx.clone(), dw.clone()
+    ws = torch.full((max(forward, backward) + 64,), 0xFF, dtype=torch.uint8, device=DEV)     # its contents mean nothing
+    p.forward(workspace=ws[:forward])
+    p.backward(dx, dw, workspace=ws[:backward])
+    _ok()
+    assert torch.equal(p.loss, want[0]) and torch.equal(dx, want[1]) and torch.equal(dw, want[2])
+    assert bool((ws[max(forward, backward):] == 0xFF).all())
+    with pytest.raises(api.Fp8Error):
+        p.forward(workspace=ws[:forward - 1])
+    with pytest.raises(api.Fp8Error):
+        p.backward(dx, dw, workspace=ws[:backward - 1])
+    with pytest.raises(ValueError):
+        p.forward(workspace=ws.cpu())
