@@ -149,7 +149,8 @@ __device__ __forceinline__ bool item_at(const Params& p, int j, int worker, int 
     return t < p.q[1].tiles;
 }
 
-// ESZ: bytes of an operand's element (1: FP8, 2: bf16).  CG: CTAs of a tile.  BN: its columns.
+// ESZ: bytes of an operand's element (1: FP8, 2: bf16).  CG: CTAs of a tile.  BN: its columns.  The logits' gradient in tiles of 128
+// columns takes four epilogue warps, each with whole rows of them: a staged box has 128 bytes a row either way.
 template <int ESZ, int CG, int BN, int MODE>
 __global__ void __launch_bounds__(THREADS, 1)
 k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_d,
@@ -162,7 +163,9 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t a_bytes = CG == 2 ? A_BYTES : p.a_bytes, stage_bytes = a_bytes + B_ROWS * K_BYTES;
     const uint32_t stages = CG == 2 && MODE != MODE_OUT ? RING_BYTES / (A_BYTES + B_ROWS * K_BYTES) : (uint32_t)p.stages;
     constexpr int SPLIT = split_of<ESZ, MODE> / KE;                   // K-blocks per use of an accumulator
-    constexpr int NC = BN / 2;                                    // columns of an epilogue thread
+    constexpr int PARTS = MODE == MODE_DZ && BN == 128 ? 1 : 2;   // warps that share a row of a tile
+    constexpr int ACTIVE = 4 * PARTS;                             // epilogue warps with something to do
+    constexpr int NC = BN / PARTS;                                // columns of an epilogue thread
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
@@ -175,7 +178,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars->full[s]), FG * CG); mbar_init(smem_u32(&bars->empty[s]), 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars->acc_full[a]), 1); mbar_init(smem_u32(&bars->acc_empty[a]), EPI_WARPS * CG); }
+        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bars->acc_full[a]), 1); mbar_init(smem_u32(&bars->acc_empty[a]), ACTIVE * CG); }
         bars->abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -293,7 +296,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                             const uint32_t st = stage + h;
                             if (kb + h < kn) {
                                 // With few rows A's part of a stage holds those alone, and the rows behind them are whatever
-                                // follows it in the stage: every row of a product is its own, and theirs are not looked at.
+                                // follows: every row of a product is its own, and theirs are not looked at.
                                 const uint32_t sa = ring + st * stage_bytes, sb = sa + a_bytes;
 #pragma unroll
                                 for (int k = 0; k < K_BYTES / K_STEP_BYTES; ++k) {
@@ -361,7 +364,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         bool ok = true;
         int it = 0, which, t;
         float v[NC];
-        for (int j = 0; ok && item_at(p, j, worker, workers, which, t); ++j) {
+        for (int j = 0; ok && half < PARTS && item_at(p, j, worker, workers, which, t); ++j) {
             const Product& q = p.q[which];
             const CUtensorMap* md = which ? &map_d1 : &map_d;
             int tm, tn;
@@ -392,18 +395,19 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q4 * 32) << 16) + half * NC;
+                constexpr int LOADS = NC >= 64 ? 2 : 1;           // in flight, one wait for all
 #pragma unroll
-                for (int c = 0; c < NC; c += 64) {                // two loads in flight, one wait for both
-                    uint32_t r[2][32];
-                    tc_ld32(taddr + c, r[0]);
-                    tc_ld32(taddr + c + 32, r[1]);
+                for (int c = 0; c < NC; c += 32 * LOADS) {
+                    uint32_t r[LOADS][32];
+#pragma unroll
+                    for (int l = 0; l < LOADS; ++l) tc_ld32(taddr + c + 32 * l, r[l]);
                     tc_wait_ld();
                     if (kc == 0) {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) v[c + i] = __uint_as_float(r[i >> 5][i & 31]);
+                        for (int i = 0; i < 32 * LOADS; ++i) v[c + i] = __uint_as_float(r[i >> 5][i & 31]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) v[c + i] += __uint_as_float(r[i >> 5][i & 31]);
+                        for (int i = 0; i < 32 * LOADS; ++i) v[c + i] += __uint_as_float(r[i >> 5][i & 31]);
                     }
                 }
                 tc_fence_before();
@@ -697,12 +701,17 @@ static bool make_plane_map(CUtensorMap* map, void* base, int64_t cols, int64_t r
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns of a tile for products with at most 128 rows (one CTA per tile): 256, or 128 where fewer rounds of the SMs are
-// needed for the same columns.
-static int few_rows_width(int64_t N) {
+// Columns of a tile for products with at most 128 rows (one CTA per tile).  A tile takes as long as its columns and rows are
+// loaded, and a little more; the width with the shortest rounds of all SMs is taken.  (8 tokens x 2048: vocabulary 2000 WIDTH_US.)
+static int few_rows_width(int64_t M, int64_t N, int least) {
     const int64_t sms = sm_count();
-    const int64_t wide = ((N + 255) / 256 + sms - 1) / sms * 256, narrow = ((N + 127) / 128 + sms - 1) / sms * 128;
-    return narrow < wide ? 128 : 256;
+    int best = 256;
+    int64_t best_cost = 0;
+    for (int bn = 256; bn >= least; bn /= 2) {
+        const int64_t cost = ((N + bn - 1) / bn + sms - 1) / sms * (bn + round_up(M, 8) + 16);
+        if (bn == 256 || cost < best_cost) { best = bn; best_cost = cost; }
+    }
+    return best;
 }
 
 // Fills in what follows from a product's sizes, layouts and formats, and its tensor maps.  q holds M, N, K, the factors, D, ldd,
@@ -737,7 +746,8 @@ template <int MODE>
 static fp8_status logits(const fp8_cross_entropy_desc* d, const void* x, const void* w, Params& p, cudaStream_t st) {
     Product& q = p.q[0];
     const int esz = d->x_t == FP8_OPERAND_BF16 ? 2 : 1;
-    const int cg = q.M > ROWS ? 2 : 1, bn = MODE == MODE_STATS && cg == 1 ? few_rows_width(q.N) : 256;
+    // (the part of a stage that the rows of A do not fill is read as rows that nobody looks at; behind the last stage that is the staging boxes)
+    const int cg = q.M > ROWS ? 2 : 1, bn = cg == 1 ? few_rows_width(q.M, q.N, MODE == MODE_STATS ? 64 : 128) : 256;
     const int a_rows = cg == 2 ? ROWS : (int)round_up(q.M, 8);
     Maps m;
     q.slices = 1;
@@ -748,8 +758,9 @@ static fp8_status logits(const fp8_cross_entropy_desc* d, const void* x, const v
     if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
     if (cg == 2) return esz == 1 ? launch<1, 2, 256, MODE>(&m, p, st) : launch<2, 2, 256, MODE>(&m, p, st);
     if constexpr (MODE == MODE_STATS) {
-        if (bn == 128) return esz == 1 ? launch<1, 1, 128, MODE>(&m, p, st) : launch<2, 1, 128, MODE>(&m, p, st);
+        if (bn == 64) return esz == 1 ? launch<1, 1, 64, MODE>(&m, p, st) : launch<2, 1, 64, MODE>(&m, p, st);
     }
+    if (bn == 128) return esz == 1 ? launch<1, 1, 128, MODE>(&m, p, st) : launch<2, 1, 128, MODE>(&m, p, st);
     return esz == 1 ? launch<1, 1, 256, MODE>(&m, p, st) : launch<2, 1, 256, MODE>(&m, p, st);
 }
 
@@ -810,7 +821,10 @@ static Cut cut_of(int64_t T, int64_t K, int64_t V, int esz) {
     return c;
 }
 
-static int64_t parts_of(int64_t T, int64_t V) { return 2 * (T > ROWS ? (V + 255) / 256 : (V + 127) / 128); }      // few rows: of either tile width
+static int64_t parts_of(int64_t T, int64_t V) {
+    const int bn = T > ROWS ? 256 : few_rows_width(T, V, 64);
+    return 2 * ((V + bn - 1) / bn);
+}
 static size_t forward_bytes(int64_t T, int64_t V) { return T > 0 ? (size_t)parts_of(T, V) * (size_t)T * 8 + (size_t)T * 4 : 0; }
 static size_t backward_bytes(int64_t T, int64_t K, int64_t V, int esz) {
     if (T <= 0) return 0;
