@@ -103,6 +103,7 @@ class AdamWOptions(ctypes.Structure):
 
 
 _pack_adamw = struct.Struct("ddddqQPPPf4x").pack
+_pack_adamw_item_into = struct.Struct("PPPPPPPPPqfiiii4x").pack_into
 
 _lib = None
 
@@ -717,40 +718,46 @@ class AdamWPlan:
         if any(len(c) != count for c in columns) or len(decays) != count:
             raise ValueError("all lists must have one length")
         self.tensors = columns                                # kept alive
-        device = params[0].device if count else torch.device("cuda", torch.cuda.current_device())
-        items = (AdamWItem * max(1, count))()
-        for it, p, g, m, v, ms, vs, copy, scale, amax, decay in zip(items, *columns, decays):
+        device = params[0].get_device() if count else torch.cuda.current_device()
+        if device < 0:
+            raise ValueError("the tensors must be on a CUDA device")
+
+        def address(t: torch.Tensor, dtypes: tuple, n: int, name: str) -> int:
+            if t.get_device() != device or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous tensor on the device of the first parameter" % name)
+            if t.numel() != n:
+                raise ValueError("%s has %d elements, not %d" % (name, t.numel(), n))
+            if t.dtype not in dtypes:
+                raise TypeError("%s must not be %s" % (name, t.dtype))
+            return t.data_ptr()
+
+        wide, f32, u8, bf16 = (torch.float32, torch.bfloat16), (torch.float32,), torch.uint8, torch.bfloat16
+        size = ctypes.sizeof(AdamWItem)
+        items = bytearray(size * max(1, count))
+        for i, (p, g, m, v, ms, vs, copy, scale, amax, decay) in enumerate(zip(*columns, decays)):
             n = p.numel()
-            for t in (p, g, m, v, ms, vs, copy, scale, amax):
-                if t is not None and t.device != device:
-                    raise ValueError("all tensors must be on one device")
-            if g.numel() != n or m.numel() != n or v.numel() != n or (copy is not None and copy.numel() != n):
-                raise ValueError("gradient, moments and copy must have the size of their parameter")
-            it.p, it.p_t, it.g, it.g_t, it.n, it.weight_decay = _dev(p, "parameter"), _wide_of(p), _dev(g, "gradient"), _wide_of(g), n, decay
-            it.m, it.v = _dev(m, "exp_avg"), _dev(v, "exp_avg_sq")
-            if m.dtype != v.dtype or m.dtype not in (torch.float32, torch.uint8):
-                raise TypeError("both moments must be float32, or both uint8 codes")
-            if (m.dtype is torch.uint8) != (ms is not None) or (ms is None) != (vs is None):
+            codes = m.dtype is u8
+            if codes != (ms is not None) or codes != (vs is not None):
                 raise TypeError("8-bit moments need their scales, and only they")
-            if ms is not None:
-                blocks = -(-n // STATE_BLOCK)
-                it.state, it.m_scale, it.v_scale = 1, _vec(ms, blocks, "exp_avg_scales"), _vec(vs, blocks, "exp_avg_sq_scales")
-            if copy is None:
-                if scale is not None or amax is not None:
-                    raise TypeError("scales and amax_outs go with a copy")
-                continue
-            it.copy = _dev(copy, "copy")
-            if copy.dtype is torch.uint8:
-                if fmt not in (E4M3, E5M2) or scale is None:
-                    raise TypeError("a uint8 copy needs its format, E4M3 or E5M2, and its scale")
-                it.copy_t, it.copy_scale = STORE_E4M3 + fmt, _scalar(scale, "scale")
-                it.copy_amax = None if amax is None else _scalar(amax, "amax_out")
-            elif copy.dtype is torch.bfloat16:
+            state = (u8,) if codes else f32
+            blocks = -(-n // STATE_BLOCK)
+            copy_at = scale_at = amax_at = copy_t = 0
+            if copy is None or copy.dtype is bf16:
                 if scale is not None or amax is not None:
                     raise TypeError("scales and amax_outs go with a uint8 copy")
-                it.copy_t = STORE_BF16
+                if copy is not None:
+                    copy_at, copy_t = address(copy, wide, n, "copy"), STORE_BF16
             else:
-                raise TypeError("copies must be bfloat16, or uint8 codes")
+                copy_at = address(copy, (u8,), n, "copy")
+                if fmt not in (E4M3, E5M2) or scale is None:
+                    raise TypeError("a uint8 copy needs its format, E4M3 or E5M2, and its scale")
+                copy_t, scale_at = STORE_E4M3 + fmt, address(scale, f32, 1, "scale")
+                amax_at = 0 if amax is None else address(amax, f32, 1, "amax_out")
+            _pack_adamw_item_into(items, i * size, address(g, wide, n, "gradient"), address(p, wide, n, "parameter"), address(m, state, n, "exp_avg"),
+                                  address(v, state, n, "exp_avg_sq"), address(ms, f32, blocks, "exp_avg_scales") if codes else 0,
+                                  address(vs, f32, blocks, "exp_avg_sq_scales") if codes else 0, copy_at, scale_at, amax_at, n, decay,
+                                  BF16 if g.dtype is bf16 else F32, BF16 if p.dtype is bf16 else F32, 1 if codes else 0, copy_t)
+        items = (AdamWItem * max(1, count)).from_buffer(items)
         self.sizes = AdamWSizes()
         _check(load().fp8_adamw_plan_size(items, count, ctypes.byref(self.sizes)), "fp8_adamw_plan_size")
         host = torch.zeros(max(16, self.sizes.table_bytes), dtype=torch.uint8)
@@ -758,7 +765,7 @@ class AdamWPlan:
         # the copy from pageable memory returns when the stream has done it, and with it the zeros: any stream may use the plan
         self.workspace = torch.zeros(self.sizes.workspace_bytes, dtype=torch.uint8, device=device)
         self.table = host.to(device)
-        self.device = device.index if device.index is not None else torch.cuda.current_device()
+        self.device = device
         self._call = (ctypes.byref(self.sizes), self.table.data_ptr(), self.workspace.data_ptr())
 
 

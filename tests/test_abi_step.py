@@ -171,3 +171,7 @@ def test_struct_layouts_match_the_header(tmp_path):
     assert api._pack_cross_entropy(1, 2, 3, 1, 2, 6, 7) == bytes(api.CrossEntropyDesc(1, 2, 3, 1, 2, 6, 7))
     o = api.AdamWOptions(1e-3, 0.9, 0.99, 1e-8, 5, 6, 16, 32, 64, 2.0)
     assert api._pack_adamw(1e-3, 0.9, 0.99, 1e-8, 5, 6, 16, 32, 64, 2.0) == bytes(o)
+    item = bytearray(ctypes.sizeof(api.AdamWItem))
+    api._pack_adamw_item_into(item, 0, 16, 32, 48, 64, 80, 96, 112, 128, 144, 7, 0.5, 1, 0, 1, 3)
+    want = api.AdamWItem(16, 32, 48, 64, 80, 96, 112, 128, 144, 7, 0.5, 1, 0, 1, 3)
+    assert bytes(item) == bytes(want)
