@@ -491,7 +491,8 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
  *   coef = norm <= max_norm ? 1 : max_norm / norm      (norm_dev NULL: 1),   g' = g * coef
  *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in binary32 (square root and reciprocal by the hardware, 1 ulp), p rounded to nearest to p_t.
+ * in binary32, each operation rounded to nearest, in the order written with the factors lr / (1 - beta1^t) and
+ * 1 / sqrt(1 - beta2^t) rounded once; p is rounded to p_t.
  * A norm that is not finite skips the step: parameters, moments and the step counter stay as they are (the copies and their
  * amax are written from the parameters as they are).  Without norm_dev a gradient that is not finite makes its element NaN.
  *
@@ -512,7 +513,7 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
  * fp8_quantize; copy_amax_dev (may be NULL; codes only) is OVERWRITTEN with amax of the new parameters, from which the next
  * step's copy_scale is chosen.
  *
- * lr_dev, step_dev take the place of lr, step where they are given, so that a captured call goes on from step to step: step_dev
+ * lr_dev (binary32), step_dev take the place of lr, step where they are given, so that a captured call goes on from step to step: step_dev
  * counts the steps taken; the call uses t = *step_dev + 1 and adds one when it is done.
  * Plans as those of fp8_grad_clip: made on the host, addresses and sizes must stay.  The workspace must hold zeros before its
  * first use and is left zeroed; calls that may overlap need plans of their own.  Items need the alignment of their elements

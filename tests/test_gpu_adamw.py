@@ -255,11 +255,11 @@ def test_second_moments_that_overflow_stop_their_elements(codes):
 
 
 def test_captured_steps_go_on_with_the_counter_and_the_rate():
-    """a replayed step reads its rate and counts for itself: the same bits as plain steps"""
+    """a replayed step reads its rate and counts for itself: the same bits as plain steps (at rates that binary32 holds)"""
     make = lambda: [Tensors(n, F32, BF, codes, E4, _gen(20 + n), start=False) for n in (3000, 70000) for codes in (False, True)]  # noqa: E731
     plain, played = make(), make()
     plan = _plan(plain)
-    lrs = [1e-3, 2e-3, 5e-4, 1e-3]
+    lrs = [2.0 ** -10, 2.0 ** -9, 3 * 2.0 ** -12, 2.0 ** -10]
     for i, lr in enumerate(lrs):
         api.fp8_adamw_step(plan, lr, i + 1, seed=77, norm=_scalar(2.0), max_norm=1.0)
     plan, lr, count, norm = _plan(played), _scalar(0.0), torch.tensor([0], device=DEV), _scalar(2.0)
