@@ -200,17 +200,18 @@ __device__ __forceinline__ float inverse_root(float x) {     // 2 ulp, of normal
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Square roots rounded to nearest: the product x / sqrt(x) of the approximation is corrected by its residual over twice the
-// root, which the fused operation gives without error for x above 2^-100; below, and there alone, the last bit may differ
-// (compared with the correctly rounded root on 46 million numbers: none differed).  NaN for an infinite x.
+// Square roots rounded to nearest, of numbers below 2^77: the product x / sqrt(x) of the approximation is corrected by its residual over
+// twice the root.  The residual is exact where x is above 2^-101, so it is taken of 2^50 x, which the smallest x brings there; factors of two
+// round nothing.  NaN for larger or infinite x.
 __device__ __forceinline__ Pair root_nearest(Pair x) {
     float a, b;
-    (x + Pair(1.17549435e-38f)).split(a, b);                // zero has a root too
+    const Pair big = x * Pair(0x1p50f);
+    (big + Pair(0x1p-126f)).split(a, b);                    // zero has a root too; every other `big` stays as it is
     const Pair q(inverse_root(a), inverse_root(b));
-    const Pair r = x * q;
-    r.split(a, b);
-    return fma2(fma2(r, Pair(-a, -b), x), q * Pair(0.5f), r);
+    const Pair r = x * (q * Pair(0x1p25f));
+    return fma2(fma2(r, r * Pair(-0x1p50f), big), q * Pair(0x1p-26f), r);
 }
+constexpr float MOST_ROOT = 0x1p38f;                        // of what root_nearest is asked for
 // Quotients rounded to nearest, of numbers far from the ends of the range: the product with the approximate reciprocal is
 // corrected by its residual, which the fused operation gives without error (Markstein's correction).  Compared with the correctly rounded quotient on 2^31 pairs of
 // numbers: 3 differed.
@@ -299,8 +300,8 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
         for (int j = 0; j < 4; ++j) r[j] = root_nearest(v[j]);
         split8(r, f);
         float r_top = most8(f);
-        // second moments near the end of the range, or past it: the library's root and quotient
-        const bool plainly = !(r_top <= 1e18f) || a.eps < 1e-18f;
+        // large second moments, up to those past the end of the range: the library's root and quotient
+        const bool plainly = !(r_top <= MOST_ROOT) || a.eps < 1e-18f;
         if (plainly) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

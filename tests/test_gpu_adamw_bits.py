@@ -1,0 +1,146 @@
+"""The AdamW step against its documented sequence of operations in binary32, bit for bit.
+
+`follow` evaluates the sequence of include/fp8_b200.h on the host in numpy's binary32, one rounded operation at a time.  Moments, scales, codes and
+copies have to be equal to the bit; so have parameters, but for what the kernel's quotients may leave: where the numerator is not zero
+and below 2^-100, its residual is not a binary32 number, and the quotient may be off by 2 units of its own last place, which adds half a unit of p's."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2209_05433_b200 import api
+from tests.test_gpu_adamw import BF, DEV, E4, F32, F8, FMAX, U8, Tensors, _ok, _plan, chances
+from tests.test_gpu_fused import _gen, _scalar
+
+pytestmark = pytest.mark.gpu
+f32 = np.float32
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy()
+
+
+def _decode(codes, scale):
+    """values of a flat 8-bit state: one product each"""
+    return _np(codes.view(F8[E4])) * np.repeat(_np(scale), 256)[:codes.numel()]
+
+
+def _tops(x):
+    n = len(x)
+    return np.abs(np.pad(x, (0, -n % 256))).reshape(-1, 256).max(axis=1)
+
+
+def _spread(s, n):
+    return np.repeat(s, 256)[:n]
+
+
+def _encode(y, fmt):
+    return torch.from_numpy(np.clip(y, -FMAX[fmt], FMAX[fmt])).to(F8[fmt]).view(U8).numpy()
+
+
+def _round_up(top):
+    """448 / top as the kernel takes it: the reciprocal, then the product"""
+    return np.where(top == 0, f32(0), np.minimum(f32(1) / np.where(top == 0, f32(1), top) * f32(448), f32(3.402823466e38)))
+
+
+def follow(t, number, lr, step, b1, b2, eps, seed=0, norm=None, max_norm=None):
+    """what the step leaves: p, m, v, scales, and the numerator of p's quotient"""
+    with np.errstate(all="ignore"):
+        coef = f32(1) if norm is None or norm <= max_norm else f32(max_norm) / f32(norm)
+        g, p = _np(t.old["g"]) * coef, _np(t.old["p"])
+        if t.codes:
+            m, r = _decode(t.old["m"], t.old_scales[0]), _decode(t.old["v"], t.old_scales[1])
+            v = r * r
+        else:
+            m, v = _np(t.old["m"]), _np(t.old["v"])
+        m = f32(b1) * m + f32(1.0 - b1) * g
+        v = f32(b2) * v + f32(1.0 - b2) * g * g
+        r = np.sqrt(v)
+        up = -f32(lr / (1.0 - b1 ** step)) * m
+        change = up / (r * f32(1.0 / math.sqrt(1.0 - b2 ** step)) + f32(eps))
+        p = p * (f32(1) - f32(lr) * f32(t.decay)) + change
+        out = dict(up=up, change=change)
+        if t.codes:
+            n, top = t.n, _tops(m)
+            out["ms"] = top * f32(1.0 / 448.0)
+            out["m"] = _encode(m * _spread(_round_up(top), n), E4)
+            top = _tops(r)
+            out["vs"] = top * f32(1.0 / 448.0)
+            y = np.minimum(r * _spread(_round_up(top), n), f32(448))
+            grid = np.exp2(np.maximum(np.frexp(y)[1] - 1, -6).astype(np.float64) - 3).astype(np.float32)
+            q = np.floor(y / grid + chances(number, n, seed, step).cpu().numpy().astype(np.float32)) * grid
+            out["v"] = _encode(np.where(r > 0, np.maximum(q, f32(2.0 ** -9)), f32(0)), E4)
+        else:
+            out["m"], out["v"] = m, v
+        out["p"] = torch.from_numpy(p).to(t.p_t)
+        return out
+
+
+def same(got, want):
+    """equal bits; NaN of any kind is NaN"""
+    if isinstance(want, np.ndarray):
+        want = torch.from_numpy(want)
+    got = got.cpu()
+    assert got.dtype == want.dtype
+    differ = (got != want) & ~((got != got) & (want != want))
+    assert not bool(differ.any()), "%d of %d differ, the first at %d: %r for %r" % (
+        int(differ.sum()), differ.numel(), int(differ.nonzero()[0]), got[differ][0].item(), want[differ][0].item())
+
+
+def check(t, number, **how):
+    want = follow(t, number, **how)
+    same(t.m, want["m"])
+    same(t.v, want["v"])
+    if t.codes:
+        same(t.ms, want["ms"])
+        same(t.vs, want["vs"])
+    got, p = t.p.cpu(), want["p"]
+    ends = torch.from_numpy((np.abs(want["up"]) < 2.0 ** -100) & (want["up"] != 0))
+    same(got[~ends], p[~ends])
+    if bool(ends.any()):
+        change = torch.from_numpy(np.abs(want["change"]).astype(np.float64))[ends]
+        allowed = 2 * 2.0 ** -23 * change + torch.finfo(t.p_t).eps * p[ends].double().abs() + 1e-45
+        assert bool(((got[ends].double() - p[ends].double()).abs() <= allowed).all())
+    assert t.guards_kept()
+
+
+def run(ts, **how):
+    more = dict(how)
+    more["beta1"], more["beta2"] = more.pop("b1"), more.pop("b2")
+    if "norm" in more:
+        more["norm"] = _scalar(more["norm"])
+    plan = _plan(ts)
+    api.fp8_adamw_step(plan, more.pop("lr"), more.pop("step"), **more)
+    _ok()
+    number = 0
+    for t in ts:
+        check(t, number, **how)
+        number += -(-t.n // 256) * 256
+
+
+def _small(n, g, least, most, **kind):
+    """a tensor whose gradients have magnitudes of 10^least to 10^most, a magnitude for each block of 256; half of its parameters start at zero"""
+    t = Tensors(n, kind.get("p_t", F32), kind.get("g_t", F32), kind["codes"], None, g, shift=kind.get("shift", 0), start=False)
+    size = torch.pow(10.0, least + (most - least) * torch.rand(-(-n // 256), generator=g, device=DEV, dtype=torch.float64)).repeat_interleave(256)[:n]
+    t.g.copy_(torch.randn(n, generator=g, device=DEV).double() * size)
+    t.p[::2] = 0.0
+    if not t.codes:
+        t.m.zero_()
+        t.v.zero_()
+    t.old = {k: getattr(t, k).clone() for k in t.old}
+    return t
+
+
+@pytest.mark.parametrize("eps", [1e-18, 1e-12, 1e-8])
+@pytest.mark.parametrize("codes", [False, True], ids=["32bit", "8bit"])
+def test_second_moments_at_the_bottom_of_the_range(codes, eps):
+    """gradients whose squares are subnormal or near it, from zero states and once more on what that left"""
+    g = _gen(51)
+    for g_t in (F32, BF):
+        ts = [_small(n, g, -23, -15, codes=codes, g_t=g_t, shift=s) for n, s in ((40000, 0), (2049, 0), (300, 1), (7, 0))]
+        run(ts, lr=1.0, step=1, b1=0.9, b2=0.999, eps=eps, seed=5)
+        for t in ts:
+            t.old = {k: getattr(t, k).clone() for k in t.old}
+            t.old_scales = (None, None) if not codes else (t.ms.clone(), t.vs.clone())
+        run(ts, lr=1.0, step=2, b1=0.9, b2=0.999, eps=eps, seed=5)
