@@ -497,10 +497,13 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
  * amax are written from the parameters as they are).  Without norm_dev a gradient that is not finite makes its element NaN.
  *
  * States.  FP8_STATE_F32: m and v are n floats.  FP8_STATE_E4M3: n codes each, in blocks of 256 consecutive elements with a
- * scale each (m_scale, v_scale: ceil(n / 256) floats), value = code * scale, scale = the block's largest magnitude / 448:
+ * scale each (m_scale, v_scale: ceil(n / 256) floats), value = code * scale.  With top = the block's largest magnitude,
+ * scale = top * binary32(1 / 448), and what becomes a code is x * ((1 / top) * 448), each operation rounded (0 where top is 0):
  *   m holds the first moment, rounded to nearest;
  *   v holds the SQUARE ROOT of the second moment, rounded up or down with the probability of its distance (to nearest it would
  *     stand still: with beta2 near 1 it moves less than half a step at a time); one that is not zero keeps at least code 1.
+ *   A first moment's scale below 2^-126 has few bits, and is 0 for a top below 3.2e-43.  For a top below 2^-119 the codes are
+ *     those of (m * 2^100) * (1 / (scale * 2^100)), so that code * scale is m as nearly as the scale allows, or 0 where the scale is.
  * With independent normal gradients v's root then scatters around its exact value by 9 % (beta2 = 0.9), 11 % (0.95), 15 % (0.99) or
  * 16 % (0.999) of it, its square is 1 to 5 % high in the mean, and the updates differ by 8 to 14 % of their mean from those
  * with binary32 moments.

@@ -234,8 +234,9 @@ __device__ __forceinline__ void split8(const Pair (&p)[4], float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) p[j].split(v[2 * j], v[2 * j + 1]);
 }
-// what brings a block's largest magnitude to 448; 0 for a block of zeros
-__device__ __forceinline__ float to_448(float most) { return most == 0.0f ? 0.0f : fminf(__frcp_rn(most) * 448.0f, 3.402823466e38f); }
+// what brings a block's largest magnitude, of 0 or from SMALL on, to 448; 0 for a block of zeros
+constexpr float SMALL = 0x1p-119f;
+__device__ __forceinline__ float to_448(float most) { return most == 0.0f ? 0.0f : __frcp_rn(most) * 448.0f; }
 
 // Code of y in [0, 448] rounded up with the probability of its distance from the code below: floor(y / step + u), u = chance / 65536.
 // Above the smallest normal value (2^-6) the step is an eighth of the power of two below y, and 8 .. 16 steps make up y, so the
@@ -330,7 +331,16 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
             split8(m, y);
             // largest magnitudes of the block (a NaN is larger than any number), and each half of the warp one factor
             const float m_most = __uint_as_float(warp_max_u32(__float_as_uint(most8(y)))), r_most = __uint_as_float(warp_max_u32(__float_as_uint(r_top)));
-            const float up = to_448((threadIdx.x & 16) ? r_most : m_most);
+            w.ms = m_most * (1.0f / 448.0f);
+            w.vs = r_most * (1.0f / 448.0f);
+            float up = to_448((threadIdx.x & 16) ? r_most : m_most);
+            if (m_most < SMALL) {
+                // The factor would overflow, and the scale is subnormal: codes of m over the scale as it is stored, both brought up by
+                // a power of two.  A scale of 0 makes them 0.  (No root of a second moment is that small.)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m[j] = m[j] * Pair(0x1p100f);
+                if (!(threadIdx.x & 16)) up = w.ms == 0.0f ? 0.0f : __frcp_rn(w.ms * 0x1p100f);
+            }
             const Pair m_up(__shfl_sync(0xFFFFFFFFu, up, 0)), r_up(__shfl_sync(0xFFFFFFFFu, up, 16));
 #pragma unroll
             for (int j = 0; j < 4; ++j) (m[j] * m_up).split(y[2 * j], y[2 * j + 1]);
@@ -345,8 +355,6 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = fminf(y[j], 448.0f);
             store_codes(e.v, i, count, encode8_chance(y, words));
-            w.ms = m_most * (1.0f / 448.0f);
-            w.vs = r_most * (1.0f / 448.0f);
         } else {
             uint32_t t[8];
             split8(m, f);

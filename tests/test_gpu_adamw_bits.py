@@ -39,9 +39,17 @@ def _encode(y, fmt):
     return torch.from_numpy(np.clip(y, -FMAX[fmt], FMAX[fmt])).to(F8[fmt]).view(U8).numpy()
 
 
-def _round_up(top):
+def _up(top):
     """448 / top as the kernel takes it: the reciprocal, then the product"""
-    return np.where(top == 0, f32(0), np.minimum(f32(1) / np.where(top == 0, f32(1), top) * f32(448), f32(3.402823466e38)))
+    return np.where(top == 0, f32(0), f32(1) / np.where(top == 0, f32(1), top) * f32(448))
+
+
+def _times_448_over(x, top, scale):
+    """what is rounded to codes; where the largest magnitude is below 2^-119, x over the scale, or 0 where that is 0"""
+    n = len(x)
+    small, at_all = _spread(top < 2.0 ** -119, n), _spread(scale > 0, n)
+    over = (x * f32(2.0 ** 100)) * np.where(at_all, f32(1) / (_spread(scale, n) * f32(2.0 ** 100)), f32(0))
+    return np.where(small, over, x * _spread(_up(top), n))
 
 
 def follow(t, number, lr, step, b1, b2, eps, seed=0, norm=None, max_norm=None):
@@ -64,10 +72,10 @@ def follow(t, number, lr, step, b1, b2, eps, seed=0, norm=None, max_norm=None):
         if t.codes:
             n, top = t.n, _tops(m)
             out["ms"] = top * f32(1.0 / 448.0)
-            out["m"] = _encode(m * _spread(_round_up(top), n), E4)
+            out["m"] = _encode(_times_448_over(m, top, out["ms"]), E4)
             top = _tops(r)
             out["vs"] = top * f32(1.0 / 448.0)
-            y = np.minimum(r * _spread(_round_up(top), n), f32(448))
+            y = np.minimum(r * _spread(_up(top), n), f32(448))
             grid = np.exp2(np.maximum(np.frexp(y)[1] - 1, -6).astype(np.float64) - 3).astype(np.float32)
             q = np.floor(y / grid + chances(number, n, seed, step).cpu().numpy().astype(np.float32)) * grid
             out["v"] = _encode(np.where(r > 0, np.maximum(q, f32(2.0 ** -9)), f32(0)), E4)
@@ -144,3 +152,17 @@ def test_second_moments_at_the_bottom_of_the_range(codes, eps):
             t.old = {k: getattr(t, k).clone() for k in t.old}
             t.old_scales = (None, None) if not codes else (t.ms.clone(), t.vs.clone())
         run(ts, lr=1.0, step=2, b1=0.9, b2=0.999, eps=eps, seed=5)
+
+
+@pytest.mark.parametrize("eps", [1e-18, 1e-8])
+def test_first_moments_at_the_bottom_of_the_range(eps):
+    """8-bit first moments whose scales are subnormal, or too small to be there at all; besides the bits, that they are worth what they
+    should be: within half a step of a code, 2^-4, and half a step of the scale, 2^-150, 448 times"""
+    g = _gen(52)
+    ts = [_small(n, g, -45, -33, codes=True, shift=s) for n, s in ((60000, 0), (2049, 0), (300, 1), (7, 0))]
+    run(ts, lr=1.0, step=1, b1=0.9, b2=0.999, eps=eps)
+    for t in ts:
+        exact = t.g.double() * 0.1
+        worth = t.m.view(F8[E4]).double() * t.ms.double().repeat_interleave(256)[:t.n]
+        top = torch.nn.functional.pad(exact, (0, -t.n % 256)).view(-1, 256).abs().amax(1).repeat_interleave(256)[:t.n]
+        assert bool(((worth - exact).abs() <= 2.0 ** -4 * 1.001 * exact.abs() + top * 2.0 ** -18 + 448 * 2.0 ** -150 * 1.01 + 2.0 ** -149).all())
