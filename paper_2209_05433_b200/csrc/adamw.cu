@@ -269,6 +269,7 @@ struct Step {
     float coef, rate, root2, lr;                            // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
     uint32_t key;
     int skip;
+    bool plainly;                                           // the library's root and quotient for all
 };
 
 // One block of 256 that is in registers: moments, parameters and what is stored.  i: the lane's first element; count: 8, or what
@@ -281,7 +282,9 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
     if (!s.skip) {
         values<P_BF16>(w.p, p);
         values<G_BF16>(w.g, g);
+        bool fits;                                          // the first moment beside a second one that does; the gradient's share is in s.plainly
         if (CODES) {
+            fits = fabsf(w.ms * s.rate) <= 1e14f;           // a code is 448 at most
             decode8(w.m, Pair(w.ms), m);
             decode8(w.v, Pair(w.vs), r);
 #pragma unroll
@@ -289,6 +292,9 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
         } else {
             values<false>(*reinterpret_cast<uint32_t(*)[8]>(w.m), m);
             values<false>(*reinterpret_cast<uint32_t(*)[8]>(w.v), v);
+            float old[8];
+            split8(m, old);
+            fits = most8(old) * fabsf(s.rate) <= 1e17f;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -301,8 +307,8 @@ __device__ __forceinline__ float update_block(const Params& a, const Entry& e, c
         for (int j = 0; j < 4; ++j) r[j] = root_nearest(v[j]);
         split8(r, f);
         float r_top = most8(f);
-        // large second moments, up to those past the end of the range: the library's root and quotient
-        const bool plainly = !(r_top <= MOST_ROOT) || a.eps < 1e-18f;
+        // moments or an eps that bring the steps of the root or the quotient near the end of the range, or past it: the library's
+        const bool plainly = !(r_top <= MOST_ROOT) || s.plainly || !fits;
         if (plainly) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -499,6 +505,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) k_adamw(const Params a) 
             s.rate = (float)((a.lr_dev ? (double)s.lr : a.lr) / -expm1((double)t * a.ln_beta1));
             s.root2 = (float)(1.0 / sqrt(-expm1((double)t * a.ln_beta2)));
         }
+        // a root of MOST_ROOT at most leaves g' at most MOST_ROOT / sqrt(rest2): times the rate, below 1e17 too
+        s.plainly = a.eps < 1e-18f || a.eps > 1e18f || !(fabsf(s.rate) * MOST_ROOT <= 1e17f * sqrtf(a.rest2));
         s.key = mix((uint32_t)a.seed ^ mix((uint32_t)(a.seed >> 32) ^ mix((uint32_t)t)));
     }
     float most = 0.0f;

@@ -91,7 +91,8 @@ def same(got, want):
         want = torch.from_numpy(want)
     got = got.cpu()
     assert got.dtype == want.dtype
-    differ = (got != want) & ~((got != got) & (want != want))
+    nan = lambda x: (x & 0x7F) == 0x7F if x.dtype == U8 else x != x  # noqa: E731
+    differ = (got != want) & ~(nan(got) & nan(want))
     assert not bool(differ.any()), "%d of %d differ, the first at %d: %r for %r" % (
         int(differ.sum()), differ.numel(), int(differ.nonzero()[0]), got[differ][0].item(), want[differ][0].item())
 
@@ -166,3 +167,33 @@ def test_first_moments_at_the_bottom_of_the_range(eps):
         worth = t.m.view(F8[E4]).double() * t.ms.double().repeat_interleave(256)[:t.n]
         top = torch.nn.functional.pad(exact, (0, -t.n % 256)).view(-1, 256).abs().amax(1).repeat_interleave(256)[:t.n]
         assert bool(((worth - exact).abs() <= 2.0 ** -4 * 1.001 * exact.abs() + top * 2.0 ** -18 + 448 * 2.0 ** -150 * 1.01 + 2.0 ** -149).all())
+
+
+@pytest.mark.parametrize("eps", [1e-18, 1e-8, 1e15, 1e25, 1e38])
+def test_first_moments_that_do_not_fit_their_second_ones(eps):
+    """states that were not grown together, infinities among them: quotients that overflow, or have a divisor whose reciprocal is subnormal"""
+    for n, shift in ((3000, 0), (100, 1)):
+        t = Tensors(n, F32, F32, False, None, _gen(53), shift=shift)
+        at = torch.arange(n, device=DEV)
+        for k, value in enumerate((float("inf"), -float("inf"), 1e30, -3e38, 1e20, 0.0)):
+            t.m[at % 97 == 2 * k] = value
+        t.v[at % 2 == 0] = 0.0
+        t.g[at % 3 == 0] = 0.0
+        t.old = {k: getattr(t, k).clone() for k in t.old}
+        run([t], lr=1e-2, step=3, b1=0.9, b2=0.99, eps=eps)
+        t = Tensors(n, F32, BF, True, None, _gen(54), shift=shift)
+        values = torch.tensor([1e30, float("inf"), 1e12, 3.4e38, 1e-5, 1e18], device=DEV)
+        t.ms.copy_(values[torch.arange(t.ms.numel(), device=DEV) % 6])
+        t.vs[::4] = 0.0
+        t.g[torch.arange(n, device=DEV) % 3 == 0] = 0.0
+        t.old = {k: getattr(t, k).clone() for k in t.old}
+        t.old_scales = t.ms.clone(), t.vs.clone()
+        run([t], lr=1e-2, step=3, b1=0.9, b2=0.99, eps=eps, seed=9)
+
+
+@pytest.mark.parametrize("lr", [1e-3, 1e6, 1e20])
+def test_rates_and_gradients_of_any_size(lr):
+    g = _gen(55)
+    for codes in (False, True):
+        ts = [_small(n, g, -10, 19, codes=codes, shift=s) for n, s in ((40000, 0), (300, 1))]
+        run(ts, lr=lr, step=1, b1=0.9, b2=0.999, eps=1e-8, seed=6)
