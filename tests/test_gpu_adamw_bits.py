@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from paper_2209_05433_b200 import api
-from tests.test_gpu_adamw import BF, DEV, E4, F32, F8, FMAX, U8, Tensors, _ok, _plan, chances
+from tests.test_gpu_adamw import BF, DEV, E4, F32, F8, FMAX, U8, Tensors, _check_copy, _ok, _plan, chances
 from tests.test_gpu_fused import _gen, _scalar
 
 pytestmark = pytest.mark.gpu
@@ -197,3 +197,28 @@ def test_rates_and_gradients_of_any_size(lr):
     for codes in (False, True):
         ts = [_small(n, g, -10, 19, codes=codes, shift=s) for n, s in ((40000, 0), (300, 1))]
         run(ts, lr=lr, step=1, b1=0.9, b2=0.999, eps=1e-8, seed=6)
+
+
+KINDS = [(p, g, codes) for p in (F32, BF) for g in (F32, BF) for codes in (False, True)]
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: "%s-%s-%s" % (str(k[0])[6:], str(k[1])[6:], "8bit" if k[2] else "32bit"))
+@pytest.mark.parametrize("numbers", [dict(lr=2e-3, step=7, b1=0.9, b2=0.98, eps=1e-8, seed=0x123456789ABC, norm=3.0, max_norm=1.25),
+                                     dict(lr=0.3, step=1, b1=0.0, b2=0.0, eps=1e-12), dict(lr=1e-4, step=100000, b1=0.95, b2=0.9999, eps=1e-6, seed=3)],
+                         ids=["clipped", "no memory", "long run"])
+def test_every_operation_is_rounded_as_documented(kind, numbers):
+    g = _gen(56)
+    sizes = [1, 7, 8, 255, 256, 257, 1000, 2048, 2049, 33333, 100001]
+    copies = [None, "bf16", E4]
+    ts = [Tensors(n, *kind, copies[i % 3], g, shift=i % 3 if i % 2 else 0, decay=0.1 * (i % 3)) for i, n in enumerate(sizes)]
+    run(ts, **numbers)
+    for t in ts:
+        _check_copy(t)
+
+
+@pytest.mark.parametrize("codes", [False, True], ids=["32bit", "8bit"])
+def test_roots_and_quotients_of_many_numbers(codes):
+    """8 million roots and quotients of ordinary size beside the host's.  (A root's correction is exact arithmetic; a quotient's reciprocal is
+    only near, which leaves about one in 10^9 an ulp off: none is to be expected here.)"""
+    t = _small(1 << 23, _gen(57), -9, 0, codes=codes)
+    run([t], lr=1e-2, step=1, b1=0.9, b2=0.999, eps=1e-8, seed=8)
