@@ -34,7 +34,6 @@ constexpr int64_t LEAST_CHUNK = 2048;                      // elements of a tens
 constexpr int64_t MOST_CHUNK = 65536;                      // at most, and
 constexpr int64_t MOST_CHUNK_32 = 8192;                    // in lists without 8-bit moments (268M parameters 1095 us; 1113 with 16384)
 constexpr int CTAS_PER_SM = 3;                             // 80 registers a thread; at 4 they spill
-constexpr int64_t AT_A_TIME = 148 * CTAS_PER_SM;           // CTAs that the GPU holds
 static_assert(MOST_CHUNK <= 32 * WARPS * BLOCK, "a lane for the scales of each of a warp's blocks");
 
 struct Entry {
@@ -588,17 +587,17 @@ fp8_status fp8_adamw_plan_size(const fp8_adamw_item* items, int64_t count, fp8_a
         amaxes += it.copy_amax_dev ? 1 : 0;
     }
     // The chunk is the smallest with which the CTAs fill whole rounds of what the GPU holds at a time, as few rounds as there can
-    // be: CTAs start together and end together.
-    int64_t chunk = LEAST_CHUNK, chunks = 0;
-    for (int64_t rounds = (total + most_chunk * AT_A_TIME - 1) / (most_chunk * AT_A_TIME);; ++rounds) {
-        chunk = total / (rounds > 0 ? rounds * AT_A_TIME : 1) / LEAST_CHUNK * LEAST_CHUNK;
-        for (chunk = chunk < LEAST_CHUNK ? LEAST_CHUNK : chunk; chunk <= most_chunk; chunk += LEAST_CHUNK) {
-            chunks = 0;
-            for (int64_t i = 0; i < count; ++i) chunks += (items[i].n + chunk - 1) / chunk;
-            if (chunks <= rounds * AT_A_TIME) break;
-        }
-        if (chunk <= most_chunk) break;
-    }
+    // be: CTAs start together and end together.  The largest chunk says how few: no chunk needs fewer.
+    const int64_t at_a_time = (int64_t)sm_count() * CTAS_PER_SM;
+    auto chunks_of = [&](int64_t chunk) {
+        int64_t n = 0;
+        for (int64_t i = 0; i < count; ++i) n += (items[i].n + chunk - 1) / chunk;
+        return n;
+    };
+    const int64_t fewest = chunks_of(most_chunk), rounds = fewest > 0 ? (fewest + at_a_time - 1) / at_a_time : 1;
+    int64_t chunk = total / (rounds * at_a_time) / LEAST_CHUNK * LEAST_CHUNK, chunks;
+    if (chunk < LEAST_CHUNK) chunk = LEAST_CHUNK;
+    while ((chunks = chunks_of(chunk)) > rounds * at_a_time) chunk += LEAST_CHUNK;
     if (chunks > 0x7FFFFFFF) return FP8_ERR_UNSUPPORTED;
     plan->count = count;
     plan->chunks = chunks;
