@@ -9,7 +9,9 @@
 // its epilogue turns it into dz (E5M2 codes for FP8 operands, bf16 for bf16), and two products read dz.  dx is added up
 // over the pieces in binary32.
 //
-// Exponentials are taken to base 2 of logits that were scaled by log2(e) with the operands' inverse scales.
+// A logit is rounded to binary32 before anything is subtracted from it, and only the difference is scaled to base 2: where one
+// logit stands alone, its lse is that number, and the gradient there softmax - 1 = 0, however large it is.  So the backward pass has
+// to find the forward pass's bits: both add the products in the same order.
 //
 // All products here are one kernel on persistent CTAs or CTA pairs: TMA-fed ring, tcgen05 into two TMEM accumulators, and
 // eight epilogue warps that take the accumulator into registers every 2048 of K (logits of bf16 operands: 512; partial sums
@@ -63,7 +65,7 @@ constexpr uint32_t TMEM_COLS = 512;
 constexpr int SHORT_K = 4;              // K-blocks of a product that is bound by its output
 constexpr int EPILOGUE_K = 8;           // K-blocks in whose time a tile's epilogue is done
 constexpr int GROUP_M = 16;             // row tiles that advance together over the columns
-constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+constexpr float LOG2E = 1.44269504088896341f;
 
 // codes written to the error latch
 enum : uint32_t { L_WAIT_EMPTY = 49, L_WAIT_FULL = 50, L_WAIT_ACC_EMPTY = 51, L_WAIT_ACC_FULL = 52 };
@@ -90,7 +92,7 @@ struct Params {
     const int64_t* target;
     int64_t first, vocab;               // vocabulary column of the first column here; all columns of the vocabulary
     float2* part;                       // [2 tiles_n][M]
-    float* logit;                       // [M]: the target's, times log2(e)
+    float* logit;                       // [M]: the target's
     const float* lse;
     const float* dloss;
     float* dz_scale;                    // written: scale of dz's codes and its inverse
@@ -121,6 +123,10 @@ __device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src,
     asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
+
+// (a - c, b - c) log2(e).  The differences one by one: as an addition of pairs they could come out fused with the product that made
+// a and b.
+__device__ __forceinline__ Pair base2(float a, float b, float c) { return Pair(__fsub_rn(a, c), __fsub_rn(b, c)) * Pair(LOG2E); }
 
 // tile index -> (row tile, column tile): GROUP_M row tiles share each sweep over the columns
 __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
@@ -229,9 +235,10 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const int m0 = (tm * CG + (int)rank) * ROWS, n0 = tn * BN + (int)rank * B_ROWS;
             const int kb0 = slice * q.slice_blocks, kn = min(q.slice_blocks, q.k_blocks - kb0);
             const int kn_pad = (kn + FG - 1) / FG * FG;
-            // Every second round starts at the end of K where the last one ended: L2 still has it.  The round is the tile's own, not the
-            // worker's count: a product's bits do not depend on what else is in the launch.
-            const bool backwards = (t / workers & 1) != 0;
+            // Every second round of dx or dw starts at the end of K where the last one ended: L2 still has it.  The round is the tile's own,
+            // not the worker's count: a product's bits do not depend on what else is in the launch.  Logits are always added up from the start, as
+            // their bits must not depend on the tiling either.
+            const bool backwards = MODE == MODE_OUT && (t / workers & 1) != 0;
             for (int kb = 0; kb < kn_pad; ++kb) {
                 ok = mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, L_WAIT_EMPTY);
                 if (!ok) break;
@@ -365,7 +372,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         uint32_t box = boxes, box_row = box + lane * 128;
         const uint64_t out_policy = MODE == MODE_DZ ? policy_evict_last() : policy_evict_first();      // dz is read next
         auto factor = [](const Product& q) { return (q.s[0] ? __ldg(q.s[0]) : 1.0f) * (q.s[1] ? __ldg(q.s[1]) : 1.0f); };
-        const float alpha0 = factor(p.q[0]) * (MODE != MODE_OUT ? LOG2E : 1.0f), alpha1 = MODE == MODE_OUT ? factor(p.q[1]) : 1.0f;
+        const float alpha0 = factor(p.q[0]), alpha1 = MODE == MODE_OUT ? factor(p.q[1]) : 1.0f;
         bool ok = true;
         int it = 0, which, t;
         float v[NC];
@@ -384,14 +391,14 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             const float alpha = MODE == MODE_OUT && which ? alpha1 : alpha0;
             int rel = -1;                                         // the target's column among this thread's, if it is there
             bool counted = false;
-            float g = 0.0f, lse2 = 0.0f;
+            float g = 0.0f, lse = 0.0f;
             if (MODE != MODE_OUT && row_ok) {
                 const int64_t target = __ldg(p.target + row), at = target - p.first - col0;
                 counted = target >= 0 && target < p.vocab;
                 if (at >= 0 && at < cols) rel = (int)at;
                 if (MODE == MODE_DZ) {
                     g = __ldg(p.dloss + row) * dz_scale;
-                    lse2 = __ldg(p.lse + row) * LOG2E;
+                    lse = __ldg(p.lse + row);
                 }
             }
             for (int kc = 0; kc < kn_pad && ok; kc += SPLIT, ++it) {
@@ -427,7 +434,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (row0 >= q.M) continue;                        // the whole warp
                 float top = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < NC; ++i) v[i] *= alpha;
+                for (int i = 0; i < NC; i += 2) (Pair(v[i], v[i + 1]) * Pair(alpha)).split(v[i], v[i + 1]);
                 if (cols < NC) {                                  // the tile at the right edge
 #pragma unroll
                     for (int i = 0; i < NC; ++i) v[i] = i < cols ? v[i] : -INFINITY;
@@ -442,10 +449,16 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
                 // a row of minus infinities keeps a sum of zero; a NaN or plus infinity makes the sum NaN
                 const float shift = top == -INFINITY ? 0.0f : top;
-                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                Pair s[2] = {Pair(0.0f), Pair(0.0f)};
 #pragma unroll
-                for (int i = 0; i < NC; ++i) s[i & 3] += exp2_fast(v[i] - shift);
-                if (row_ok) p.part[(int64_t)(2 * tn + half) * q.M + row] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+                for (int i = 0; i < NC; i += 2) {
+                    float a, b;
+                    base2(v[i], v[i + 1], shift).split(a, b);
+                    s[i >> 1 & 1] = s[i >> 1 & 1] + Pair(exp2_fast(a), exp2_fast(b));
+                }
+                float s0, s1;
+                (s[0] + s[1]).split(s0, s1);
+                if (row_ok) p.part[(int64_t)(2 * tn + half) * q.M + row] = make_float2(top, s0 + s1);
                 continue;
             }
             bool tail = false;                                    // this row's last columns are here, in `rest`
@@ -469,7 +482,13 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         const int base = c + sub * 32;
                         if (MODE == MODE_DZ) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] = exp2_fast(fmaf(v[base + i], alpha, -lse2));
+                            for (int i = 0; i < 32; i += 2) {
+                                float a, b;
+                                (Pair(v[base + i], v[base + i + 1]) * Pair(alpha)).split(a, b);
+                                base2(a, b, lse).split(a, b);
+                                y[i] = exp2_fast(a);
+                                y[i + 1] = exp2_fast(b);
+                            }
                             if (__any_sync(0xFFFFFFFFu, rel >= base && rel < base + 32)) {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) y[i] -= base + i == rel ? 1.0f : 0.0f;
@@ -563,7 +582,7 @@ __global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const fl
     grid_dependency_wait();
     auto join = [](float2 a, float2 b) {
         const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
-        return make_float2(top, a.y * exp2_fast(a.x - shift) + b.y * exp2_fast(b.x - shift));
+        return make_float2(top, a.y * exp2_fast((a.x - shift) * LOG2E) + b.y * exp2_fast((b.x - shift) * LOG2E));
     };
     const int64_t row = (int64_t)blockIdx.x * rows + row_in;
     float2 sum = make_float2(-INFINITY, 0.0f);
@@ -576,9 +595,9 @@ __global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const fl
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, w[j].x);
             const float shift = top == -INFINITY ? 0.0f : top;
-            float s = sum.y * exp2_fast(sum.x - shift);
+            float s = sum.y * exp2_fast((sum.x - shift) * LOG2E);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += w[j].y * exp2_fast(w[j].x - shift);
+            for (int j = 0; j < 8; ++j) s += w[j].y * exp2_fast((w[j].x - shift) * LOG2E);
             sum = make_float2(top, s);
         }
     }
@@ -588,11 +607,11 @@ __global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const fl
         if (threadIdx.x < d) got[threadIdx.x] = sum = join(sum, got[threadIdx.x + d]);
     }
     if (threadIdx.x < rows && row < M) {
-        const float l2 = log2f(sum.y);
+        const float l = logf(sum.y);
         const int64_t t = target[row];
-        lse[row] = (sum.x + l2) * LN2;
+        lse[row] = sum.x + l;
         // the largest logit and the target's are near each other where the loss is small: their difference first
-        loss[row] = t >= 0 && t < vocab ? ((sum.x - logit[row]) + l2) * LN2 : 0.0f;
+        loss[row] = t >= 0 && t < vocab ? (sum.x - logit[row]) + l : 0.0f;
     }
 }
 
