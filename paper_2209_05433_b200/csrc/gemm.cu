@@ -859,22 +859,19 @@ void loss_read_clear_latch(unsigned int out2[2]);          // defined with the l
 extern "C" {
 
 fp8_status fp8_async_status(uint32_t* detail) {
-    unsigned int latch[2] = {0u, 0u};
+    unsigned int latch[4][2] = {};
     if (cudaDeviceSynchronize() != cudaSuccess) return FP8_ERR_CUDA;
-    unsigned int cast_latch[2];
-    fp8_cast_read_clear_latch(cast_latch);
-    if (cast_latch[0] == 0u) fused_read_clear_latch(cast_latch);
-    if (cast_latch[0] == 0u) loss_read_clear_latch(cast_latch);
-    if (cudaMemcpyFromSymbol(latch, g_async_latch, sizeof(latch)) != cudaSuccess) return FP8_ERR_CUDA;
-    if (latch[0] == 0u && cast_latch[0] != 0u) {
-        if (detail) *detail = cast_latch[0];
-        return FP8_ERR_TIMEOUT;
-    }
-    if (detail) *detail = latch[0];
-    if (latch[0] == 0u) return FP8_OK;
+    // every file's, whatever the others say: what is not read now would be taken for a later call's error
+    if (cudaMemcpyFromSymbol(latch[0], g_async_latch, sizeof(latch[0])) != cudaSuccess) return FP8_ERR_CUDA;
+    fp8_cast_read_clear_latch(latch[1]);
+    fused_read_clear_latch(latch[2]);
+    loss_read_clear_latch(latch[3]);
     const unsigned int zero[2] = {0u, 0u};
-    if (cudaMemcpyToSymbol(g_async_latch, zero, sizeof(zero)) != cudaSuccess) return FP8_ERR_CUDA;
-    return FP8_ERR_TIMEOUT;
+    if (latch[0][0] != 0u && cudaMemcpyToSymbol(g_async_latch, zero, sizeof(zero)) != cudaSuccess) return FP8_ERR_CUDA;
+    unsigned int first = 0u;
+    for (int i = 0; i < 4 && first == 0u; ++i) first = latch[i][0];
+    if (detail) *detail = first;
+    return first == 0u ? FP8_OK : FP8_ERR_TIMEOUT;
 }
 
 }  // extern "C"
