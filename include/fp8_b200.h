@@ -573,7 +573,8 @@ fp8_status fp8_adamw_step(const fp8_adamw_plan* plan, const void* table_dev, voi
  * there give NaN.)
  * The gradient of the logits: FP8 operands take E5M2 codes encode(dz * s) with s = 57344 / max |dloss[t]| over the tokens that
  * count (1 where that is 0 or not finite): |dz| never exceeds it, so no amax of dz is needed, and what is below 1.2e-10 of it
- * becomes 0.  bf16 operands take bf16.  dz never leaves the workspace.
+ * becomes 0.  bf16 operands take bf16.  dz never leaves the workspace.  A dloss that is not finite, of a token that counts, makes
+ * that token's row of dx and all of dw NaN or (bf16) infinite.
  * Precision: products are exact, their sums as FP8_ACC_SPLIT; exponentials by the hardware (2 ulp).  z and lse are binary32
  * numbers, so exp(z - lse) may be off by 2^-24 |lse| of itself; but where one logit of a row stands alone, lse is that number,
  * and dz is exactly dloss or 0, as the backward pass adds up the same z.  A row with a NaN or a

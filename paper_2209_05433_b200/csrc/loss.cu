@@ -398,6 +398,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (at >= 0 && at < cols) rel = (int)at;
                 if (MODE == MODE_DZ) {
                     g = __ldg(p.dloss + row) * dz_scale;
+                    if (ESZ == 1 && !(fabsf(g) <= 3.402823466e38f)) g = NAN;      // codes saturate: an infinity would leave them finite
                     lse = __ldg(p.lse + row);
                 }
             }

@@ -96,3 +96,18 @@ def test_a_nan_in_a_weight(T, K, V):
     p.target.fill_(-1)                                            # nothing counts: dw is zero
     dx, dw = _run(p)
     assert not dw.any() and not p.loss.any()
+
+
+@pytest.mark.parametrize("fmt", [E4, None], ids=["fp8", "bf16"])
+@pytest.mark.parametrize("T,K,V", SHAPES)
+def test_an_infinite_factor_leaves_nothing_finite_of_its_token(T, K, V, fmt):
+    """a saturating conversion must not make numbers of it"""
+    p = loss.Problem(T, K, V, fmt, fmt, ignored=0.0)
+    for factor in (float("inf"), -float("inf"), float("nan")):
+        p.dloss[2] = factor
+        dx, dw = _run(p)
+        others = torch.arange(T, device=DEV) != 2
+        assert not torch.isfinite(dx[2]).any() and not torch.isfinite(dw).any() and bool(torch.isfinite(dx[others]).all())
+    p.target[2] = -5                                              # it does not count: nothing of it is looked at
+    dx, dw = _run(p)
+    assert not dx[2].any() and bool(torch.isfinite(dx).all()) and bool(torch.isfinite(dw).all())
