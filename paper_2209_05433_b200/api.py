@@ -734,6 +734,7 @@ class AdamWPlan:
         wide, f32, u8, bf16 = (torch.float32, torch.bfloat16), (torch.float32,), torch.uint8, torch.bfloat16
         size = ctypes.sizeof(AdamWItem)
         items = bytearray(size * max(1, count))
+        written: list[int] = []
         for i, (p, g, m, v, ms, vs, copy, scale, amax, decay) in enumerate(zip(*columns, decays)):
             n = p.numel()
             codes = m.dtype is u8
@@ -753,10 +754,16 @@ class AdamWPlan:
                     raise TypeError("a uint8 copy needs its format, E4M3 or E5M2, and its scale")
                 copy_t, scale_at = STORE_E4M3 + fmt, address(scale, f32, 1, "scale")
                 amax_at = 0 if amax is None else address(amax, f32, 1, "amax_out")
-            _pack_adamw_item_into(items, i * size, address(g, wide, n, "gradient"), address(p, wide, n, "parameter"), address(m, state, n, "exp_avg"),
-                                  address(v, state, n, "exp_avg_sq"), address(ms, f32, blocks, "exp_avg_scales") if codes else 0,
-                                  address(vs, f32, blocks, "exp_avg_sq_scales") if codes else 0, copy_at, scale_at, amax_at, n, decay,
-                                  BF16 if g.dtype is bf16 else F32, BF16 if p.dtype is bf16 else F32, 1 if codes else 0, copy_t)
+            at = (address(p, wide, n, "parameter"), address(m, state, n, "exp_avg"), address(v, state, n, "exp_avg_sq"),
+                  address(ms, f32, blocks, "exp_avg_scales") if codes else 0, address(vs, f32, blocks, "exp_avg_sq_scales") if codes else 0, copy_at)
+            _pack_adamw_item_into(items, i * size, address(g, wide, n, "gradient"), *at, scale_at, amax_at, n, decay, BF16 if g.dtype is bf16 else F32,
+                                  BF16 if p.dtype is bf16 else F32, 1 if codes else 0, copy_t)
+            if n > 0:
+                written.extend(filter(None, at))
+            if amax_at:
+                written.append(amax_at)
+        if len(set(written)) != len(written):
+            raise ValueError("a tensor that the step writes is in the plan twice")
         items = (AdamWItem * max(1, count)).from_buffer(items)
         self.sizes = AdamWSizes()
         _check(load().fp8_adamw_plan_size(items, count, ctypes.byref(self.sizes)), "fp8_adamw_plan_size")
