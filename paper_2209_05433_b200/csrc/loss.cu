@@ -48,9 +48,11 @@ constexpr int K_BYTES = 128;            // K-block: one 128-byte swizzle row, 12
 constexpr int K_STEP_BYTES = 32;        // K of one tcgen05.mma
 // Of K, what one use of the accumulator covers.  The tensor core truncates what it adds, once per K_STEP_BYTES: a logit that
 // grows steadily loses up to that many steps times 2^-24 of itself.  bf16 products have more bits to lose and half the steps
-// per use: with 2048 their loss was off by 6e-6 in root mean square (sums in binary32: 4e-6), with 512 by 1.5e-6 (FP8: 5e-7).  The
-// gradient of the logits takes the same, so that its logits are those of the sum; the products behind it are rounded coarsely.
-template <int ESZ, int MODE> constexpr int split_of = ESZ == 1 || MODE == MODE_OUT ? 2048 : 512;
+// per use: with 2048 their loss was off by 6e-6 in root mean square (sums in binary32: 4e-6), with 512 by 1.8e-6 (FP8 with 2048: 4e-7, sums in
+// binary32 9e-7, many tokens of width 8808).  Up to 128 tokens, where the weights' stream hides it, FP8 takes 512 too (75 tokens of width
+// 2306: lse off by 5e-7 instead of 1.7e-6, one token against 131072 x 4096 111 us as before).  The
+// gradient of the logits takes what the logits take, so that they are the same bits; the products behind it are rounded coarsely.
+template <int ESZ, int CG, int MODE> constexpr int split_of = MODE == MODE_OUT || (ESZ == 1 && CG == 2) ? 2048 : 512;
 constexpr int FG = 2;                   // K-blocks consumed per barrier wait
 constexpr int MAX_STAGES = 12;
 constexpr uint32_t A_BYTES = ROWS * K_BYTES;
@@ -173,7 +175,7 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     constexpr int B_ROWS = BN / CG;                               // columns of the tile that this CTA loads
     const uint32_t a_bytes = CG == 2 ? A_BYTES : p.a_bytes, stage_bytes = a_bytes + B_ROWS * K_BYTES;
     const uint32_t stages = CG == 2 && MODE != MODE_OUT ? RING_BYTES / (A_BYTES + B_ROWS * K_BYTES) : (uint32_t)p.stages;
-    constexpr int SPLIT = split_of<ESZ, MODE> / KE;                   // K-blocks per use of an accumulator
+    constexpr int SPLIT = split_of<ESZ, CG, MODE> / KE;                   // K-blocks per use of an accumulator
     constexpr int PARTS = MODE == MODE_DZ && BN == 128 ? 1 : 2;   // warps that share a row of a tile
     constexpr int ACTIVE = 4 * PARTS;                             // epilogue warps with something to do
     constexpr int NC = BN / PARTS;                                // columns of an epilogue thread
