@@ -48,11 +48,11 @@ constexpr int K_BYTES = 128;            // K-block: one 128-byte swizzle row, 12
 constexpr int K_STEP_BYTES = 32;        // K of one tcgen05.mma
 // Of K, what one use of the accumulator covers.  The tensor core truncates what it adds, once per K_STEP_BYTES: a logit that
 // grows steadily loses up to that many steps times 2^-24 of itself.  bf16 products have more bits to lose and half the steps
-// per use: with 2048 their loss was off by 6e-6 in root mean square (sums in binary32: 4e-6), with 512 by 1.8e-6 (FP8 with 2048: 4e-7, sums in
-// binary32 9e-7, many tokens of width 8808).  Up to 128 tokens, where the weights' stream hides it, FP8 takes 512 too (75 tokens of width
-// 2306: lse off by 5e-7 instead of 1.7e-6, one token against 131072 x 4096 111 us as before).  The
-// gradient of the logits takes what the logits take, so that they are the same bits; the products behind it are rounded coarsely.
-template <int ESZ, int CG, int MODE> constexpr int split_of = MODE == MODE_OUT || (ESZ == 1 && CG == 2) ? 2048 : 512;
+// per use: with 2048 their loss was off by 6e-6 in root mean square (sums in binary32: 4e-6), with 512 by 1.8e-6 (FP8 with 2048, many tokens
+// of width 8808: 4e-7, sums in binary32 9e-7).  Up to 128 tokens, where the stream of weights nearly hides it, FP8 takes 1024 (75 tokens of
+// width 2306: lse off by 8e-7 instead of 1.7e-6; with 512 5e-7, but one token against 131072 x 4096 takes 116 us, with 1024 112.6, with 2048
+// 111.3).  The gradient of the logits takes what the logits take, so that they are the same bits; the products behind it are rounded coarsely.
+template <int ESZ, int CG, int MODE> constexpr int split_of = MODE == MODE_OUT || (ESZ == 1 && CG == 2) ? 2048 : ESZ == 1 ? 1024 : 512;
 constexpr int FG = 2;                   // K-blocks consumed per barrier wait
 constexpr int MAX_STAGES = 12;
 constexpr uint32_t A_BYTES = ROWS * K_BYTES;
