@@ -492,7 +492,8 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
  *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * in binary32, each operation rounded to nearest, in the order written with the factors lr / (1 - beta1^t) and
- * 1 / sqrt(1 - beta2^t) rounded once; p is rounded to p_t.
+ * 1 / sqrt(1 - beta2^t) rounded once; p is rounded to p_t.  (A quotient may, rarely, be off by its last bit, or by two where its
+ * numerator is below 2^-100.)
  * A norm that is not finite skips the step: parameters, moments and the step counter stay as they are (the copies and their
  * amax are written from the parameters as they are).  Without norm_dev a gradient that is not finite makes its element NaN.
  *

@@ -699,8 +699,9 @@ STATE_BLOCK = 256            # elements of an 8-bit state that share a scale
 
 
 class AdamWPlan:
-    """The tensors that fp8_adamw_step goes over, laid out once, as ClipPlan does: lists of one length, each tensor contiguous
-    and once in the plan.
+    """The tensors that fp8_adamw_step goes over, laid out once, as ClipPlan does: lists of one length, each tensor contiguous,
+    and each that is written once in the plan.  Like ClipPlan it goes by the tensors' addresses, gradients' among them, and keeps them
+    alive; a step whose gradients live in other tensors needs a new one, whose making waits for the stream (288 tensors: 0.7 ms, one: 30 us).
 
     params, grads: float32 or bfloat16.  exp_avgs, exp_avg_sqs: float32, or uint8 codes (E4M3) with one float32 scale for every
     256 elements in exp_avg_scales, exp_avg_sq_scales; exp_avg_sqs then holds the square root of the second moment.  All of them

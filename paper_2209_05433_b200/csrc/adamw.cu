@@ -9,12 +9,14 @@
 // its distance.  To nearest, r would stand still: with b2 near 1 it moves by less than half a step at a time.  An r that is
 // not zero keeps at least the smallest code: a divisor must not vanish beside an m that did not.
 //
-// The arithmetic is rounded operation by operation, in the order written above, roots and quotients correctly: a rounding up or
-// down hangs on the last bit, and whoever follows the formula in binary32 gets the same parameters, moments and codes.
+// The arithmetic is rounded operation by operation, in the order written above: a rounding up or down hangs on the last bit, and
+// whoever follows the formula in binary32 gets the same moments, scales and codes, and the same parameters but for the few
+// quotients that come out a last bit off (none of 8 million; more where the numerator is below 2^-100).
 //
 // Bound by HBM: every element is read and written once.  A warp takes a block of 256, a lane eight neighbours of it.  268M
-// binary32 parameters with bf16 gradients and E4M3 copies: 1100 us with 32-bit moments (6.6 TB/s), 743 us with 8-bit ones (5.4 TB/s:
-// 55 instructions per element take half of the issue slots).  288 small tensors, 3M elements: 14.6 us.
+// binary32 parameters with bf16 gradients and E4M3 copies: 1124 us with 32-bit moments (6.5 TB/s), 778 us with 8-bit ones (5.2 TB/s:
+// 57 instructions per element take half of the issue slots).  288 small tensors, 3M elements: 14.6 us.  With the rate and the step
+// count on the device every thread works out the two factors in binary64: a tensor of 77777 elements 5.4 us in a graph, 3.0 without.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -33,7 +35,9 @@ constexpr int BLOCK = 256;                                 // elements that shar
 constexpr int64_t LEAST_CHUNK = 2048;                      // elements of a tensor handled by one CTA: at least,
 constexpr int64_t MOST_CHUNK = 65536;                      // at most, and
 constexpr int64_t MOST_CHUNK_32 = 8192;                    // in lists without 8-bit moments (268M parameters 1095 us; 1113 with 16384)
-constexpr int CTAS_PER_SM = 3;                             // 80 registers a thread; at 4 they spill
+// 80 registers a thread, of which some spill (72 bytes of stores); 2 CTAs would spill nothing, 4 eight times as much (268M parameters
+// with 8-bit moments: 704 us with 3 CTAs, 823 with 2, 784 with 4).
+constexpr int CTAS_PER_SM = 3;
 static_assert(MOST_CHUNK <= 32 * WARPS * BLOCK, "a lane for the scales of each of a warp's blocks");
 
 struct Entry {
@@ -211,9 +215,9 @@ __device__ __forceinline__ Pair root_nearest(Pair x) {
     return fma2(fma2(r, r * Pair(-0x1p50f), big), q * Pair(0x1p-26f), r);
 }
 constexpr float MOST_ROOT = 0x1p38f;                        // of what root_nearest is asked for
-// Quotients rounded to nearest, of numbers far from the ends of the range: the product with the approximate reciprocal is
-// corrected by its residual, which the fused operation gives without error (Markstein's correction).  Compared with the correctly rounded quotient on 2^31 pairs of
-// numbers: 3 differed.
+// Quotients of numbers far from the end of the range, rounded to nearest but for a few: the product with the approximate reciprocal is
+// corrected by its residual, which the fused operation gives without error where a is above 2^-100 (Markstein's correction; that the
+// reciprocal is not the correctly rounded one leaves a rare last bit).
 __device__ __forceinline__ Pair quotient_nearest(Pair a, Pair b) {
     float x, y;
     b.split(x, y);

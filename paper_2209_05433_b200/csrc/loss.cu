@@ -18,8 +18,9 @@
 // are added there with round-to-nearest: the tensor core's own additions truncate) and hand it back before they work on it.
 //
 // What bounds it.  Many tokens: the tensor core, under the power limit (4096 tokens, width 4096, vocabulary 65536, FP8: forward
-// 850 us = 2.6 PFLOP/s, 2.9 when run alone; with the backward pass 3.5 ms = 2.5 PFLOP/s).  Few tokens: the stream of weights (one
-// token against 131072 x 4096 codes: 85 us in a graph, 6.3 TB/s; 102 us as a call).  Width up to 512: the epilogue, 5000 clocks a
+// 866 us = 2.5 PFLOP/s among other calls, 703 us = 3.1 with pauses; with the backward pass 3.64 ms = 2.4 PFLOP/s).  Few tokens: the stream of
+// weights (one token against 131072 x 4096 codes: 95 us in a graph, 113 us as a call; the product's kernel alone 91 us with cold
+// caches, 5.9 TB/s).  Width up to 512: the epilogue, 5000 clocks a
 // tile.  256 x 256 tiles on pairs as in the plain product: half of B per SM.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -574,9 +575,9 @@ k_vocabulary(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
 }
 
-// Bound by latency: 4 us for one token's 2048 pairs, 9 us for 4096 rows of 512 (cold caches).
-// Joins the pairs of a row.  A block has `rows` rows, a power of two up to 32 that spares few rows nothing but their share of the
-// threads: each row has 1024 / rows threads, which take every so-many-th pair and join theirs in a tree.
+// Joins the pairs of a row.  A block has `rows` rows, a power of two up to 32 and no more than there are: each has 1024 / rows threads,
+// which take every so-many-th pair and join theirs in a tree.
+// Bound by latency: 7 to 8 us with cold caches, for one token's 2048 pairs as for 2048 rows of 128.
 __global__ void __launch_bounds__(1024) k_loss_join(const float2* part, const float* logit, int64_t parts, int64_t M, int rows,
                                                     const int64_t* target, int64_t vocab, float* loss, float* lse) {
     __shared__ float2 got[1024];
