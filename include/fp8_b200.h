@@ -503,7 +503,7 @@ fp8_status fp8_grad_clip(const fp8_clip_plan* plan, const void* table_dev, void*
  *   m holds the first moment, rounded to nearest;
  *   v holds the SQUARE ROOT of the second moment, rounded up or down with the probability of its distance (to nearest it would
  *     stand still: with beta2 near 1 it moves less than half a step at a time); one that is not zero keeps at least code 1.
- *   A first moment's scale below 2^-126 has few bits, and is 0 for a top below 3.2e-43.  For a top below 2^-119 the codes are
+ *   A first moment's scale below 2^-126 has few bits, and is 0 for a top of 3.1e-43 or less.  For a top below 2^-119 the codes are
  *     those of (m * 2^100) * (1 / (scale * 2^100)), so that code * scale is m as nearly as the scale allows, or 0 where the scale is.
  * With independent normal gradients v's root then scatters around its exact value by 9 % (beta2 = 0.9), 11 % (0.95), 15 % (0.99) or
  * 16 % (0.999) of it, its square is 1 to 5 % high in the mean, and the updates differ by 8 to 14 % of their mean from those
@@ -578,7 +578,7 @@ fp8_status fp8_adamw_step(const fp8_adamw_plan* plan, const void* table_dev, voi
  * that token's row of dx and all of dw NaN or (bf16) infinite.
  * Precision: products are exact, their sums as FP8_ACC_SPLIT; exponentials by the hardware (2 ulp).  z and lse are binary32
  * numbers, so exp(z - lse) may be off by 2^-24 |lse| of itself; but where one logit of a row stands alone, lse is that number,
- * and dz is exactly dloss or 0, as the backward pass adds up the same z.  A row with a NaN or a
+ * and dz is exactly dloss, -dloss or 0, as a backward pass of the same descriptor adds up the same z.  A row with a NaN or a
  * plus-infinite logit gives NaN; a row of minus infinities has lse = -inf.
  * fp8_cross_entropy_backward reads the lse that the forward pass wrote and the per-token factors dloss (1/tokens for a mean).
  * dx and dw are OVERWRITTEN; either may be NULL.  tokens == 0: dw = 0, nothing else is touched.  width and vocab are at least 1.
